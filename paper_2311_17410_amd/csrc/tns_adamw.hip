@@ -1,0 +1,256 @@
+// AdamW over all tensors of a model in one launch, states in 32 or in 8 bits (include/tns_train.h).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <new>
+#include <vector>
+
+#include "../../include/tns_train.h"
+#include "tns_internal.h"
+#include "tns_values.h"
+
+using tns::as_float;
+using tns::as_value;
+using tns::bf16;
+using tns::DeviceGuard;
+using tns::fail;
+using tns::fail_hip;
+
+namespace {
+
+constexpr int kBlock = 256;           // weights that share a scale: four per lane of a wave
+constexpr int kTile = 4096;           // weights per workgroup of four waves
+constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull, kMix1 = 0xBF58476D1CE4E5B9ull, kMix2 = 0x94D049BB133111EBull;
+
+__host__ __device__ inline uint64_t mix64(uint64_t z) {        // output function of splitmix64
+    z = (z ^ (z >> 30)) * kMix1;
+    z = (z ^ (z >> 27)) * kMix2;
+    return z ^ (z >> 31);
+}
+
+struct Tensor {
+    float* param;
+    bf16* copy;
+    const void* grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t n;
+    uint64_t word0;                   // number of the random word of its first four weights
+    float decay;
+};
+
+struct Tile {
+    int32_t tensor;
+    uint32_t index;                   // of the tile in its tensor
+};
+
+struct Step {                         // factors of one step, rounded to fp32 once
+    float beta1, rest1, beta2, rest2, lr, rate, root, eps;
+    uint64_t key;
+};
+
+// Largest of the wave's values, as the bits of magnitudes (a NaN is larger than everything).
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+    for (int by = 32; by; by >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, by));
+    return v;
+}
+
+// Four codes and their values.
+__device__ __forceinline__ void from_codes(uint32_t codes, float scale, float (&v)[4]) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    v[0] = lo[0] * scale; v[1] = lo[1] * scale; v[2] = hi[0] * scale; v[3] = hi[1] * scale;
+}
+
+// The wave's 256 values as codes; `valid`: how many of the lane's four exist (the others are 0 and stay 0).
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t to_codes(const float (&v)[4], uint64_t random, float& scale) {
+#pragma clang fp contract(off)
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+    top = wave_max(top);
+    float t = __uint_as_float(top);
+    if (t < 0x1p-100f) { scale = 0.0f; return 0; }
+    scale = t * (1.0f / 448.0f);
+    const float by = 448.0f / t;
+    uint32_t codes = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float y = v[j] * by;
+        if (!SIGNED) y = fmaxf(y, 0x1p-6f);
+        const uint32_t bits = __float_as_uint(y), size = bits & 0x7fffffffu;
+        uint32_t code = ((size + ((uint32_t)(random >> (16 * j)) & 0xffffu) * 16u) >> 20) - (120u << 3);
+        code = size < (121u << 23) ? 0u : (min(code, 0x7eu) | (SIGNED ? bits >> 24 & 0x80u : 0u));
+        codes |= code << (8 * j);
+    }
+    return codes;
+}
+
+template <int BITS, typename G>
+__global__ void __launch_bounds__(256) k_adamw(const Tensor* __restrict__ tensors, const Tile* __restrict__ tiles, const Step s, const float* __restrict__ grad_scale) {
+#pragma clang fp contract(off)
+    const float gs = grad_scale ? *grad_scale : 1.0f;
+    if (gs == 0.0f || !(fabsf(gs) <= 3.402823466e+38f)) return;
+    const Tile tile = tiles[blockIdx.x];
+    const Tensor t = tensors[tile.tensor];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float keep = 1.0f - s.lr * t.decay;
+    for (int j = 0; j < kTile / kBlock / 4; ++j) {
+        const int64_t block = (int64_t)tile.index * (kTile / kBlock) + wave * (kTile / kBlock / 4) + j, i0 = block * kBlock + lane * 4;
+        if (block * kBlock >= t.n) return;
+        const int n = (int)min(max(t.n - i0, (int64_t)0), (int64_t)4);
+        float g[4] = {}, m[4] = {}, v[4] = {}, r[4], p[4] = {};
+        uint32_t mc = 0, vc = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < n) {
+                g[k] = as_float(static_cast<const G*>(t.grad)[i0 + k]) * gs;
+                p[k] = t.param[i0 + k];
+                if (BITS == 32) {
+                    m[k] = static_cast<const float*>(t.m)[i0 + k];
+                    v[k] = static_cast<const float*>(t.v)[i0 + k];
+                } else {
+                    mc |= (uint32_t)static_cast<const uint8_t*>(t.m)[i0 + k] << (8 * k);
+                    vc |= (uint32_t)static_cast<const uint8_t*>(t.v)[i0 + k] << (8 * k);
+                }
+            }
+        if (BITS == 8) {
+            from_codes(mc, t.m_scale[block], m);
+            from_codes(vc, t.v_scale[block], r);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = r[k] * r[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            m[k] = s.beta1 * m[k] + s.rest1 * g[k];
+            v[k] = s.beta2 * v[k] + s.rest2 * (g[k] * g[k]);
+            r[k] = sqrtf(v[k]);
+            p[k] = p[k] * keep - (s.rate * m[k]) / (r[k] * s.root + s.eps);
+            if (k >= n) m[k] = r[k] = 0.0f;
+        }
+        if (BITS == 8) {
+            const uint64_t random = mix64(s.key + kGolden * (t.word0 + (uint64_t)(i0 >> 2) + 1));
+            float ms, vs;
+            mc = to_codes<true>(m, random, ms);
+            vc = to_codes<false>(r, random, vs);
+            if (lane == 0) { t.m_scale[block] = ms; t.v_scale[block] = vs; }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < n) {
+                t.param[i0 + k] = p[k];
+                if (t.copy) t.copy[i0 + k] = as_value<bf16>(p[k]);
+                if (BITS == 32) {
+                    static_cast<float*>(t.m)[i0 + k] = m[k];
+                    static_cast<float*>(t.v)[i0 + k] = v[k];
+                } else {
+                    static_cast<uint8_t*>(t.m)[i0 + k] = (uint8_t)(mc >> (8 * k));
+                    static_cast<uint8_t*>(t.v)[i0 + k] = (uint8_t)(vc >> (8 * k));
+                }
+            }
+    }
+}
+
+}  // namespace
+
+struct tns_adamw {
+    tns_adamw_config cfg;
+    Tensor* tensors = nullptr;
+    Tile* tiles = nullptr;
+    int64_t num_tiles = 0;
+};
+
+extern "C" {
+
+int tns_adamw_create(const tns_adamw_config* cfg, int32_t count, const tns_adamw_tensor* tensors, tns_adamw** out) {
+    tns::clear_error();
+    if (!cfg || !out || (count > 0 && !tensors)) return fail(TNS_EINVAL, "null configuration, tensors or output pointer");
+    if (count < 0) return fail(TNS_EINVAL, "negative number of tensors");
+    if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return fail(TNS_EINVAL, "beta1 and beta2 must be in [0, 1)");
+    if (!(cfg->eps >= 0.0 && std::isfinite(cfg->eps))) return fail(TNS_EINVAL, "eps must be finite and not negative");
+    if (cfg->state_bits != 8 && cfg->state_bits != 32) return fail(TNS_EINVAL, "states have 8 or 32 bits");
+    if (cfg->grad_dtype != TNS_F32 && cfg->grad_dtype != TNS_BF16) return fail(TNS_EINVAL, "unknown grad_dtype");
+    if (cfg->device < 0 || cfg->reserved) return fail(TNS_EINVAL, "negative device ordinal or reserved field in use");
+    int64_t total = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const tns_adamw_tensor& t = tensors[i];
+        if (t.n < 0) return fail(TNS_EINVAL, "negative number of weights");
+        if (t.n > (int64_t)1 << 40) return fail(TNS_ESIZE, "more than 2^40 weights in one tensor");
+        if (t.n && (!t.d_param || !t.d_grad || !t.d_m || !t.d_v)) return fail(TNS_EINVAL, "null weights, gradient or state");
+        if (t.n && cfg->state_bits == 8 && (!t.d_m_scale || !t.d_v_scale)) return fail(TNS_EINVAL, "null scales of a state of 8 bits");
+        if (!std::isfinite(t.weight_decay)) return fail(TNS_EINVAL, "weight_decay must be finite");
+        total += (t.n + kTile - 1) / kTile;
+        if (total > (int64_t)INT32_MAX) return fail(TNS_ESIZE, "more than 2^43 weights in all");
+    }
+    DeviceGuard guard(cfg->device);
+    if (guard.error() != hipSuccess) return fail_hip(guard.error(), "selecting the optimizer's device");
+    tns_adamw* opt = nullptr;
+    try {
+        opt = new tns_adamw();
+        opt->cfg = *cfg;
+        opt->num_tiles = total;
+        std::vector<Tensor> ts;
+        std::vector<Tile> tiles;
+        ts.reserve(count);
+        tiles.reserve(total);
+        uint64_t word = 0;
+        for (int32_t i = 0; i < count; ++i) {
+            const tns_adamw_tensor& t = tensors[i];
+            ts.push_back({t.d_param, static_cast<bf16*>(t.d_copy), t.d_grad, t.d_m, t.d_v, t.d_m_scale, t.d_v_scale, t.n, word, (float)t.weight_decay});
+            for (int64_t k = 0; k * kTile < t.n; ++k) tiles.push_back({i, (uint32_t)k});
+            word += (uint64_t)((t.n + kBlock - 1) / kBlock) * (kBlock / 4);
+        }
+        if (total) {
+            hipError_t e = tns::device_malloc((void**)&opt->tensors, ts.size() * sizeof(Tensor));
+            if (e == hipSuccess) e = tns::device_malloc((void**)&opt->tiles, tiles.size() * sizeof(Tile));
+            if (e == hipSuccess) e = hipMemcpy(opt->tensors, ts.data(), ts.size() * sizeof(Tensor), hipMemcpyHostToDevice);
+            if (e == hipSuccess) e = hipMemcpy(opt->tiles, tiles.data(), tiles.size() * sizeof(Tile), hipMemcpyHostToDevice);
+            if (e != hipSuccess) {
+                tns_adamw_destroy(opt);
+                return fail_hip(e, "copying the optimizer's tables");
+            }
+        }
+    } catch (const std::bad_alloc&) {
+        tns_adamw_destroy(opt);
+        return fail(TNS_ENOMEM, "host allocation failed");
+    }
+    *out = opt;
+    return TNS_OK;
+}
+
+int tns_adamw_step(tns_adamw* opt, double lr, int64_t t, const float* d_grad_scale, void* hip_stream) {
+    tns::clear_error();
+    if (!opt) return fail(TNS_EINVAL, "null optimizer");
+    if (t < 1) return fail(TNS_EINVAL, "steps count from 1");
+    if (!std::isfinite(lr)) return fail(TNS_EINVAL, "lr must be finite");
+    if (opt->num_tiles == 0) return TNS_OK;
+    DeviceGuard guard(opt->cfg.device);
+    if (guard.error() != hipSuccess) return fail_hip(guard.error(), "selecting the optimizer's device");
+    const tns_adamw_config& c = opt->cfg;
+    const Step s{(float)c.beta1, (float)(1.0 - c.beta1), (float)c.beta2, (float)(1.0 - c.beta2), (float)lr,
+                 (float)(lr / (1.0 - std::pow(c.beta1, (double)t))), (float)(1.0 / std::sqrt(1.0 - std::pow(c.beta2, (double)t))), (float)c.eps,
+                 mix64(c.seed + kGolden * (uint64_t)t)};
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)opt->num_tiles), dim3(256), 0, static_cast<hipStream_t>(hip_stream), opt->tensors, opt->tiles, s, d_grad_scale);
+    };
+    if (c.state_bits == 32) c.grad_dtype == TNS_F32 ? launch(k_adamw<32, float>) : launch(k_adamw<32, bf16>);
+    else c.grad_dtype == TNS_F32 ? launch(k_adamw<8, float>) : launch(k_adamw<8, bf16>);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? (int)TNS_OK : fail_hip(e, "tns_adamw_step");
+}
+
+int tns_adamw_destroy(tns_adamw* opt) {
+    if (!opt) return TNS_OK;
+    DeviceGuard guard(opt->cfg.device);
+    if (guard.error() == hipSuccess) {
+        (void)hipDeviceSynchronize();
+        if (opt->tensors) (void)hipFree(opt->tensors);
+        if (opt->tiles) (void)hipFree(opt->tiles);
+    }
+    delete opt;
+    return TNS_OK;
+}
+
+}  // extern "C"
