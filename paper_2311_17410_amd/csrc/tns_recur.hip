@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/tns_train.h"
 #include "tns_internal.h"
@@ -19,11 +20,54 @@ using tns::kLog2e;
 
 namespace {
 
-constexpr int kSaved = 16;            // rows from one saved state to the next
-constexpr int kGroups = 1024;         // workgroups that share the lists of a gradient
+constexpr int kWave = 64, kWaves = 4;  // lanes of a wave, waves of a workgroup
+constexpr int kSaved = 16;             // rows from one saved state to the next, and rows that a wave has in its registers
+constexpr int kBatch = 64;             // rows whose lists and gaps the lanes of a wave hold
 
+// Values of the V channels of a lane, as they lie in memory.
+template <typename T, int V> struct Pack;
+template <> struct Pack<float, 1> {
+    float raw;
+    __device__ float get(int) const { return raw; }
+    __device__ void set(int, float v) { raw = v; }
+};
+template <> struct Pack<bf16, 1> {
+    bf16 raw;
+    __device__ float get(int) const { return as_float(raw); }
+    __device__ void set(int, float v) { raw = as_value<bf16>(v); }
+};
+template <> struct Pack<bf16, 2> {
+    uint32_t raw;
+    __device__ float get(int i) const { return __uint_as_float(i ? raw & 0xffff0000u : raw << 16); }
+    __device__ void set(int i, float v) { raw = i ? (raw & 0xffffu) | (uint32_t)as_value<bf16>(v).bits << 16 : (uint32_t)as_value<bf16>(v).bits; }
+};
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load(const T* p) { return *reinterpret_cast<const Pack<T, V>*>(p); }
+template <typename T, int V>
+__device__ __forceinline__ void store(T* p, const float (&v)[V]) {
+    Pack<T, V> k;
+#pragma unroll
+    for (int i = 0; i < V; ++i) k.set(i, v[i]);
+    *reinterpret_cast<Pack<T, V>*>(p) = k;
+}
+template <int V>
+__device__ __forceinline__ void load_floats(const float* p, float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = p ? p[i] : 0.0f;
+}
+template <int V>
+__device__ __forceinline__ void store_floats(float* p, const float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = v[i];
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float read_lane(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+
+// The lists (tns_recur with its types) as one walk over all events: place p of the walk is row p, or, newest first, row total - 1 - p; the
+// j-th list of the walk is list j or S - 1 - j.  Whatever rowptr holds, a place below `total` has a row below `rows` and a list below S.
 template <typename T>
-struct Lists {                        // tns_recur with its types
+struct Lists {
     int64_t S, rows;
     const int64_t* rowptr;
     const T *u, *x;
@@ -31,95 +75,429 @@ struct Lists {                        // tns_recur with its types
     const float *ts, *decay, *h0, *t0;
     int dim;
     bool newest_first;
+
+    __device__ int64_t total() const { return min(max(rowptr[S], (int64_t)0), rows); }
+    __device__ int64_t begin_of(int64_t j, int64_t total) const {         // 0 <= j <= S
+        const int64_t at = min(max(rowptr[newest_first ? S - j : j], (int64_t)0), total);
+        return newest_first ? total - at : at;
+    }
+    __device__ int64_t row(int64_t p, int64_t total) const { return newest_first ? total - 1 - p : p; }
+    __device__ int64_t list(int64_t j) const { return newest_first ? S - 1 - j : j; }
+    __device__ const float* h0_of(int64_t j) const { return h0 ? h0 + list(j) * dim : nullptr; }
 };
 
-// Rows of a list in the order of time: row(i) for i = 0 .. n-1, and the place of that event in the walk over all lists.
-struct Walk {
-    int64_t begin, n, total;
-    bool newest_first;
-    template <typename T>
-    __device__ Walk(const Lists<T>& l, int64_t s) : newest_first(l.newest_first) {
-        total = min(max(l.rowptr[l.S], (int64_t)0), l.rows);
-        begin = min(max(l.rowptr[s], (int64_t)0), total);
-        n = min(max(l.rowptr[s + 1], begin), total) - begin;
+// The list that holds place p: the last one that begins at or before it.  Called by the whole wave, which looks at 64 lists a step.
+template <typename T>
+__device__ int find_list(const Lists<T>& l, int64_t total, int64_t p) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = l.S;
+    while (hi - lo > 1) {
+        const int64_t by = (hi - lo + kWave - 1) / kWave, j = lo + (lane + 1) * by;
+        const int64_t c = __popcll(__ballot(j < hi && l.begin_of(j, total) <= p));
+        lo += c * by;
+        hi = min(lo + by, hi);
     }
-    __device__ int64_t row(int64_t i) const { return newest_first ? begin + n - 1 - i : begin + i; }
-    __device__ int64_t place(int64_t i) const { return newest_first ? total - 1 - row(i) : row(i); }
+    return (int)lo;
+}
+
+// What the lanes know of the 64 places from p0 on: lane i the list of place p0 + i; bit i of `starts` and `ends`, whether that place is
+// the first and the last of its list (places from total on: neither).
+struct Batch {
+    int list;
+    uint64_t starts, ends;
 };
 
-template <typename T>
-__device__ float gap_at(const Lists<T>& l, const Walk& w, int64_t s, int64_t i) {
-    const float t = l.ts[w.row(i)];
-    return gap_of(t, i ? l.ts[w.row(i - 1)] : l.t0 ? l.t0[s] : t);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256) k_recur_run(const Lists<T> l, T* h_out, int64_t ld_h, float* last, float* saved) {
-    const int64_t s = blockIdx.x;
-    const Walk w(l, s);
-    for (int c = threadIdx.x; c < l.dim; c += 256) {
-        float h = l.h0 ? l.h0[s * l.dim + c] : 0.0f;
-        const float rate = l.ts ? -kLog2e * l.decay[c] : 0.0f;
-        for (int64_t i = 0; i < w.n; ++i) {
-            const int64_t r = w.row(i);
-            if (saved && w.place(i) % kSaved == 0) saved[w.place(i) / kSaved * l.dim + c] = h;
-            float z, f;
-            gate_of(as_float(l.u[r * l.ld_u + c]), z, f);
-            if (l.ts) f *= __builtin_amdgcn_exp2f(rate * gap_at(l, w, s, i));
-            h = f * h + z * as_float(l.x[r * l.ld_x + c]);
-            if (h_out) h_out[r * ld_h + c] = as_value<T>(h);
-        }
-        if (last) last[s * l.dim + c] = h;
-    }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256) k_recur_grad(const Lists<T> l, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
-                                                    T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
-    for (int c = threadIdx.x; c < l.dim; c += 256) {
-        float sum = 0.0f;
-        const float rate = l.ts ? -kLog2e * l.decay[c] : 0.0f;
-        for (int64_t s = blockIdx.x; s < l.S; s += gridDim.x) {
-            const Walk w(l, s);
-            float back = dlast ? dlast[s * l.dim + c] : 0.0f;
-            int64_t end = w.n;
-            while (end > 0) {
-                const int64_t first = max(end - 1 - w.place(end - 1) % kSaved, (int64_t)0);
-                float before[kSaved], h = w.place(first) % kSaved == 0 && first ? saved[w.place(first) / kSaved * l.dim + c] : l.h0 ? l.h0[s * l.dim + c] : 0.0f;
-                for (int64_t i = first; i < end; ++i) {
-                    before[i - first] = h;
-                    float z, f;
-                    gate_of(as_float(l.u[w.row(i) * l.ld_u + c]), z, f);
-                    if (l.ts) f *= __builtin_amdgcn_exp2f(rate * gap_at(l, w, s, i));
-                    h = f * h + z * as_float(l.x[w.row(i) * l.ld_x + c]);
-                }
-                for (int64_t i = end - 1; i >= first; --i) {
-                    const int64_t r = w.row(i);
-                    float z, rest;
-                    gate_of(as_float(l.u[r * l.ld_u + c]), z, rest);
-                    const float gap = l.ts ? gap_at(l, w, s, i) : 0.0f;
-                    const float f = l.ts ? rest * __builtin_amdgcn_exp2f(rate * gap) : rest;
-                    if (dh) back += as_float(dh[r * ld_dh + c]);
-                    dx[r * ld_dx + c] = as_value<T>(z * back);
-                    const float keep = f * before[i - first];
-                    du[r * ld_du + c] = as_value<T>(z * back * (rest * as_float(l.x[r * l.ld_x + c]) - keep));
-                    sum -= back * keep * gap;
-                    back *= f;
-                }
-                end = first;
+// From the list that holds the first place (FORWARD) or the last one that there is (otherwise) to those of all.
+template <bool FORWARD, typename T>
+__device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, int64_t p0, int from) {
+    const int lane = threadIdx.x & 63;
+    int passed = 0;                    // borders between the place that is known and the lane's
+    for (int64_t base = from;; base += FORWARD ? kWave : -kWave) {
+        // The next 64 borders, as places of the batch: list base + 1 + lane begins there, or list base - lane.
+        const int64_t j = FORWARD ? base + 1 + lane : base - lane;
+        const bool is = FORWARD ? j < l.S : j > 0;
+        const int64_t rel = is ? l.begin_of(j, total) - p0 : FORWARD ? kBatch : 0;
+        const int at = (int)min(max(rel, (int64_t)0), (int64_t)kBatch);
+        const bool inside = FORWARD ? at < kBatch : at > 0;
+        const uint64_t some = __ballot(inside);
+        if (some) {                    // borders in order: how many lie at or before the lane's place (beyond it)
+            int n = 0;
+#pragma unroll
+            for (int by = 32; by; by >>= 1) {
+                const int border = __shfl(at, n + by - 1);
+                if (FORWARD ? border <= lane : border > lane) n += by;
             }
-            if (dh0) dh0[s * l.dim + c] = back;
+            const int border = __shfl(at, 63);
+            if (n == 63 && (FORWARD ? border <= lane : border > lane)) n = 64;
+            passed += n;
         }
-        if (sums) sums[(int64_t)blockIdx.x * l.dim + c] = sum;
+        if (some != ~0ull) break;
+    }
+    Batch b;
+    b.list = (int)min(max((int64_t)from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
+    const int64_t p = p0 + lane;
+    const bool first = p < total && l.begin_of(b.list, total) == p, last = p < total && l.begin_of((int64_t)b.list + 1, total) == p + 1;
+    b.starts = __ballot(first);
+    b.ends = __ballot(last);
+    return b;
+}
+
+// Gap before the event of lane's place.
+template <typename T>
+__device__ __forceinline__ float gap_at(const Lists<T>& l, int64_t total, int64_t p0, const Batch& b) {
+    const int lane = threadIdx.x & 63;
+    const int64_t p = min(p0 + lane, total - 1);
+    const float t = l.ts[l.row(p, total)];
+    if (b.starts >> lane & 1) return l.t0 ? gap_of(t, l.t0[l.list(b.list)]) : 0.0f;
+    return gap_of(t, l.ts[l.row(max(p - 1, (int64_t)0), total)]);
+}
+
+// f and z of a lane's channels.
+template <int V, bool DECAY, typename P>
+__device__ __forceinline__ void gates(const P& u, const float (&rate)[V], float gap, float (&z)[V], float (&rest)[V], float (&f)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        gate_of(u.get(i), z[i], rest[i]);
+        f[i] = DECAY ? rest[i] * __builtin_amdgcn_exp2f(rate[i] * gap) : rest[i];
     }
 }
 
-__global__ void __launch_bounds__(256) k_recur_sums(const float* sums, int groups, int dim, float* out) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= dim) return;
+// The wave's share of the work: rows of a tile, V channels a lane.  Lanes beyond the last channel repeat it (they store what it stores).
+template <int V>
+struct Unit {
+    int64_t tile;
+    int c;
+    __device__ Unit(int dim, int blocks, int64_t wave) {
+        tile = wave / blocks;
+        c = min((int)(wave % blocks) * kWave * V + (int)(threadIdx.x & 63) * V, dim - V);
+    }
+};
+__device__ __forceinline__ int64_t wave_id() { return (int64_t)blockIdx.x * kWaves + uniform(threadIdx.x >> 6); }
+
+template <typename T, int V>
+struct Group {                          // rows of a group as they were read
+    Pack<T, V> u[kSaved], x[kSaved];
+};
+// Reads n rows from place p on (n may be less than a group: the last row again).
+template <typename T, int V, bool FIRST, bool SECOND>
+__device__ __forceinline__ void read_rows(Pack<T, V> (&a)[kSaved], Pack<T, V> (&b)[kSaved], const Lists<T>& l, const T* first, int64_t ld_first, const T* second,
+                                          int64_t ld_second, int64_t total, int64_t p, int c) {
+#pragma unroll
+    for (int r = 0; r < kSaved; ++r) {
+        const int64_t row = l.row(max(min(p + r, total - 1), (int64_t)0), total);
+        if (FIRST) a[r] = load<T, V>(first + row * ld_first + c);
+        if (SECOND) b[r] = load<T, V>(second + row * ld_second + c);
+    }
+}
+
+// Rate of the decay in powers of two.
+template <int V, bool DECAY, typename T>
+__device__ __forceinline__ void rates(const Lists<T>& l, int c, float (&rate)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) rate[i] = DECAY ? -kLog2e * l.decay[c + i] : 0.0f;
+}
+
+// ---- carries -------------------------------------------------------------------------------------------
+// The walk is cut into tiles.  carry[k] is what enters tile k: the state before its first event, or (backward) what the events after its
+// last one send back.  A tile whose part of the crossing list begins (ends) inside it knows what it hands on (closed); one that lies
+// inside a list altogether hands on A * what enters + B (open): it writes B as the carry and A beside it, and k_recur_join puts them together.
+
+template <typename T, int V, bool DECAY>
+__global__ void __launch_bounds__(256) k_recur_tails(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, float* carry, float* factor, uint8_t* open) {
+    const int64_t wave = wave_id();
+    const Unit<V> w(l.dim, blocks, wave);
+    if (w.tile >= tiles - 1) return;
+    const int64_t total = l.total(), begin = w.tile * tile_rows, end = begin + tile_rows;
+    bool is_open = false;
+    if (end < total) {
+        const int j = find_list(l, total, end - 1);
+        const int64_t first = l.begin_of(j, total);
+        if (l.begin_of((int64_t)j + 1, total) > end) {
+            is_open = first < begin;
+            float rate[V], h[V], a[V];
+            rates<V, DECAY>(l, w.c, rate);
+            load_floats<V>(is_open || !l.h0 ? nullptr : l.h0_of(j) + w.c, h);
+#pragma unroll
+            for (int i = 0; i < V; ++i) a[i] = 1.0f;
+            Pack<T, V> u[kSaved], x[kSaved];
+            for (int64_t p = max(first, begin); p < end; p += kSaved) {
+                read_rows<T, V, true, true>(u, x, l, l.u, l.ld_u, l.x, l.ld_x, total, p, w.c);
+                float gap = 0.0f;
+                if (DECAY) {
+                    const int64_t q = min(p + (threadIdx.x & (kSaved - 1)), end - 1);
+                    const float t = l.ts[l.row(q, total)];
+                    gap = q == first ? l.t0 ? gap_of(t, l.t0[l.list(j)]) : 0.0f : gap_of(t, l.ts[l.row(q - 1, total)]);
+                }
+                const int n = (int)min(end - p, (int64_t)kSaved);
+#pragma unroll
+                for (int r = 0; r < kSaved; ++r) {
+                    if (r >= n) continue;
+                    float z[V], rest[V], f[V];
+                    gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, r) : 0.0f, z, rest, f);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        h[i] = f[i] * h[i] + z[i] * x[r].get(i);
+                        a[i] *= f[i];
+                    }
+                }
+            }
+            store_floats<V>(carry + (w.tile + 1) * l.dim + w.c, h);
+            if (is_open) store_floats<V>(factor + (w.tile + 1) * l.dim + w.c, a);
+        }
+    }
+    if (wave % blocks == 0 && (threadIdx.x & 63) == 0) open[w.tile + 1] = is_open;
+}
+
+template <typename T, int V, bool DECAY>
+__global__ void __launch_bounds__(256) k_recur_heads(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, const T* dh, int64_t ld_dh, const float* dlast,
+                                                     float* carry, float* factor, uint8_t* open) {
+    const int64_t wave = wave_id();
+    const Unit<V> w(l.dim, blocks, wave);
+    if (w.tile >= tiles - 1) return;
+    const int64_t total = l.total(), begin = (w.tile + 1) * tile_rows;      // (tile 0 has nothing before it)
+    bool is_open = false;
+    if (begin < total) {
+        const int j = find_list(l, total, begin);
+        if (l.begin_of(j, total) < begin) {
+            const int64_t last = l.begin_of((int64_t)j + 1, total), end = min(last, begin + tile_rows);
+            is_open = end < last;
+            float rate[V], back[V], a[V];
+            rates<V, DECAY>(l, w.c, rate);
+            load_floats<V>(is_open || !dlast ? nullptr : dlast + l.list(j) * l.dim + w.c, back);
+#pragma unroll
+            for (int i = 0; i < V; ++i) a[i] = 1.0f;
+            Pack<T, V> u[kSaved], d[kSaved];
+            for (int64_t p = begin + (end - 1 - begin) / kSaved * kSaved; p >= begin; p -= kSaved) {
+                read_rows<T, V, true, false>(u, d, l, l.u, l.ld_u, l.u, 0, total, p, w.c);
+                if (dh) read_rows<T, V, false, true>(u, d, l, l.u, 0, dh, ld_dh, total, p, w.c);
+                float gap = 0.0f;
+                if (DECAY) {
+                    const int64_t q = min(p + (threadIdx.x & (kSaved - 1)), end - 1);
+                    gap = gap_of(l.ts[l.row(q, total)], l.ts[l.row(q - 1, total)]);      // (the list's first event is not here)
+                }
+                const int n = (int)min(end - p, (int64_t)kSaved);
+#pragma unroll
+                for (int r = kSaved - 1; r >= 0; --r) {
+                    if (r >= n) continue;
+                    float z[V], rest[V], f[V];
+                    gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, r) : 0.0f, z, rest, f);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if (dh) back[i] += d[r].get(i);
+                        back[i] *= f[i];
+                        a[i] *= f[i];
+                    }
+                }
+            }
+            store_floats<V>(carry + w.tile * l.dim + w.c, back);
+            if (is_open) store_floats<V>(factor + w.tile * l.dim + w.c, a);
+        }
+    }
+    if (wave % blocks == 0 && (threadIdx.x & 63) == 0) open[w.tile] = is_open;
+}
+
+// Puts the open tiles' carries together, from tile 1 on or (BACKWARD) from the last but one down: kChannels channels a workgroup, each
+// with kParts parts of the tiles: every thread joins its part, the parts are scanned, every thread goes through its part again.
+constexpr int kChannels = 16, kParts = 1024 / kChannels;
+template <bool BACKWARD>
+__global__ void __launch_bounds__(1024) k_recur_join(int64_t tiles, int dim, float* carry, const float* factor, const uint8_t* open) {
+    __shared__ float s_a[kParts][kChannels], s_b[kParts][kChannels];
+    __shared__ int s_any;
+    if (threadIdx.x == 0) s_any = 0;
+    __syncthreads();
+    const int64_t n = tiles - 1;                            // carries that tiles have written
+    auto at = [&](int64_t i) { return BACKWARD ? n - 1 - i : i + 1; };
+    int any = 0;
+    for (int64_t i = threadIdx.x; i < n; i += 1024) any |= open[at(i)];
+    if (any) s_any = 1;
+    __syncthreads();
+    if (!s_any) return;
+    const int part = threadIdx.x / kChannels, ch = threadIdx.x % kChannels, c = min((int)blockIdx.x * kChannels + ch, dim - 1);
+    const bool mine = (int)blockIdx.x * kChannels + ch < dim;
+    const int64_t per = (n + kParts - 1) / kParts, begin = min(part * per, n), end = min(begin + per, n);
+    float a = 1.0f, b = 0.0f;                               // what the part does to the carry that enters it; a = 0 once a tile was closed
+    for (int64_t i = begin; i < end; ++i) {
+        const int64_t k = at(i);
+        const float v = carry[k * dim + c];
+        if (open[k]) {
+            const float f = factor[k * dim + c];
+            b = f * b + v;
+            a *= f;
+        } else {
+            a = 0.0f;
+            b = v;
+        }
+    }
+    s_a[part][ch] = a;
+    s_b[part][ch] = b;
+    __syncthreads();
+    float enter = 0.0f;                                     // (the first tile written is never open: no list crosses the walk's ends)
+    for (int q = 0; q < part; ++q) enter = (s_a[q][ch] == 0.0f ? 0.0f : s_a[q][ch] * enter) + s_b[q][ch];
+    for (int64_t i = begin; i < end; ++i) {
+        const int64_t k = at(i);
+        float v = carry[k * dim + c];
+        if (open[k]) {
+            v = factor[k * dim + c] * enter + v;
+            if (mine) carry[k * dim + c] = v;
+        }
+        enter = v;
+    }
+}
+
+// ---- states --------------------------------------------------------------------------------------------
+
+// Rows of an array [S, dim] that belong to lists without events: those of h0, or zero.  64 lists a wave.
+template <typename T>
+__device__ void fill_empty(const Lists<T>& l, int64_t first, const float* from, float* to) {
+    const int lane = threadIdx.x & 63;
+    const int64_t total = l.total(), s = first + lane;
+    uint64_t empty = __ballot(s < l.S && min(max(l.rowptr[min(s, l.S)], (int64_t)0), total) >= min(max(l.rowptr[min(s + 1, l.S)], (int64_t)0), total));
+    for (; empty; empty &= empty - 1) {
+        const int64_t at = (first + __ffsll((unsigned long long)empty) - 1) * l.dim;
+        for (int c = lane; c < l.dim; c += kWave) to[at + c] = from ? from[at + c] : 0.0f;
+    }
+}
+
+template <typename T, int V, bool DECAY>
+__global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, const float* carry, T* h_out, int64_t ld_h,
+                                                      float* last, float* saved) {
+    const int64_t wave = wave_id();
+    if (wave >= tiles * blocks) {
+        const int64_t first = (wave - tiles * blocks) * kWave;
+        if (last && first < l.S) fill_empty(l, first, l.h0, last);
+        return;
+    }
+    const Unit<V> w(l.dim, blocks, wave);
+    const int64_t total = l.total(), begin = w.tile * tile_rows, end = min(begin + tile_rows, total);
+    if (begin >= end) return;
+    float rate[V], h[V];
+    rates<V, DECAY>(l, w.c, rate);
+    int j = find_list(l, total, begin);
+    load_floats<V>(l.begin_of(j, total) < begin ? carry + w.tile * l.dim + w.c : nullptr, h);
+    Pack<T, V> u[kSaved], x[kSaved];
+    read_rows<T, V, true, true>(u, x, l, l.u, l.ld_u, l.x, l.ld_x, total, begin, w.c);
+    for (int64_t p0 = begin; p0 < end; p0 += kBatch) {
+        const Batch b = locate<true>(l, total, p0, j);
+        j = __builtin_amdgcn_readlane(b.list, kBatch - 1);
+        const float gap = DECAY ? gap_at(l, total, p0, b) : 0.0f;
+        for (int q = 0; q < kBatch && p0 + q < end; q += kSaved) {
+            const int64_t p = p0 + q;
+            Pack<T, V> next_u[kSaved], next_x[kSaved];
+            read_rows<T, V, true, true>(next_u, next_x, l, l.u, l.ld_u, l.x, l.ld_x, total, p + kSaved, w.c);
+            const int n = (int)min(end - p, (int64_t)kSaved);
+            const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
+            if (saved) store_floats<V>(saved + p / kSaved * l.dim + w.c, h);
+#pragma unroll
+            for (int r = 0; r < kSaved; ++r) {
+                if (r >= n) continue;
+                if (starts >> r & 1) load_floats<V>(l.h0 ? l.h0_of(__builtin_amdgcn_readlane(b.list, q + r)) + w.c : nullptr, h);
+                float z[V], rest[V], f[V];
+                gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, q + r) : 0.0f, z, rest, f);
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[i] = f[i] * h[i] + z[i] * x[r].get(i);
+                if (h_out) store<T, V>(h_out + l.row(p + r, total) * ld_h + w.c, h);
+                if (last && (ends >> r & 1)) store_floats<V>(last + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c, h);
+            }
+#pragma unroll
+            for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; }
+        }
+    }
+}
+
+// ---- gradients -----------------------------------------------------------------------------------------
+
+template <typename T, int V, bool DECAY>
+__global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, const float* carry, const float* saved, const T* dh,
+                                                     int64_t ld_dh, const float* dlast, T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
+    const int64_t wave = wave_id();
+    if (wave >= tiles * blocks) {
+        const int64_t first = (wave - tiles * blocks) * kWave;
+        if (dh0 && first < l.S) fill_empty(l, first, dlast, dh0);
+        return;
+    }
+    const Unit<V> w(l.dim, blocks, wave);
+    const int64_t total = l.total(), begin = w.tile * tile_rows, end = min(begin + tile_rows, total);
+    float sum[V] = {};
+    if (begin < end) {
+        float rate[V], back[V];
+        rates<V, DECAY>(l, w.c, rate);
+        int j = find_list(l, total, end - 1);
+        load_floats<V>(end < total && l.begin_of((int64_t)j + 1, total) > end ? carry + w.tile * l.dim + w.c : nullptr, back);
+        const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved;
+        Pack<T, V> u[kSaved], x[kSaved], d[kSaved];
+        auto read = [&](Pack<T, V>(&ru)[kSaved], Pack<T, V>(&rx)[kSaved], Pack<T, V>(&rd)[kSaved], int64_t p) {
+            read_rows<T, V, true, true>(ru, rx, l, l.u, l.ld_u, l.x, l.ld_x, total, p, w.c);
+            if (dh) read_rows<T, V, true, false>(rd, rd, l, dh, ld_dh, dh, 0, total, p, w.c);
+        };
+        read(u, x, d, last_group);
+        for (int64_t p0 = begin + (end - 1 - begin) / kBatch * kBatch; p0 >= begin; p0 -= kBatch) {
+            const Batch b = locate<false>(l, total, p0, j);
+            j = __builtin_amdgcn_readfirstlane(b.list);
+            const float gap = DECAY ? gap_at(l, total, p0, b) : 0.0f;
+            for (int q = (int)(min(end - p0, (int64_t)kBatch) - 1) / kSaved * kSaved; q >= 0; q -= kSaved) {
+                const int64_t p = p0 + q;
+                Pack<T, V> next_u[kSaved], next_x[kSaved], next_d[kSaved];
+                read(next_u, next_x, next_d, p - kSaved);
+                const int n = (int)min(end - p, (int64_t)kSaved);
+                const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
+                float h[V];
+                load_floats<V>(starts & 1 ? nullptr : saved + p / kSaved * l.dim + w.c, h);
+                // Forward through the group: dx = z back, du = slope back, and what the event keeps of the state before it.
+                float z[kSaved][V], f[kSaved][V], slope[kSaved][V], kept[kSaved][V];
+#pragma unroll
+                for (int r = 0; r < kSaved; ++r) {
+                    if (r >= n) continue;
+                    if (starts >> r & 1) load_floats<V>(l.h0 ? l.h0_of(__builtin_amdgcn_readlane(b.list, q + r)) + w.c : nullptr, h);
+                    float rest[V];
+                    gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, q + r) : 0.0f, z[r], rest, f[r]);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float in = x[r].get(i);
+                        kept[r][i] = f[r][i] * h[i];
+                        slope[r][i] = z[r][i] * (rest[i] * in - kept[r][i]);
+                        h[i] = kept[r][i] + z[r][i] * in;
+                    }
+                }
+#pragma unroll
+                for (int r = kSaved - 1; r >= 0; --r) {
+                    if (r >= n) continue;
+                    if (ends >> r & 1) load_floats<V>(dlast ? dlast + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c : nullptr, back);
+                    const float g = DECAY ? read_lane(gap, q + r) : 0.0f;
+                    float vu[V], vx[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if (dh) back[i] += d[r].get(i);
+                        vx[i] = z[r][i] * back[i];
+                        vu[i] = slope[r][i] * back[i];
+                        if (DECAY) sum[i] -= kept[r][i] * back[i] * g;
+                        back[i] *= f[r][i];
+                    }
+                    const int64_t row = l.row(p + r, total);
+                    store<T, V>(dx + row * ld_dx + w.c, vx);
+                    store<T, V>(du + row * ld_du + w.c, vu);
+                    if (dh0 && (starts >> r & 1)) store_floats<V>(dh0 + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c, back);
+                }
+#pragma unroll
+                for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; d[r] = next_d[r]; }
+            }
+        }
+    }
+    if (DECAY && sums) store_floats<V>(sums + w.tile * l.dim + w.c, sum);
+}
+
+// Sums of the tiles' shares, kChannels channels a workgroup, in a fixed order.
+__global__ void __launch_bounds__(1024) k_recur_sums(const float* sums, int64_t tiles, int dim, float* out) {
+    __shared__ float s_sum[kParts][kChannels];
+    const int part = threadIdx.x / kChannels, ch = threadIdx.x % kChannels, c = (int)blockIdx.x * kChannels + ch;
     float sum = 0.0f;
-    for (int g = 0; g < groups; ++g) sum += sums[(int64_t)g * dim + c];
-    out[c] = sum;
+    if (c < dim)
+        for (int64_t k = part; k < tiles; k += kParts) sum += sums[k * dim + c];
+    s_sum[part][ch] = sum;
+    for (int n = kParts / 2; n; n /= 2) {
+        __syncthreads();
+        if (part < n) s_sum[part][ch] += s_sum[part + n][ch];
+    }
+    if (part == 0 && c < dim) out[c] = s_sum[0][ch];
 }
 
 template <typename T>
@@ -174,8 +552,34 @@ int check_workspace(const void* p, size_t have, size_t need) {
     return TNS_OK;
 }
 
-size_t run_bytes(const tns_recur&) { return 0; }
-size_t grad_bytes(const tns_recur& r) { return (size_t)kGroups * r.dim * 4; }
+// Rows of a tile: as many as leave a wave for every place of the chip (1024 SIMDs, four waves each and more), 64 to 1024.
+int64_t tile_rows_of(int64_t rows, int dim) {
+    const int64_t blocks = (dim + kWave - 1) / kWave;
+    int64_t n = kBatch;
+    while (n < 1024 && rows / n * blocks > 8192) n *= 2;
+    return n;
+}
+
+size_t aligned(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+struct Workspace {                      // carries and factors of the tiles, which of them are open; sums in the factors' place
+    int64_t tile_rows, tiles;
+    float *carry, *factor;
+    uint8_t* open;
+    size_t bytes;
+};
+Workspace carve(const tns_recur& r, void* base) {
+    Workspace w{};
+    w.tile_rows = tile_rows_of(r.rows, r.dim);
+    w.tiles = (r.rows + w.tile_rows - 1) / w.tile_rows;
+    const size_t rows = aligned((size_t)w.tiles * r.dim * 4);
+    char* const p = static_cast<char*>(base);
+    w.carry = reinterpret_cast<float*>(p);
+    w.factor = reinterpret_cast<float*>(p + rows);
+    w.open = reinterpret_cast<uint8_t*>(p + 2 * rows);
+    w.bytes = 2 * rows + aligned((size_t)w.tiles);
+    return w;
+}
 size_t saved_bytes(const tns_recur& r) { return (size_t)((r.rows + kSaved - 1) / kSaved) * r.dim * 4; }
 
 template <typename T>
@@ -184,20 +588,62 @@ Lists<T> typed(const tns_recur& r) {
             r.d_ts, r.d_decay, r.d_h0, r.d_t0, r.dim, (r.flags & TNS_NEWEST_FIRST) != 0};
 }
 
-template <typename T>
-void launch_run(const tns_recur& r, void* h, int64_t ld_h, float* last, void* saved, hipStream_t stream) {
-    hipLaunchKernelGGL((k_recur_run<T>), dim3((unsigned)r.S), dim3(256), 0, stream, typed<T>(r), static_cast<T*>(h), ld_h, last, static_cast<float*>(saved));
+// Grid of the kernels that have a wave for every tile and block of channels, and for every 64 lists where `lists` is set.
+struct Grid {
+    int blocks;
+    unsigned tails, all;
+};
+Grid grid_of(const tns_recur& r, const Workspace& w, int V, bool lists) {
+    const int blocks = (r.dim + kWave * V - 1) / (kWave * V);
+    auto groups = [](int64_t waves) { return (unsigned)((waves + kWaves - 1) / kWaves); };
+    return {blocks, w.tiles > 1 ? groups((w.tiles - 1) * blocks) : 0, groups(w.tiles * blocks + (lists ? (r.S + kWave - 1) / kWave : 0))};
 }
 
-template <typename T>
+template <typename T, int V, bool DECAY>
+void launch_run(const tns_recur& r, void* h, int64_t ld_h, float* last, void* saved, void* workspace, hipStream_t stream) {
+    const Workspace w = carve(r, workspace);
+    const Grid g = grid_of(r, w, V, last != nullptr);
+    const Lists<T> l = typed<T>(r);
+    if (g.tails) {
+        hipLaunchKernelGGL((k_recur_tails<T, V, DECAY>), dim3(g.tails), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, w.carry, w.factor, w.open);
+        hipLaunchKernelGGL((k_recur_join<false>), dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.tiles, r.dim, w.carry, w.factor, w.open);
+    }
+    if (g.all)
+        hipLaunchKernelGGL((k_recur_states<T, V, DECAY>), dim3(g.all), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, w.carry, static_cast<T*>(h), ld_h, last,
+                           static_cast<float*>(saved));
+}
+
+template <typename T, int V, bool DECAY>
 void launch_grad(const tns_recur& r, const void* saved, const void* dh, int64_t ld_dh, const float* dlast, void* du, int64_t ld_du, void* dx,
                  int64_t ld_dx, float* ddecay, float* dh0, void* workspace, hipStream_t stream) {
-    const int groups = (int)std::min<int64_t>(r.S, kGroups);
-    float* const sums = ddecay ? static_cast<float*>(workspace) : nullptr;
-    if (groups)
-        hipLaunchKernelGGL((k_recur_grad<T>), dim3(groups), dim3(256), 0, stream, typed<T>(r), static_cast<const float*>(saved), static_cast<const T*>(dh), ld_dh,
-                           dlast, static_cast<T*>(du), ld_du, static_cast<T*>(dx), ld_dx, dh0, sums);
-    if (ddecay) hipLaunchKernelGGL(k_recur_sums, dim3((r.dim + 255) / 256), dim3(256), 0, stream, sums, groups, r.dim, ddecay);
+    const Workspace w = carve(r, workspace);
+    const Grid g = grid_of(r, w, V, dh0 != nullptr);
+    const Lists<T> l = typed<T>(r);
+    const T* const d = static_cast<const T*>(dh);
+    if (g.tails) {
+        hipLaunchKernelGGL((k_recur_heads<T, V, DECAY>), dim3(g.tails), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, d, ld_dh, dlast, w.carry, w.factor, w.open);
+        hipLaunchKernelGGL((k_recur_join<true>), dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.tiles, r.dim, w.carry, w.factor, w.open);
+    }
+    if (g.all)
+        hipLaunchKernelGGL((k_recur_grads<T, V, DECAY>), dim3(g.all), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, w.carry, static_cast<const float*>(saved), d,
+                           ld_dh, dlast, static_cast<T*>(du), ld_du, static_cast<T*>(dx), ld_dx, dh0, ddecay ? w.factor : nullptr);
+    if (ddecay) hipLaunchKernelGGL(k_recur_sums, dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.factor, w.tiles, r.dim, ddecay);
+}
+
+// Calls `go` with the type, the channels a lane has and whether there is a decay.  Two channels in 16 bits where every row allows reads of
+// four bytes and the lanes of the last wave are not fewer for it.
+template <typename F>
+void choose(const tns_recur& r, bool pairs, const F& go) {
+    const bool decay = r.d_decay && r.rows > 0;
+    auto with = [&](auto value, auto v) {
+        if (decay) go(value, v, std::true_type{});
+        else go(value, v, std::false_type{});
+    };
+    pairs = pairs && r.dim % 2 == 0 && r.ld_u % 2 == 0 && r.ld_x % 2 == 0 && !misaligned(r.d_u, 4) && !misaligned(r.d_x, 4) &&
+            (r.dim + 127) / 128 * 2 <= (r.dim + 63) / 64;
+    if (r.dtype == TNS_F32) with(float{}, std::integral_constant<int, 1>{});
+    else if (pairs) with(bf16{}, std::integral_constant<int, 2>{});
+    else with(bf16{}, std::integral_constant<int, 1>{});
 }
 
 int launched(const char* what) {
@@ -212,8 +658,8 @@ extern "C" {
 int tns_recur_workspace(const tns_recur* r, size_t* run, size_t* grad, size_t* saved) {
     tns::clear_error();
     if (int e = check(r)) return e;
-    if (run) *run = run_bytes(*r);
-    if (grad) *grad = grad_bytes(*r);
+    if (run) *run = carve(*r, nullptr).bytes;
+    if (grad) *grad = carve(*r, nullptr).bytes;
     if (saved) *saved = saved_bytes(*r);
     return TNS_OK;
 }
@@ -224,10 +670,12 @@ int tns_recur_run(const tns_recur* r, void* d_h, int64_t ld_h, float* d_h_last, 
     if (int e = check_arrays(r)) return e;
     if (d_h && ld_h < r->dim) return fail(TNS_EINVAL, "rows of h overlap");
     if (misaligned(d_saved, 256)) return fail(TNS_EINVAL, "saved states must be 256-byte aligned");
-    if (int e = check_workspace(d_workspace, workspace_bytes, run_bytes(*r))) return e;
+    if (int e = check_workspace(d_workspace, workspace_bytes, carve(*r, nullptr).bytes)) return e;
     if (r->S == 0) return TNS_OK;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    (r->dtype == TNS_F32 ? launch_run<float> : launch_run<bf16>)(*r, d_h, ld_h, d_h_last, d_saved, stream);
+    choose(*r, ld_h % 2 == 0 && !misaligned(d_h, 4), [&](auto value, auto v, auto decay) {
+        launch_run<decltype(value), v(), decay()>(*r, d_h, ld_h, d_h_last, d_saved, d_workspace, stream);
+    });
     return launched("tns_recur_run");
 }
 
@@ -239,10 +687,16 @@ int tns_recur_grad(const tns_recur* r, const void* d_saved, const void* d_dh, in
     if (misaligned(d_saved, 256)) return fail(TNS_EINVAL, "saved states must be 256-byte aligned");
     if (ld_du < r->dim || ld_dx < r->dim || (d_dh && ld_dh < r->dim)) return fail(TNS_EINVAL, "rows of dh, du or dx overlap");
     if (d_ddecay && !r->d_decay) return fail(TNS_EINVAL, "gradient of a decay that is not there");
-    if (int e = check_workspace(d_workspace, workspace_bytes, grad_bytes(*r))) return e;
+    if (int e = check_workspace(d_workspace, workspace_bytes, carve(*r, nullptr).bytes)) return e;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    (r->dtype == TNS_F32 ? launch_grad<float> : launch_grad<bf16>)(*r, d_saved, d_dh, ld_dh, d_dh_last, d_du, ld_du, d_dx, ld_dx, d_ddecay, d_dh0,
-                                                                   d_workspace, stream);
+    if (r->S == 0) {
+        if (d_ddecay) hipLaunchKernelGGL(k_recur_sums, dim3((r->dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, nullptr, 0, r->dim, d_ddecay);
+        return launched("tns_recur_grad");
+    }
+    const bool pairs = ld_du % 2 == 0 && ld_dx % 2 == 0 && (!d_dh || ld_dh % 2 == 0) && !misaligned(d_du, 4) && !misaligned(d_dx, 4) && !misaligned(d_dh, 4);
+    choose(*r, pairs, [&](auto value, auto v, auto decay) {
+        launch_grad<decltype(value), v(), decay()>(*r, d_saved, d_dh, ld_dh, d_dh_last, d_du, ld_du, d_dx, ld_dx, d_ddecay, d_dh0, d_workspace, stream);
+    });
     return launched("tns_recur_grad");
 }
 
