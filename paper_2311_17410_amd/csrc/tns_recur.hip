@@ -87,40 +87,61 @@ struct Lists {
 };
 
 // The list that holds place p: the last one that begins at or before it.  Called by the whole wave, which looks at 64 lists a step.
+// (What a ballot votes on is computed without branches here and below: behind a load that some lanes skipped, the compiler folded the
+// skipping lanes' vote away and the two sides saw different results.)
 template <typename T>
 __device__ int find_list(const Lists<T>& l, int64_t total, int64_t p) {
     const int lane = threadIdx.x & 63;
     int64_t lo = 0, hi = l.S;
     while (hi - lo > 1) {
         const int64_t by = (hi - lo + kWave - 1) / kWave, j = lo + (lane + 1) * by;
-        const int64_t c = __popcll(__ballot(j < hi && l.begin_of(j, total) <= p));
+        const int64_t at = l.begin_of(min(j, hi), total);
+        const int64_t c = __popcll(__ballot((j < hi) & (at <= p)));
         lo += c * by;
         hi = min(lo + by, hi);
     }
     return (int)lo;
 }
 
-// What the lanes know of the 64 places from p0 on: lane i the list of place p0 + i; bit i of `starts` and `ends`, whether that place is
-// the first and the last of its list (places from total on: neither).
+// What the lanes know of the 64 places from p0 on: lane i the list of place p0 + i and the gap before its event; bit i of `starts` and
+// `ends`, whether that place is the first and the last of its list.  A walk through a tile reads what it needs for the next 64 (a window of
+// the borders between lists, the times) while it is busy with these.
 struct Batch {
     int list;
+    float gap;
     uint64_t starts, ends;
 };
+struct Ahead {                          // of the batch at p0, as it was read
+    int64_t p0, from;                   // `from`: the list of the place before (FORWARD) or after the batch, or of its first (last) one
+    int border;                         // of lane i: list from + 1 + i begins at that place of the batch (FORWARD), or list from - i
+    float time;
+};
 
-// From the list that holds the first place (FORWARD) or the last one that there is (otherwise) to those of all.
 template <bool FORWARD, typename T>
-__device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, int64_t p0, int from) {
+__device__ __forceinline__ int border_at(const Lists<T>& l, int64_t total, int64_t p0, int64_t base) {
     const int lane = threadIdx.x & 63;
-    int passed = 0;                    // borders between the place that is known and the lane's
-    for (int64_t base = from;; base += FORWARD ? kWave : -kWave) {
-        // The next 64 borders, as places of the batch: list base + 1 + lane begins there, or list base - lane.
-        const int64_t j = FORWARD ? base + 1 + lane : base - lane;
-        const bool is = FORWARD ? j < l.S : j > 0;
-        const int64_t rel = is ? l.begin_of(j, total) - p0 : FORWARD ? kBatch : 0;
-        const int at = (int)min(max(rel, (int64_t)0), (int64_t)kBatch);
-        const bool inside = FORWARD ? at < kBatch : at > 0;
-        const uint64_t some = __ballot(inside);
-        if (some) {                    // borders in order: how many lie at or before the lane's place (beyond it)
+    const int64_t j = FORWARD ? base + 1 + lane : base - lane;
+    const int64_t at = l.begin_of(FORWARD ? min(j, l.S) : max(j, (int64_t)0), total) - p0;
+    const int64_t rel = FORWARD ? (j <= l.S ? at : kBatch + 1) : (j >= 0 ? at : -1);
+    return (int)min(max(rel, (int64_t)(FORWARD ? 0 : -1)), (int64_t)(kBatch + (FORWARD ? 1 : 0)));
+}
+
+template <bool FORWARD, bool DECAY, typename T>
+__device__ __forceinline__ Ahead look_ahead(const Lists<T>& l, int64_t total, int64_t p0, int64_t from) {
+    const int64_t p = min(max(p0 + (int)(threadIdx.x & 63), (int64_t)0), total - 1);
+    return {p0, from, border_at<FORWARD>(l, total, p0, from), DECAY ? l.ts[l.row(p, total)] : 0.0f};
+}
+
+// The batch.  FORWARD: `edge`, whether the first place is the first of `from` (a batch that begins a walk); backward: whether the place
+// `last` (the last one of the walk that the batch holds) is the last of its list.  `before`: the time of the event before the batch.
+template <bool FORWARD, bool DECAY, typename T>
+__device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const Ahead& a, bool edge, int last, float before) {
+    const int lane = threadIdx.x & 63;
+    int passed = 0, more = 0;                   // borders between `from` and the lane's place; and the place after lane 63's (FORWARD), before lane 0's
+    int at = a.border;
+    for (int64_t base = a.from;;) {
+        const uint64_t some = __ballot(FORWARD ? at <= kBatch : at >= 0);
+        if (some) {                             // they come in order: how many lie at or before (beyond) the lane's place
             int n = 0;
 #pragma unroll
             for (int by = 32; by; by >>= 1) {
@@ -130,26 +151,31 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, int64_
             const int border = __shfl(at, 63);
             if (n == 63 && (FORWARD ? border <= lane : border > lane)) n = 64;
             passed += n;
-        }
+            more += __popcll(some);
+                    }
         if (some != ~0ull) break;
+        base += FORWARD ? kWave : -kWave;
+        at = border_at<FORWARD>(l, total, a.p0, base);
     }
     Batch b;
-    b.list = (int)min(max((int64_t)from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
-    const int64_t p = p0 + lane;
-    const bool first = p < total && l.begin_of(b.list, total) == p, last = p < total && l.begin_of((int64_t)b.list + 1, total) == p + 1;
-    b.starts = __ballot(first);
-    b.ends = __ballot(last);
+    b.list = (int)min(max(a.from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
+    if (FORWARD) {
+        const int prev = __shfl_up(passed, 1);
+        b.starts = __ballot((lane != 0) & (passed != prev)) | (uint64_t)(edge | (uniform(passed) != 0));
+        b.ends = b.starts >> 1 | (uint64_t)(more != __builtin_amdgcn_readlane(passed, 63)) << 63;
+    } else {
+        const int prev = __shfl_up(passed, 1);
+        b.starts = __ballot((lane != 0) & (passed != prev)) | (uint64_t)(more != uniform(passed));
+        b.ends = b.starts >> 1 | (uint64_t)edge << last;
+    }
+    b.gap = 0.0f;
+    if (DECAY) {
+        float t = __shfl_up(a.time, 1);
+        if (lane == 0) t = before;
+        if (b.starts >> lane & 1) t = l.t0 ? l.t0[l.list(b.list)] : a.time;
+        b.gap = gap_of(a.time, t);
+    }
     return b;
-}
-
-// Gap before the event of lane's place.
-template <typename T>
-__device__ __forceinline__ float gap_at(const Lists<T>& l, int64_t total, int64_t p0, const Batch& b) {
-    const int lane = threadIdx.x & 63;
-    const int64_t p = min(p0 + lane, total - 1);
-    const float t = l.ts[l.row(p, total)];
-    if (b.starts >> lane & 1) return l.t0 ? gap_of(t, l.t0[l.list(b.list)]) : 0.0f;
-    return gap_of(t, l.ts[l.row(max(p - 1, (int64_t)0), total)]);
 }
 
 // f and z of a lane's channels.
@@ -174,10 +200,6 @@ struct Unit {
 };
 __device__ __forceinline__ int64_t wave_id() { return (int64_t)blockIdx.x * kWaves + uniform(threadIdx.x >> 6); }
 
-template <typename T, int V>
-struct Group {                          // rows of a group as they were read
-    Pack<T, V> u[kSaved], x[kSaved];
-};
 // Reads n rows from place p on (n may be less than a group: the last row again).
 template <typename T, int V, bool FIRST, bool SECOND>
 __device__ __forceinline__ void read_rows(Pack<T, V> (&a)[kSaved], Pack<T, V> (&b)[kSaved], const Lists<T>& l, const T* first, int64_t ld_first, const T* second,
@@ -298,10 +320,10 @@ __global__ void __launch_bounds__(256) k_recur_heads(const Lists<T> l, int64_t t
 
 // Puts the open tiles' carries together, from tile 1 on or (BACKWARD) from the last but one down: kChannels channels a workgroup, each
 // with kParts parts of the tiles: every thread joins its part, the parts are scanned, every thread goes through its part again.
-constexpr int kChannels = 16, kParts = 1024 / kChannels;
+constexpr int kChannels = 8, kParts = 1024 / kChannels, kAtOnce = 8;
 template <bool BACKWARD>
 __global__ void __launch_bounds__(1024) k_recur_join(int64_t tiles, int dim, float* carry, const float* factor, const uint8_t* open) {
-    __shared__ float s_a[kParts][kChannels], s_b[kParts][kChannels];
+    __shared__ float s_a[2][kParts][kChannels], s_b[2][kParts][kChannels];
     __shared__ int s_any;
     if (threadIdx.x == 0) s_any = 0;
     __syncthreads();
@@ -315,32 +337,54 @@ __global__ void __launch_bounds__(1024) k_recur_join(int64_t tiles, int dim, flo
     const int part = threadIdx.x / kChannels, ch = threadIdx.x % kChannels, c = min((int)blockIdx.x * kChannels + ch, dim - 1);
     const bool mine = (int)blockIdx.x * kChannels + ch < dim;
     const int64_t per = (n + kParts - 1) / kParts, begin = min(part * per, n), end = min(begin + per, n);
-    float a = 1.0f, b = 0.0f;                               // what the part does to the carry that enters it; a = 0 once a tile was closed
-    for (int64_t i = begin; i < end; ++i) {
-        const int64_t k = at(i);
-        const float v = carry[k * dim + c];
-        if (open[k]) {
-            const float f = factor[k * dim + c];
-            b = f * b + v;
-            a *= f;
-        } else {
-            a = 0.0f;
-            b = v;
+    float v[kAtOnce], f[kAtOnce];
+    uint8_t is[kAtOnce];
+    auto read = [&](int64_t i) {
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r) {
+            const int64_t k = at(min(i + r, end - 1));
+            is[r] = open[k];
+            v[r] = carry[k * dim + c];
+            f[r] = factor[k * dim + c];                     // (whatever lies there if the tile was closed)
         }
+    };
+    float a = 1.0f, b = 0.0f;                               // what the part does to the carry that enters it: b alone once a tile was closed
+    bool all = true;
+    for (int64_t i = begin; i < end; i += kAtOnce) {
+        read(i);
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r)
+            if (i + r < end) {
+                b = is[r] ? f[r] * b + v[r] : v[r];
+                a = is[r] ? a * f[r] : 1.0f;
+                all = all && is[r];
+            }
     }
-    s_a[part][ch] = a;
-    s_b[part][ch] = b;
+    if (!all) a = __uint_as_float(0x7fc00000u);             // marks a part that lets nothing through
+    auto join = [](float la, float lb, float ra, float rb, float& oa, float& ob) {      // left part, then right part; a NaN marks "closed"
+        ob = ra == ra ? ra * lb + rb : rb;
+        oa = ra == ra && la == la ? ra * la : __uint_as_float(0x7fc00000u);
+    };
+    s_a[0][part][ch] = a;
+    s_b[0][part][ch] = b;
+    int from = 0;
+    for (int by = 1; by < kParts; by *= 2, from ^= 1) {
+        __syncthreads();
+        float oa = s_a[from][part][ch], ob = s_b[from][part][ch];
+        if (part >= by) join(s_a[from][part - by][ch], s_b[from][part - by][ch], oa, ob, oa, ob);
+        s_a[from ^ 1][part][ch] = oa;
+        s_b[from ^ 1][part][ch] = ob;
+    }
     __syncthreads();
-    float enter = 0.0f;                                     // (the first tile written is never open: no list crosses the walk's ends)
-    for (int q = 0; q < part; ++q) enter = (s_a[q][ch] == 0.0f ? 0.0f : s_a[q][ch] * enter) + s_b[q][ch];
-    for (int64_t i = begin; i < end; ++i) {
-        const int64_t k = at(i);
-        float v = carry[k * dim + c];
-        if (open[k]) {
-            v = factor[k * dim + c] * enter + v;
-            if (mine) carry[k * dim + c] = v;
-        }
-        enter = v;
+    float enter = part ? s_b[from][part - 1][ch] : 0.0f;    // (the first tile written is never open: no list crosses the walk's ends)
+    for (int64_t i = begin; i < end; i += kAtOnce) {
+        read(i);
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r)
+            if (i + r < end) {
+                enter = is[r] ? f[r] * enter + v[r] : v[r];
+                if (mine && is[r]) carry[at(i + r) * dim + c] = enter;
+            }
     }
 }
 
@@ -351,7 +395,8 @@ template <typename T>
 __device__ void fill_empty(const Lists<T>& l, int64_t first, const float* from, float* to) {
     const int lane = threadIdx.x & 63;
     const int64_t total = l.total(), s = first + lane;
-    uint64_t empty = __ballot(s < l.S && min(max(l.rowptr[min(s, l.S)], (int64_t)0), total) >= min(max(l.rowptr[min(s + 1, l.S)], (int64_t)0), total));
+    const int64_t begin = min(max(l.rowptr[min(s, l.S)], (int64_t)0), total), end = min(max(l.rowptr[min(s + 1, l.S)], (int64_t)0), total);
+    uint64_t empty = __ballot((s < l.S) & (begin >= end));
     for (; empty; empty &= empty - 1) {
         const int64_t at = (first + __ffsll((unsigned long long)empty) - 1) * l.dim;
         for (int c = lane; c < l.dim; c += kWave) to[at + c] = from ? from[at + c] : 0.0f;
@@ -370,16 +415,17 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t 
     const Unit<V> w(l.dim, blocks, wave);
     const int64_t total = l.total(), begin = w.tile * tile_rows, end = min(begin + tile_rows, total);
     if (begin >= end) return;
-    float rate[V], h[V];
-    rates<V, DECAY>(l, w.c, rate);
-    int j = find_list(l, total, begin);
-    load_floats<V>(l.begin_of(j, total) < begin ? carry + w.tile * l.dim + w.c : nullptr, h);
     Pack<T, V> u[kSaved], x[kSaved];
     read_rows<T, V, true, true>(u, x, l, l.u, l.ld_u, l.x, l.ld_x, total, begin, w.c);
+    float rate[V], h[V];
+    rates<V, DECAY>(l, w.c, rate);
+    const int j = find_list(l, total, begin);
+    const bool fresh = l.begin_of(j, total) == begin;
+    load_floats<V>(fresh ? nullptr : carry + w.tile * l.dim + w.c, h);
+    Batch b = locate<true, DECAY>(l, total, look_ahead<true, DECAY>(l, total, begin, j), fresh, 0, DECAY ? l.ts[l.row(max(begin - 1, (int64_t)0), total)] : 0.0f);
     for (int64_t p0 = begin; p0 < end; p0 += kBatch) {
-        const Batch b = locate<true>(l, total, p0, j);
-        j = __builtin_amdgcn_readlane(b.list, kBatch - 1);
-        const float gap = DECAY ? gap_at(l, total, p0, b) : 0.0f;
+        const Ahead ahead = look_ahead<true, DECAY>(l, total, p0 + kBatch, __builtin_amdgcn_readlane(b.list, kBatch - 1));
+        const float time = DECAY ? l.ts[l.row(min(p0 + kBatch - 1, total - 1), total)] : 0.0f;
         for (int q = 0; q < kBatch && p0 + q < end; q += kSaved) {
             const int64_t p = p0 + q;
             Pack<T, V> next_u[kSaved], next_x[kSaved];
@@ -392,7 +438,7 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t 
                 if (r >= n) continue;
                 if (starts >> r & 1) load_floats<V>(l.h0 ? l.h0_of(__builtin_amdgcn_readlane(b.list, q + r)) + w.c : nullptr, h);
                 float z[V], rest[V], f[V];
-                gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, q + r) : 0.0f, z, rest, f);
+                gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z, rest, f);
 #pragma unroll
                 for (int i = 0; i < V; ++i) h[i] = f[i] * h[i] + z[i] * x[r].get(i);
                 if (h_out) store<T, V>(h_out + l.row(p + r, total) * ld_h + w.c, h);
@@ -401,6 +447,7 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t 
 #pragma unroll
             for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; }
         }
+        if (p0 + kBatch < end) b = locate<true, DECAY>(l, total, ahead, false, 0, time);
     }
 }
 
@@ -419,29 +466,35 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
     const int64_t total = l.total(), begin = w.tile * tile_rows, end = min(begin + tile_rows, total);
     float sum[V] = {};
     if (begin < end) {
+        const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved, last_batch = begin + (end - 1 - begin) / kBatch * kBatch;
+        Pack<T, V> u[kSaved], x[kSaved], d[kSaved];
+        float enter[V];                                     // state before the group
+        auto read_inputs = [&](int64_t p) {
+            read_rows<T, V, true, true>(u, x, l, l.u, l.ld_u, l.x, l.ld_x, total, p, w.c);
+            load_floats<V>(saved + max(p, (int64_t)0) / kSaved * l.dim + w.c, enter);
+        };
+        auto read_grads = [&](int64_t p) {
+            if (dh) read_rows<T, V, true, false>(d, d, l, dh, ld_dh, dh, 0, total, p, w.c);
+        };
+        read_inputs(last_group);
+        read_grads(last_group);
         float rate[V], back[V];
         rates<V, DECAY>(l, w.c, rate);
-        int j = find_list(l, total, end - 1);
-        load_floats<V>(end < total && l.begin_of((int64_t)j + 1, total) > end ? carry + w.tile * l.dim + w.c : nullptr, back);
-        const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved;
-        Pack<T, V> u[kSaved], x[kSaved], d[kSaved];
-        auto read = [&](Pack<T, V>(&ru)[kSaved], Pack<T, V>(&rx)[kSaved], Pack<T, V>(&rd)[kSaved], int64_t p) {
-            read_rows<T, V, true, true>(ru, rx, l, l.u, l.ld_u, l.x, l.ld_x, total, p, w.c);
-            if (dh) read_rows<T, V, true, false>(rd, rd, l, dh, ld_dh, dh, 0, total, p, w.c);
-        };
-        read(u, x, d, last_group);
-        for (int64_t p0 = begin + (end - 1 - begin) / kBatch * kBatch; p0 >= begin; p0 -= kBatch) {
-            const Batch b = locate<false>(l, total, p0, j);
-            j = __builtin_amdgcn_readfirstlane(b.list);
-            const float gap = DECAY ? gap_at(l, total, p0, b) : 0.0f;
+        const int j = find_list(l, total, end - 1);
+        const bool over = l.begin_of((int64_t)j + 1, total) <= end;
+        load_floats<V>(over ? nullptr : carry + w.tile * l.dim + w.c, back);
+        auto time_before = [&](int64_t p) { return DECAY ? l.ts[l.row(max(p - 1, (int64_t)0), total)] : 0.0f; };
+        Batch b = locate<false, DECAY>(l, total, look_ahead<false, DECAY>(l, total, last_batch, j), over, (int)(end - 1 - last_batch), time_before(last_batch));
+        for (int64_t p0 = last_batch; p0 >= begin; p0 -= kBatch) {
+            const Ahead ahead = look_ahead<false, DECAY>(l, total, p0 - kBatch, __builtin_amdgcn_readfirstlane(b.list));
+            const float time = time_before(p0 - kBatch);
             for (int q = (int)(min(end - p0, (int64_t)kBatch) - 1) / kSaved * kSaved; q >= 0; q -= kSaved) {
                 const int64_t p = p0 + q;
-                Pack<T, V> next_u[kSaved], next_x[kSaved], next_d[kSaved];
-                read(next_u, next_x, next_d, p - kSaved);
                 const int n = (int)min(end - p, (int64_t)kSaved);
                 const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
                 float h[V];
-                load_floats<V>(starts & 1 ? nullptr : saved + p / kSaved * l.dim + w.c, h);
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[i] = enter[i];
                 // Forward through the group: dx = z back, du = slope back, and what the event keeps of the state before it.
                 float z[kSaved][V], f[kSaved][V], slope[kSaved][V], kept[kSaved][V];
 #pragma unroll
@@ -449,7 +502,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
                     if (r >= n) continue;
                     if (starts >> r & 1) load_floats<V>(l.h0 ? l.h0_of(__builtin_amdgcn_readlane(b.list, q + r)) + w.c : nullptr, h);
                     float rest[V];
-                    gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, q + r) : 0.0f, z[r], rest, f[r]);
+                    gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z[r], rest, f[r]);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const float in = x[r].get(i);
@@ -458,11 +511,12 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
                         h[i] = kept[r][i] + z[r][i] * in;
                     }
                 }
+                read_inputs(p - kSaved);
 #pragma unroll
                 for (int r = kSaved - 1; r >= 0; --r) {
                     if (r >= n) continue;
                     if (ends >> r & 1) load_floats<V>(dlast ? dlast + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c : nullptr, back);
-                    const float g = DECAY ? read_lane(gap, q + r) : 0.0f;
+                    const float g = DECAY ? read_lane(b.gap, q + r) : 0.0f;
                     float vu[V], vx[V];
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
@@ -477,9 +531,10 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
                     store<T, V>(du + row * ld_du + w.c, vu);
                     if (dh0 && (starts >> r & 1)) store_floats<V>(dh0 + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c, back);
                 }
-#pragma unroll
-                for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; d[r] = next_d[r]; }
+                read_grads(p - kSaved);
             }
+            const bool border = b.starts & 1;
+            if (p0 > begin) b = locate<false, DECAY>(l, total, ahead, border, kBatch - 1, time);
         }
     }
     if (DECAY && sums) store_floats<V>(sums + w.tile * l.dim + w.c, sum);
@@ -491,7 +546,13 @@ __global__ void __launch_bounds__(1024) k_recur_sums(const float* sums, int64_t 
     const int part = threadIdx.x / kChannels, ch = threadIdx.x % kChannels, c = (int)blockIdx.x * kChannels + ch;
     float sum = 0.0f;
     if (c < dim)
-        for (int64_t k = part; k < tiles; k += kParts) sum += sums[k * dim + c];
+        for (int64_t k = part; k < tiles; k += kParts * kAtOnce) {
+            float v[kAtOnce];
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r) v[r] = k + r * kParts < tiles ? sums[(k + r * kParts) * dim + c] : 0.0f;
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r) sum += v[r];
+        }
     s_sum[part][ch] = sum;
     for (int n = kParts / 2; n; n /= 2) {
         __syncthreads();
@@ -552,10 +613,10 @@ int check_workspace(const void* p, size_t have, size_t need) {
     return TNS_OK;
 }
 
-// Rows of a tile: as many as leave a wave for every place of the chip (1024 SIMDs, four waves each and more), 64 to 1024.
+// Rows of a tile: as many as leave a wave for every place of the chip (1024 SIMDs, four waves each and more), 16 to 1024.
 int64_t tile_rows_of(int64_t rows, int dim) {
     const int64_t blocks = (dim + kWave - 1) / kWave;
-    int64_t n = kBatch;
+    int64_t n = kSaved;
     while (n < 1024 && rows / n * blocks > 8192) n *= 2;
     return n;
 }
