@@ -23,37 +23,33 @@ namespace {
 constexpr int kWave = 64, kWaves = 4;  // lanes of a wave, waves of a workgroup
 constexpr int kSaved = 16;             // rows from one saved state to the next, and rows that a wave has in its registers
 constexpr int kBatch = 64;             // rows whose lists and gaps the lanes of a wave hold
+constexpr uint32_t kGroupMask = (1u << kSaved) - 1;
 
 // Values of the V channels of a lane, as they lie in memory.
 template <typename T, int V> struct Pack;
 template <> struct Pack<float, 1> {
     float raw;
     __device__ float get(int) const { return raw; }
-    __device__ void set(int, float v) { raw = v; }
 };
 template <> struct Pack<bf16, 1> {
     bf16 raw;
     __device__ float get(int) const { return as_float(raw); }
-    __device__ void set(int, float v) { raw = as_value<bf16>(v); }
 };
 template <> struct Pack<bf16, 2> {
     uint32_t raw;
     __device__ float get(int i) const { return __uint_as_float(i ? raw & 0xffff0000u : raw << 16); }
-    __device__ void set(int i, float v) { raw = i ? (raw & 0xffffu) | (uint32_t)as_value<bf16>(v).bits << 16 : (uint32_t)as_value<bf16>(v).bits; }
 };
-template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> load(const T* p) { return *reinterpret_cast<const Pack<T, V>*>(p); }
-template <typename T, int V>
-__device__ __forceinline__ void store(T* p, const float (&v)[V]) {
-    Pack<T, V> k;
-#pragma unroll
-    for (int i = 0; i < V; ++i) k.set(i, v[i]);
-    *reinterpret_cast<Pack<T, V>*>(p) = k;
-}
 template <int V>
 __device__ __forceinline__ void load_floats(const float* p, float (&v)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = p ? p[i] : 0.0f;
+    for (int i = 0; i < V; ++i) v[i] = p[i];
+}
+template <int V>
+__device__ __forceinline__ void load_or_zero(const float* p, float (&v)[V]) {      // (p is the same or null for the whole wave)
+    if (p) load_floats<V>(p, v);
+    else
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = 0.0f;
 }
 template <int V>
 __device__ __forceinline__ void store_floats(float* p, const float (&v)[V]) {
@@ -62,6 +58,10 @@ __device__ __forceinline__ void store_floats(float* p, const float (&v)[V]) {
 }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ float read_lane(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 
 // The lists (tns_recur with its types) as one walk over all events: place p of the walk is row p, or, newest first, row total - 1 - p; the
@@ -76,7 +76,7 @@ struct Lists {
     int dim;
     bool newest_first;
 
-    __device__ int64_t total() const { return min(max(rowptr[S], (int64_t)0), rows); }
+    __device__ int64_t total() const { return uniform(min(max(rowptr[S], (int64_t)0), rows)); }
     __device__ int64_t begin_of(int64_t j, int64_t total) const {         // 0 <= j <= S
         const int64_t at = min(max(rowptr[newest_first ? S - j : j], (int64_t)0), total);
         return newest_first ? total - at : at;
@@ -100,7 +100,7 @@ __device__ int find_list(const Lists<T>& l, int64_t total, int64_t p) {
         lo += c * by;
         hi = min(lo + by, hi);
     }
-    return (int)lo;
+    return uniform((int)lo);
 }
 
 // What the lanes know of the 64 places from p0 on: lane i the list of place p0 + i and the gap before its event; bit i of `starts` and
@@ -108,6 +108,7 @@ __device__ int find_list(const Lists<T>& l, int64_t total, int64_t p) {
 // the borders between lists, the times) while it is busy with these.
 struct Batch {
     int list;
+    int edge;                           // the last place's list (FORWARD), or the first one's, counted along the walk
     float gap;
     uint64_t starts, ends;
 };
@@ -158,7 +159,9 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
         at = border_at<FORWARD>(l, total, a.p0, base);
     }
     Batch b;
-    b.list = (int)min(max(a.from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
+    const int list = (int)min(max(a.from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
+    b.edge = __builtin_amdgcn_readlane(list, FORWARD ? kBatch - 1 : 0);
+    b.list = (int)l.list(list);
     if (FORWARD) {
         const int prev = __shfl_up(passed, 1);
         b.starts = __ballot((lane != 0) & (passed != prev)) | (uint64_t)(edge | (uniform(passed) != 0));
@@ -172,11 +175,71 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
     if (DECAY) {
         float t = __shfl_up(a.time, 1);
         if (lane == 0) t = before;
-        if (b.starts >> lane & 1) t = l.t0 ? l.t0[l.list(b.list)] : a.time;
+        if (b.starts >> lane & 1) t = l.t0 ? l.t0[b.list] : a.time;
         b.gap = gap_of(a.time, t);
     }
     return b;
 }
+
+// Has the wave wait for values that it has read, here rather than at their first use: the code of a group branches, and from behind a
+// branch the compiler can only wait for as few requests on their way as its shortest path has, the next group's among them.
+template <typename P>
+__device__ __forceinline__ void arrive(P& v) {
+    if constexpr (sizeof(P) == 2) {
+        uint32_t bits = __builtin_bit_cast(uint16_t, v);
+        asm volatile("" : "+v"(bits));
+        v = __builtin_bit_cast(P, (uint16_t)bits);
+    } else {
+        float word = __builtin_bit_cast(float, v);
+        asm volatile("" : "+v"(word));
+        v = __builtin_bit_cast(P, word);
+    }
+}
+template <typename P, int N>
+__device__ __forceinline__ void arrive(P (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) arrive(v[i]);
+}
+
+// Rows of an fp32 array [S, dim] (h0 at the first events of lists, dlast at the last ones) that a group of rows needs: the first two are
+// read with the group's rows, any more when their event comes.
+template <int V>
+struct Edges {
+    float v[2][V] = {};
+    int left;                           // of the two
+
+    template <bool FORWARD>
+    __device__ void read(const float* base, const Batch& b, uint32_t mask, int q, int dim, int c) {
+        left = 2;
+        if (!base) {
+            left = 1 << 30;
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (!mask) break;
+            const int r = FORWARD ? __builtin_ctz(mask) : 31 - __builtin_clz(mask);
+            mask &= ~(1u << r);
+            load_floats<V>(at(base, b, q + r, dim) + c, v[k]);
+        }
+    }
+    __device__ static const float* at(const float* base, const Batch& b, int place, int dim) {
+        return base + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(b.list, place) * (uint32_t)dim;
+    }
+    __device__ void take(const float* base, const Batch& b, int place, int dim, int c, float (&to)[V]) {
+        if (left > 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                to[i] = base ? v[0][i] : 0.0f;
+                v[0][i] = v[1][i];
+            }
+            --left;
+        } else {
+            load_floats<V>(at(base, b, place, dim) + c, to);
+            arrive(to);
+        }
+    }
+};
 
 // f and z of a lane's channels.
 template <int V, bool DECAY, typename P>
@@ -198,18 +261,76 @@ struct Unit {
         c = min((int)(wave % blocks) * kWave * V + (int)(threadIdx.x & 63) * V, dim - V);
     }
 };
-__device__ __forceinline__ int64_t wave_id() { return (int64_t)blockIdx.x * kWaves + uniform(threadIdx.x >> 6); }
+__device__ __forceinline__ int64_t wave_id() { return (int64_t)blockIdx.x * kWaves + uniform((int)(threadIdx.x >> 6)); }
 
-// Reads n rows from place p on (n may be less than a group: the last row again).
-template <typename T, int V, bool FIRST, bool SECOND>
-__device__ __forceinline__ void read_rows(Pack<T, V> (&a)[kSaved], Pack<T, V> (&b)[kSaved], const Lists<T>& l, const T* first, int64_t ld_first, const T* second,
-                                          int64_t ld_second, int64_t total, int64_t p, int c) {
-#pragma unroll
-    for (int r = 0; r < kSaved; ++r) {
-        const int64_t row = l.row(max(min(p + r, total - 1), (int64_t)0), total);
-        if (FIRST) a[r] = load<T, V>(first + row * ld_first + c);
-        if (SECOND) b[r] = load<T, V>(second + row * ld_second + c);
+// An array's rows along the walk: place p lies at origin + p * step bytes.  Everything but the channel is the same for the whole wave:
+// the addresses are the scalar unit's work, two additions a row.
+#if defined(__HIP_DEVICE_COMPILE__)
+#define TNS_GLOBAL __attribute__((address_space(1)))
+#else
+#define TNS_GLOBAL                      // (the host's pass over the kernels knows no address spaces)
+#endif
+using Global = TNS_GLOBAL char*;
+struct Along {
+    Global origin;
+    int64_t step;
+    template <typename L, typename T>
+    __device__ Along(const L& l, T* base, int64_t ld, int64_t total) {
+        T* const first = l.newest_first ? base + (total - 1) * ld : base;
+        origin = (Global)(char*)const_cast<std::remove_const_t<T>*>(first);
+        step = (l.newest_first ? -ld : ld) * (int64_t)sizeof(T);
     }
+    __device__ Global at(int64_t p) const { return origin + p * step; }
+    // The next row (the one before).  Opaque to the compiler, which would keep the sixteen multiples of the step that a group takes in
+    // scalar registers, for every array, and move them to vector registers and back as there are not that many.
+    __device__ Global next(Global q) const { q += step; asm("" : "+s"(q)); return q; }
+    __device__ Global back(Global q) const { q -= step; asm("" : "+s"(q)); return q; }
+};
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_row(Global row, uint32_t bytes) {
+    asm("" : "+v"(bytes));              // (stays 32 bits: address = scalar base + vector offset)
+    return *(const TNS_GLOBAL Pack<T, V>*)(row + bytes);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_row(Global row, uint32_t bytes, const float (&v)[V]) {
+    asm("" : "+v"(bytes));
+    if constexpr (V == 2) {
+        using Two = float __attribute__((ext_vector_type(2)));
+        using Halves = __bf16 __attribute__((ext_vector_type(2)));
+        *(TNS_GLOBAL Halves*)(row + bytes) = __builtin_convertvector((Two{v[0], v[1]}), Halves);
+    } else {
+        *(TNS_GLOBAL T*)(row + bytes) = as_value<T>(v[0]);
+    }
+}
+// The kSaved rows from place p on, 0 <= p < total; the walk's last row again where there are no more.
+template <typename T, int V>
+__device__ __forceinline__ void read_rows(Pack<T, V> (&a)[kSaved], const Along& rows, int64_t total, int64_t p, int c) {
+    const uint32_t bytes = (uint32_t)c * sizeof(T);
+    Global q = rows.at(p);
+    if (p + kSaved <= total) {
+#pragma unroll
+        for (int r = 0; r < kSaved; ++r, q = rows.next(q)) a[r] = load_row<T, V>(q, bytes);
+    } else {
+        const int n = (int)(total - p);
+#pragma unroll
+        for (int r = 0; r < kSaved; ++r) {
+            a[r] = load_row<T, V>(q, bytes);
+            if (r + 1 < n) q = rows.next(q);
+        }
+    }
+}
+// Runs go(r) for the first n of a group's rows, in order or from the last one back.
+template <typename F>
+__device__ __forceinline__ void each_row(int n, const F& go) {
+#pragma unroll
+    for (int r = 0; r < kSaved; ++r)
+        if (r < n) go(r);
+}
+template <typename F>
+__device__ __forceinline__ void each_row_back(int n, const F& go) {
+#pragma unroll
+    for (int r = kSaved - 1; r >= 0; --r)
+        if (r < n) go(r);
 }
 
 // Rate of the decay in powers of two.
@@ -233,17 +354,19 @@ __global__ void __launch_bounds__(256) k_recur_tails(const Lists<T> l, int64_t t
     bool is_open = false;
     if (end < total) {
         const int j = find_list(l, total, end - 1);
-        const int64_t first = l.begin_of(j, total);
-        if (l.begin_of((int64_t)j + 1, total) > end) {
+        const int64_t first = uniform(l.begin_of(j, total));
+        if (uniform(l.begin_of((int64_t)j + 1, total)) > end) {
             is_open = first < begin;
             float rate[V], h[V], a[V];
             rates<V, DECAY>(l, w.c, rate);
-            load_floats<V>(is_open || !l.h0 ? nullptr : l.h0_of(j) + w.c, h);
+            load_or_zero<V>(is_open || !l.h0 ? nullptr : l.h0_of(j) + w.c, h);
 #pragma unroll
             for (int i = 0; i < V; ++i) a[i] = 1.0f;
             Pack<T, V> u[kSaved], x[kSaved];
+            const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total);
             for (int64_t p = max(first, begin); p < end; p += kSaved) {
-                read_rows<T, V, true, true>(u, x, l, l.u, l.ld_u, l.x, l.ld_x, total, p, w.c);
+                read_rows<T, V>(u, rows_u, total, p, w.c);
+                read_rows<T, V>(x, rows_x, total, p, w.c);
                 float gap = 0.0f;
                 if (DECAY) {
                     const int64_t q = min(p + (threadIdx.x & (kSaved - 1)), end - 1);
@@ -251,9 +374,7 @@ __global__ void __launch_bounds__(256) k_recur_tails(const Lists<T> l, int64_t t
                     gap = q == first ? l.t0 ? gap_of(t, l.t0[l.list(j)]) : 0.0f : gap_of(t, l.ts[l.row(q - 1, total)]);
                 }
                 const int n = (int)min(end - p, (int64_t)kSaved);
-#pragma unroll
-                for (int r = 0; r < kSaved; ++r) {
-                    if (r >= n) continue;
+                each_row(n, [&](int r) {
                     float z[V], rest[V], f[V];
                     gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, r) : 0.0f, z, rest, f);
 #pragma unroll
@@ -261,7 +382,7 @@ __global__ void __launch_bounds__(256) k_recur_tails(const Lists<T> l, int64_t t
                         h[i] = f[i] * h[i] + z[i] * x[r].get(i);
                         a[i] *= f[i];
                     }
-                }
+                });
             }
             store_floats<V>(carry + (w.tile + 1) * l.dim + w.c, h);
             if (is_open) store_floats<V>(factor + (w.tile + 1) * l.dim + w.c, a);
@@ -280,36 +401,35 @@ __global__ void __launch_bounds__(256) k_recur_heads(const Lists<T> l, int64_t t
     bool is_open = false;
     if (begin < total) {
         const int j = find_list(l, total, begin);
-        if (l.begin_of(j, total) < begin) {
-            const int64_t last = l.begin_of((int64_t)j + 1, total), end = min(last, begin + tile_rows);
+        if (uniform(l.begin_of(j, total)) < begin) {
+            const int64_t last = uniform(l.begin_of((int64_t)j + 1, total)), end = min(last, begin + tile_rows);
             is_open = end < last;
             float rate[V], back[V], a[V];
             rates<V, DECAY>(l, w.c, rate);
-            load_floats<V>(is_open || !dlast ? nullptr : dlast + l.list(j) * l.dim + w.c, back);
+            load_or_zero<V>(is_open || !dlast ? nullptr : dlast + l.list(j) * l.dim + w.c, back);
 #pragma unroll
             for (int i = 0; i < V; ++i) a[i] = 1.0f;
-            Pack<T, V> u[kSaved], d[kSaved];
+            Pack<T, V> u[kSaved], d[kSaved] = {};
+            const Along rows_u(l, l.u, l.ld_u, total), rows_d(l, dh, ld_dh, total);
             for (int64_t p = begin + (end - 1 - begin) / kSaved * kSaved; p >= begin; p -= kSaved) {
-                read_rows<T, V, true, false>(u, d, l, l.u, l.ld_u, l.u, 0, total, p, w.c);
-                if (dh) read_rows<T, V, false, true>(u, d, l, l.u, 0, dh, ld_dh, total, p, w.c);
+                read_rows<T, V>(u, rows_u, total, p, w.c);
+                if (dh) read_rows<T, V>(d, rows_d, total, p, w.c);
                 float gap = 0.0f;
                 if (DECAY) {
                     const int64_t q = min(p + (threadIdx.x & (kSaved - 1)), end - 1);
                     gap = gap_of(l.ts[l.row(q, total)], l.ts[l.row(q - 1, total)]);      // (the list's first event is not here)
                 }
                 const int n = (int)min(end - p, (int64_t)kSaved);
-#pragma unroll
-                for (int r = kSaved - 1; r >= 0; --r) {
-                    if (r >= n) continue;
+                each_row_back(n, [&](int r) {
                     float z[V], rest[V], f[V];
                     gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, r) : 0.0f, z, rest, f);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        if (dh) back[i] += d[r].get(i);
+                        back[i] += d[r].get(i);
                         back[i] *= f[i];
                         a[i] *= f[i];
                     }
-                }
+                });
             }
             store_floats<V>(carry + w.tile * l.dim + w.c, back);
             if (is_open) store_floats<V>(factor + w.tile * l.dim + w.c, a);
@@ -416,38 +536,59 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t 
     const int64_t total = l.total(), begin = w.tile * tile_rows, end = min(begin + tile_rows, total);
     if (begin >= end) return;
     Pack<T, V> u[kSaved], x[kSaved];
-    read_rows<T, V, true, true>(u, x, l, l.u, l.ld_u, l.x, l.ld_x, total, begin, w.c);
+    const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total);
+    const Along rows_h(l, h_out, ld_h, total);
+    read_rows<T, V>(u, rows_u, total, begin, w.c);
+    read_rows<T, V>(x, rows_x, total, begin, w.c);
     float rate[V], h[V];
     rates<V, DECAY>(l, w.c, rate);
     const int j = find_list(l, total, begin);
-    const bool fresh = l.begin_of(j, total) == begin;
-    load_floats<V>(fresh ? nullptr : carry + w.tile * l.dim + w.c, h);
+    const bool fresh = uniform(l.begin_of(j, total)) == begin;
+    load_or_zero<V>(fresh ? nullptr : carry + w.tile * l.dim + w.c, h);
     Batch b = locate<true, DECAY>(l, total, look_ahead<true, DECAY>(l, total, begin, j), fresh, 0, DECAY ? l.ts[l.row(max(begin - 1, (int64_t)0), total)] : 0.0f);
-    for (int64_t p0 = begin; p0 < end; p0 += kBatch) {
-        const Ahead ahead = look_ahead<true, DECAY>(l, total, p0 + kBatch, __builtin_amdgcn_readlane(b.list, kBatch - 1));
-        const float time = DECAY ? l.ts[l.row(min(p0 + kBatch - 1, total - 1), total)] : 0.0f;
-        for (int q = 0; q < kBatch && p0 + q < end; q += kSaved) {
-            const int64_t p = p0 + q;
-            Pack<T, V> next_u[kSaved], next_x[kSaved];
-            read_rows<T, V, true, true>(next_u, next_x, l, l.u, l.ld_u, l.x, l.ld_x, total, p + kSaved, w.c);
-            const int n = (int)min(end - p, (int64_t)kSaved);
-            const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
-            if (saved) store_floats<V>(saved + p / kSaved * l.dim + w.c, h);
-#pragma unroll
-            for (int r = 0; r < kSaved; ++r) {
-                if (r >= n) continue;
-                if (starts >> r & 1) load_floats<V>(l.h0 ? l.h0_of(__builtin_amdgcn_readlane(b.list, q + r)) + w.c : nullptr, h);
-                float z[V], rest[V], f[V];
-                gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z, rest, f);
-#pragma unroll
-                for (int i = 0; i < V; ++i) h[i] = f[i] * h[i] + z[i] * x[r].get(i);
-                if (h_out) store<T, V>(h_out + l.row(p + r, total) * ld_h + w.c, h);
-                if (last && (ends >> r & 1)) store_floats<V>(last + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c, h);
-            }
-#pragma unroll
-            for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; }
+    Edges<V> enter;
+    enter.template read<true>(l.h0, b, (uint32_t)b.starts & kGroupMask, 0, l.dim, w.c);
+    Ahead ahead = look_ahead<true, DECAY>(l, total, begin + kBatch, b.edge);
+    float time = DECAY ? l.ts[l.row(min(begin + kBatch - 1, total - 1), total)] : 0.0f;
+    for (int64_t p = begin; p < end; p += kSaved) {
+        const int q = (int)(p - begin) & (kBatch - 1);
+        const bool more = p + kSaved < end, turn = q + kSaved == kBatch;
+        arrive(u);
+        arrive(x);
+        arrive(enter.v);
+        Batch next = b;
+        if (more && turn) next = locate<true, DECAY>(l, total, ahead, false, 0, time);
+        Pack<T, V> next_u[kSaved], next_x[kSaved];
+        Edges<V> next_enter;
+        if (more) {
+            read_rows<T, V>(next_u, rows_u, total, p + kSaved, w.c);
+            read_rows<T, V>(next_x, rows_x, total, p + kSaved, w.c);
+            const int next_q = turn ? 0 : q + kSaved;
+            next_enter.template read<true>(l.h0, next, (uint32_t)(next.starts >> next_q) & kGroupMask, next_q, l.dim, w.c);
         }
-        if (p0 + kBatch < end) b = locate<true, DECAY>(l, total, ahead, false, 0, time);
+        if (more && turn) {
+            ahead = look_ahead<true, DECAY>(l, total, p + kSaved + kBatch, next.edge);
+            if (DECAY) time = l.ts[l.row(min(p + kSaved + kBatch - 1, total - 1), total)];
+        }
+        const int n = (int)min(end - p, (int64_t)kSaved);
+        const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
+        if (saved) store_floats<V>(saved + p / kSaved * l.dim + w.c, h);
+        Global to = rows_h.at(p);
+        each_row(n, [&](int r) {
+            if (starts >> r & 1) enter.take(l.h0, b, q + r, l.dim, w.c, h);
+            float z[V], rest[V], f[V];
+            gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z, rest, f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[i] = f[i] * h[i] + z[i] * x[r].get(i);
+            if (h_out) store_row<T, V>(to, (uint32_t)w.c * sizeof(T), h);
+            to = rows_h.next(to);
+            if (ends >> r & 1)
+                if (last) store_floats<V>(last + (Edges<V>::at(last, b, q + r, l.dim) - last) + w.c, h);
+        });
+#pragma unroll
+        for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; }
+        enter = next_enter;
+        b = next;
     }
 }
 
@@ -467,74 +608,98 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
     float sum[V] = {};
     if (begin < end) {
         const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved, last_batch = begin + (end - 1 - begin) / kBatch * kBatch;
-        Pack<T, V> u[kSaved], x[kSaved], d[kSaved];
+        Pack<T, V> u[kSaved], x[kSaved], d[kSaved] = {};      // (d stays zero without dh)
         float enter[V];                                     // state before the group
+        const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total), rows_d(l, dh, ld_dh, total);
+        const Along rows_du(l, du, ld_du, total), rows_dx(l, dx, ld_dx, total);
         auto read_inputs = [&](int64_t p) {
-            read_rows<T, V, true, true>(u, x, l, l.u, l.ld_u, l.x, l.ld_x, total, p, w.c);
-            load_floats<V>(saved + max(p, (int64_t)0) / kSaved * l.dim + w.c, enter);
+            read_rows<T, V>(u, rows_u, total, p, w.c);
+            read_rows<T, V>(x, rows_x, total, p, w.c);
+            load_floats<V>(saved + p / kSaved * l.dim + w.c, enter);
         };
         auto read_grads = [&](int64_t p) {
-            if (dh) read_rows<T, V, true, false>(d, d, l, dh, ld_dh, dh, 0, total, p, w.c);
+            if (dh) read_rows<T, V>(d, rows_d, total, p, w.c);
         };
         read_inputs(last_group);
         read_grads(last_group);
         float rate[V], back[V];
         rates<V, DECAY>(l, w.c, rate);
         const int j = find_list(l, total, end - 1);
-        const bool over = l.begin_of((int64_t)j + 1, total) <= end;
-        load_floats<V>(over ? nullptr : carry + w.tile * l.dim + w.c, back);
+        const bool over = uniform(l.begin_of((int64_t)j + 1, total)) <= end;
+        load_or_zero<V>(over ? nullptr : carry + w.tile * l.dim + w.c, back);
         auto time_before = [&](int64_t p) { return DECAY ? l.ts[l.row(max(p - 1, (int64_t)0), total)] : 0.0f; };
         Batch b = locate<false, DECAY>(l, total, look_ahead<false, DECAY>(l, total, last_batch, j), over, (int)(end - 1 - last_batch), time_before(last_batch));
-        for (int64_t p0 = last_batch; p0 >= begin; p0 -= kBatch) {
-            const Ahead ahead = look_ahead<false, DECAY>(l, total, p0 - kBatch, __builtin_amdgcn_readfirstlane(b.list));
-            const float time = time_before(p0 - kBatch);
-            for (int q = (int)(min(end - p0, (int64_t)kBatch) - 1) / kSaved * kSaved; q >= 0; q -= kSaved) {
-                const int64_t p = p0 + q;
-                const int n = (int)min(end - p, (int64_t)kSaved);
-                const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
-                float h[V];
+        Edges<V> start, leave;
+        auto part = [](uint64_t bits, int q) { return (uint32_t)(bits >> q) & kGroupMask; };
+        int q = (int)(last_group - last_batch);
+        start.template read<true>(l.h0, b, part(b.starts, q), q, l.dim, w.c);
+        leave.template read<false>(dlast, b, part(b.ends, q), q, l.dim, w.c);
+        Ahead ahead = look_ahead<false, DECAY>(l, total, last_batch - kBatch, b.edge);
+        float time = time_before(last_batch - kBatch);
+        for (int64_t p = last_group; p >= begin; p -= kSaved) {
+            const bool more = p > begin, turn = q == 0;
+            const int n = (int)min(end - p, (int64_t)kSaved);
+            const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
+            arrive(u);
+            arrive(x);
+            arrive(enter);
+            arrive(start.v);
+            float h[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) h[i] = enter[i];
-                // Forward through the group: dx = z back, du = slope back, and what the event keeps of the state before it.
-                float z[kSaved][V], f[kSaved][V], slope[kSaved][V], kept[kSaved][V];
+            for (int i = 0; i < V; ++i) h[i] = enter[i];
+            // Forward through the group: dx = z back, du = slope back, and what the event keeps of the state before it.
+            float z[kSaved][V], f[kSaved][V], slope[kSaved][V], kept[kSaved][V];
+            each_row(n, [&](int r) {
+                if (starts >> r & 1) start.take(l.h0, b, q + r, l.dim, w.c, h);
+                float rest[V];
+                gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z[r], rest, f[r]);
 #pragma unroll
-                for (int r = 0; r < kSaved; ++r) {
-                    if (r >= n) continue;
-                    if (starts >> r & 1) load_floats<V>(l.h0 ? l.h0_of(__builtin_amdgcn_readlane(b.list, q + r)) + w.c : nullptr, h);
-                    float rest[V];
-                    gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z[r], rest, f[r]);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float in = x[r].get(i);
-                        kept[r][i] = f[r][i] * h[i];
-                        slope[r][i] = z[r][i] * (rest[i] * in - kept[r][i]);
-                        h[i] = kept[r][i] + z[r][i] * in;
-                    }
+                for (int i = 0; i < V; ++i) {
+                    const float in = x[r].get(i);
+                    kept[r][i] = f[r][i] * h[i];
+                    slope[r][i] = z[r][i] * (rest[i] * in - kept[r][i]);
+                    h[i] = kept[r][i] + z[r][i] * in;
                 }
+            });
+            arrive(d);
+            arrive(leave.v);
+            Batch next = b;
+            if (more && turn) next = locate<false, DECAY>(l, total, ahead, (bool)(b.starts & 1), kBatch - 1, time);
+            const int next_q = turn ? kBatch - kSaved : q - kSaved;
+            if (more) {
                 read_inputs(p - kSaved);
-#pragma unroll
-                for (int r = kSaved - 1; r >= 0; --r) {
-                    if (r >= n) continue;
-                    if (ends >> r & 1) load_floats<V>(dlast ? dlast + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c : nullptr, back);
-                    const float g = DECAY ? read_lane(b.gap, q + r) : 0.0f;
-                    float vu[V], vx[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        if (dh) back[i] += d[r].get(i);
-                        vx[i] = z[r][i] * back[i];
-                        vu[i] = slope[r][i] * back[i];
-                        if (DECAY) sum[i] -= kept[r][i] * back[i] * g;
-                        back[i] *= f[r][i];
-                    }
-                    const int64_t row = l.row(p + r, total);
-                    store<T, V>(dx + row * ld_dx + w.c, vx);
-                    store<T, V>(du + row * ld_du + w.c, vu);
-                    if (dh0 && (starts >> r & 1)) store_floats<V>(dh0 + l.list(__builtin_amdgcn_readlane(b.list, q + r)) * l.dim + w.c, back);
-                }
-                read_grads(p - kSaved);
+                start.template read<true>(l.h0, next, part(next.starts, next_q), next_q, l.dim, w.c);
             }
-            const bool border = b.starts & 1;
-            if (p0 > begin) b = locate<false, DECAY>(l, total, ahead, border, kBatch - 1, time);
+            if (more && turn) {
+                ahead = look_ahead<false, DECAY>(l, total, p - 2 * kBatch, next.edge);
+                time = time_before(p - 2 * kBatch);
+            }
+            Global to_x = rows_dx.at(p + n - 1), to_u = rows_du.at(p + n - 1);
+            each_row_back(n, [&](int r) {
+                if (ends >> r & 1) leave.take(dlast, b, q + r, l.dim, w.c, back);
+                const float g = DECAY ? read_lane(b.gap, q + r) : 0.0f;
+                float vu[V], vx[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    back[i] += d[r].get(i);
+                    vx[i] = z[r][i] * back[i];
+                    vu[i] = slope[r][i] * back[i];
+                    if (DECAY) sum[i] -= kept[r][i] * back[i] * g;
+                    back[i] *= f[r][i];
+                }
+                store_row<T, V>(to_x, (uint32_t)w.c * sizeof(T), vx);
+                store_row<T, V>(to_u, (uint32_t)w.c * sizeof(T), vu);
+                to_x = rows_dx.back(to_x);
+                to_u = rows_du.back(to_u);
+                if (starts >> r & 1)
+                    if (dh0) store_floats<V>(dh0 + (Edges<V>::at(dh0, b, q + r, l.dim) - dh0) + w.c, back);
+            });
+            if (more) {
+                read_grads(p - kSaved);
+                leave.template read<false>(dlast, next, part(next.ends, next_q), next_q, l.dim, w.c);
+            }
+            b = next;
+            q = next_q;
         }
     }
     if (DECAY && sums) store_floats<V>(sums + w.tile * l.dim + w.c, sum);
