@@ -251,17 +251,9 @@ __device__ __forceinline__ void gates(const P& u, const float (&rate)[V], float 
     }
 }
 
-// The wave's share of the work: rows of a tile, V channels a lane.  Lanes beyond the last channel repeat it (they store what it stores).
+// Channels of a lane, V from c on, in a block of 64 V.  Lanes beyond the last channel repeat it (they store what it stores).
 template <int V>
-struct Unit {
-    int64_t tile;
-    int c;
-    __device__ Unit(int dim, int blocks, int64_t wave) {
-        tile = wave / blocks;
-        c = min((int)(wave % blocks) * kWave * V + (int)(threadIdx.x & 63) * V, dim - V);
-    }
-};
-__device__ __forceinline__ int64_t wave_id() { return (int64_t)blockIdx.x * kWaves + uniform((int)(threadIdx.x >> 6)); }
+__device__ __forceinline__ int channel_of(int dim, int block) { return min(block * kWave * V + (int)(threadIdx.x & 63) * V, dim - V); }
 
 // An array's rows along the walk: place p lies at origin + p * step bytes.  Everything but the channel is the same for the whole wave:
 // the addresses are the scalar unit's work, two additions a row.
@@ -340,38 +332,125 @@ __device__ __forceinline__ void rates(const Lists<T>& l, int c, float (&rate)[V]
     for (int i = 0; i < V; ++i) rate[i] = DECAY ? -kLog2e * l.decay[c + i] : 0.0f;
 }
 
+// A workgroup's share: block of channels and the q-th group of tiles.  Workgroups go round the eight XCDs; those of one group of tiles come
+// eight apart and so meet in one L2, as their blocks of channels share cache lines wherever rows are no multiple of them (172 channels of
+// fp32, 1.35 M rows: states 452 -> 338 us, gradients 776 -> 599 us).
+constexpr int kXcds = 8;
+struct Share {
+    int64_t q;
+    int block;
+    __device__ Share(int64_t workgroup, int blocks) {
+        const int64_t at = workgroup % (kXcds * blocks);
+        q = workgroup / (kXcds * blocks) * kXcds + at % kXcds;
+        block = (int)(at / kXcds);
+    }
+};
+__host__ __device__ constexpr int64_t workgroups_of(int64_t groups, int blocks) { return (groups + kXcds - 1) / kXcds * kXcds * blocks; }
+
 // ---- carries -------------------------------------------------------------------------------------------
-// The walk is cut into tiles.  carry[k] is what enters tile k: the state before its first event, or (backward) what the events after its
-// last one send back.  A tile whose part of the crossing list begins (ends) inside it knows what it hands on (closed); one that lies
-// inside a list altogether hands on A * what enters + B (open): it writes B as the carry and A beside it, and k_recur_join puts them together.
+// The walk is cut into tiles, sixteen tiles to a span.  What enters a tile is the state before its first event, or (backward) what the
+// events after its last one send back.  A tile whose part of the crossing list begins (ends) inside it knows what it hands on, B (closed);
+// one that lies inside a list altogether hands on A * what enters + B (open).  A workgroup of a wave for every tile of a span finds both
+// and puts them together: for every tile what its span's entering carry becomes on the way to it, and what it becomes behind the span;
+// k_recur_join then goes along the spans.  All in a fixed order, so that a result does not depend on which wave was first.
+constexpr int kSpan = 16;
+struct Carries {
+    float *b, *a;                       // [tiles, dim]: what enters a tile is b, or a * (what enters its span) + b where `open`
+    float *span_b, *span_a;             // [spans, dim]: what the span before hands on; after the join, span_b is what enters
+    uint8_t *open, *span_open;
+    int32_t* list;                      // list of a tile's first place, or (backward) its last one
+    int64_t tile_rows, tiles;
+};
+
+template <int V>
+struct Effect {
+    float a[V], b[V];
+    bool open;
+};
+// `e` followed by an effect that lies in LDS.
+template <int V>
+__device__ __forceinline__ void follow(Effect<V>& e, const float* a, const float* b, bool open) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        e.b[i] = open ? a[i] * e.b[i] + b[i] : b[i];
+        e.a[i] *= a[i];
+    }
+    e.open = e.open && open;
+}
+
+template <int V, bool FORWARD>
+__device__ __forceinline__ void join_span(const Carries& t, const Effect<V>& mine, int64_t span, int64_t tile, int dim, int c, bool lead) {
+    __shared__ float s_a[kSpan][kWave * V], s_b[kSpan][kWave * V];
+    __shared__ int s_open[kSpan];
+    const int lane = threadIdx.x & 63, w = uniform((int)(threadIdx.x >> 6));
+    store_floats<V>(&s_a[w][lane * V], mine.a);
+    store_floats<V>(&s_b[w][lane * V], mine.b);
+    if (lane == 0) s_open[w] = mine.open;
+    __syncthreads();
+    Effect<V> e;
+#pragma unroll
+    for (int i = 0; i < V; ++i) { e.a[i] = 1.0f; e.b[i] = 0.0f; }
+    e.open = true;
+    const int before = FORWARD ? w : kSpan - 1 - w;      // tiles of the span on the way to this one
+    for (int k = 0; k < before; ++k) {
+        const int from = FORWARD ? k : kSpan - 1 - k;
+        follow<V>(e, &s_a[from][lane * V], &s_b[from][lane * V], s_open[from]);
+    }
+    if (tile < t.tiles) {
+        store_floats<V>(t.b + tile * dim + c, e.b);
+        if (e.open) store_floats<V>(t.a + tile * dim + c, e.a);
+        if (lead) t.open[tile] = e.open;
+    }
+    const int64_t to = FORWARD ? span + 1 : span - 1;
+    if (before == kSpan - 1 && to >= 0 && to * kSpan < t.tiles) {
+        follow<V>(e, mine.a, mine.b, mine.open);
+        store_floats<V>(t.span_b + to * dim + c, e.b);
+        if (e.open) store_floats<V>(t.span_a + to * dim + c, e.a);
+        if (lead) t.span_open[to] = e.open;
+    }
+}
+// What enters a tile that its list reaches into.
+template <int V>
+__device__ __forceinline__ void carry_of(const Carries& t, int64_t tile, int dim, int c, float (&v)[V]) {
+    float a[V], b[V], e[V];
+    const bool open = uniform((int)t.open[tile]);
+    load_floats<V>(t.b + tile * dim + c, b);
+    load_floats<V>(t.a + tile * dim + c, a);             // (whatever lies there where it is not open)
+    load_floats<V>(t.span_b + tile / kSpan * dim + c, e);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = open ? a[i] * e[i] + b[i] : b[i];
+}
 
 template <typename T, int V, bool DECAY>
-__global__ void __launch_bounds__(256) k_recur_tails(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, float* carry, float* factor, uint8_t* open) {
-    const int64_t wave = wave_id();
-    const Unit<V> w(l.dim, blocks, wave);
-    if (w.tile >= tiles - 1) return;
-    const int64_t total = l.total(), begin = w.tile * tile_rows, end = begin + tile_rows;
-    bool is_open = false;
+__global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l, const Carries t, int blocks) {
+    const Share share(blockIdx.x, blocks);
+    const int64_t span = share.q, tile = span * kSpan + uniform((int)(threadIdx.x >> 6));
+    if (span * kSpan >= t.tiles) return;
+    const int c = channel_of<V>(l.dim, share.block);
+    const bool lead = share.block == 0 && (threadIdx.x & 63) == 0;
+    const int64_t total = l.total(), begin = tile * t.tile_rows, end = begin + t.tile_rows;
+    Effect<V> e = {};
     if (end < total) {
-        const int j = find_list(l, total, end - 1);
+        const int j = find_list(l, total, end);
+        if (lead) t.list[tile + 1] = j;
         const int64_t first = uniform(l.begin_of(j, total));
-        if (uniform(l.begin_of((int64_t)j + 1, total)) > end) {
-            is_open = first < begin;
-            float rate[V], h[V], a[V];
-            rates<V, DECAY>(l, w.c, rate);
-            load_or_zero<V>(is_open || !l.h0 ? nullptr : l.h0_of(j) + w.c, h);
+        if (first < end) {
+            e.open = first < begin;
+            float rate[V];
+            rates<V, DECAY>(l, c, rate);
+            load_or_zero<V>(e.open || !l.h0 ? nullptr : l.h0_of(j) + c, e.b);
 #pragma unroll
-            for (int i = 0; i < V; ++i) a[i] = 1.0f;
+            for (int i = 0; i < V; ++i) e.a[i] = 1.0f;
             Pack<T, V> u[kSaved], x[kSaved];
             const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total);
             for (int64_t p = max(first, begin); p < end; p += kSaved) {
-                read_rows<T, V>(u, rows_u, total, p, w.c);
-                read_rows<T, V>(x, rows_x, total, p, w.c);
+                read_rows<T, V>(u, rows_u, end, p, c);
+                read_rows<T, V>(x, rows_x, end, p, c);
                 float gap = 0.0f;
                 if (DECAY) {
                     const int64_t q = min(p + (threadIdx.x & (kSaved - 1)), end - 1);
-                    const float t = l.ts[l.row(q, total)];
-                    gap = q == first ? l.t0 ? gap_of(t, l.t0[l.list(j)]) : 0.0f : gap_of(t, l.ts[l.row(q - 1, total)]);
+                    const float t1 = l.ts[l.row(q, total)], t0 = l.ts[l.row(max(q - 1, (int64_t)0), total)];
+                    gap = gap_of(t1, q != first ? t0 : l.t0 ? l.t0[l.list(j)] : t1);
                 }
                 const int n = (int)min(end - p, (int64_t)kSaved);
                 each_row(n, [&](int r) {
@@ -379,41 +458,41 @@ __global__ void __launch_bounds__(256) k_recur_tails(const Lists<T> l, int64_t t
                     gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, r) : 0.0f, z, rest, f);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        h[i] = f[i] * h[i] + z[i] * x[r].get(i);
-                        a[i] *= f[i];
+                        e.b[i] = f[i] * e.b[i] + z[i] * x[r].get(i);
+                        e.a[i] *= f[i];
                     }
                 });
             }
-            store_floats<V>(carry + (w.tile + 1) * l.dim + w.c, h);
-            if (is_open) store_floats<V>(factor + (w.tile + 1) * l.dim + w.c, a);
         }
     }
-    if (wave % blocks == 0 && (threadIdx.x & 63) == 0) open[w.tile + 1] = is_open;
+    join_span<V, true>(t, e, span, tile, l.dim, c, lead);
 }
 
 template <typename T, int V, bool DECAY>
-__global__ void __launch_bounds__(256) k_recur_heads(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, const T* dh, int64_t ld_dh, const float* dlast,
-                                                     float* carry, float* factor, uint8_t* open) {
-    const int64_t wave = wave_id();
-    const Unit<V> w(l.dim, blocks, wave);
-    if (w.tile >= tiles - 1) return;
-    const int64_t total = l.total(), begin = (w.tile + 1) * tile_rows;      // (tile 0 has nothing before it)
-    bool is_open = false;
-    if (begin < total) {
-        const int j = find_list(l, total, begin);
-        if (uniform(l.begin_of(j, total)) < begin) {
-            const int64_t last = uniform(l.begin_of((int64_t)j + 1, total)), end = min(last, begin + tile_rows);
-            is_open = end < last;
-            float rate[V], back[V], a[V];
-            rates<V, DECAY>(l, w.c, rate);
-            load_or_zero<V>(is_open || !dlast ? nullptr : dlast + l.list(j) * l.dim + w.c, back);
+__global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l, const Carries t, int blocks, const T* dh, int64_t ld_dh, const float* dlast) {
+    const Share share(blockIdx.x, blocks);
+    const int64_t span = share.q, tile = span * kSpan + uniform((int)(threadIdx.x >> 6));
+    if (span * kSpan >= t.tiles) return;
+    const int c = channel_of<V>(l.dim, share.block);
+    const bool lead = share.block == 0 && (threadIdx.x & 63) == 0;
+    const int64_t total = l.total(), begin = tile * t.tile_rows;
+    Effect<V> e = {};
+    if (begin > 0 && begin < total) {
+        const int j = find_list(l, total, begin - 1);
+        if (lead) t.list[tile - 1] = j;
+        const int64_t last = uniform(l.begin_of((int64_t)j + 1, total)), end = min(last, begin + t.tile_rows);
+        if (last > begin) {
+            e.open = end < last;
+            float rate[V];
+            rates<V, DECAY>(l, c, rate);
+            load_or_zero<V>(e.open || !dlast ? nullptr : dlast + l.list(j) * l.dim + c, e.b);
 #pragma unroll
-            for (int i = 0; i < V; ++i) a[i] = 1.0f;
+            for (int i = 0; i < V; ++i) e.a[i] = 1.0f;
             Pack<T, V> u[kSaved], d[kSaved] = {};
             const Along rows_u(l, l.u, l.ld_u, total), rows_d(l, dh, ld_dh, total);
             for (int64_t p = begin + (end - 1 - begin) / kSaved * kSaved; p >= begin; p -= kSaved) {
-                read_rows<T, V>(u, rows_u, total, p, w.c);
-                if (dh) read_rows<T, V>(d, rows_d, total, p, w.c);
+                read_rows<T, V>(u, rows_u, end, p, c);
+                if (dh) read_rows<T, V>(d, rows_d, end, p, c);
                 float gap = 0.0f;
                 if (DECAY) {
                     const int64_t q = min(p + (threadIdx.x & (kSaved - 1)), end - 1);
@@ -425,29 +504,27 @@ __global__ void __launch_bounds__(256) k_recur_heads(const Lists<T> l, int64_t t
                     gates<V, DECAY>(u[r], rate, DECAY ? read_lane(gap, r) : 0.0f, z, rest, f);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        back[i] += d[r].get(i);
-                        back[i] *= f[i];
-                        a[i] *= f[i];
+                        e.b[i] += d[r].get(i);
+                        e.b[i] *= f[i];
+                        e.a[i] *= f[i];
                     }
                 });
             }
-            store_floats<V>(carry + w.tile * l.dim + w.c, back);
-            if (is_open) store_floats<V>(factor + w.tile * l.dim + w.c, a);
         }
     }
-    if (wave % blocks == 0 && (threadIdx.x & 63) == 0) open[w.tile] = is_open;
+    join_span<V, false>(t, e, span, tile, l.dim, c, lead);
 }
 
-// Puts the open tiles' carries together, from tile 1 on or (BACKWARD) from the last but one down: kChannels channels a workgroup, each
-// with kParts parts of the tiles: every thread joins its part, the parts are scanned, every thread goes through its part again.
+// Puts the open spans' carries together, from span 1 on or (BACKWARD) from the last but one down: kChannels channels a workgroup, each
+// with kParts parts of the spans: every thread joins its part, the parts are scanned, every thread goes through its part again.
 constexpr int kChannels = 8, kParts = 1024 / kChannels, kAtOnce = 8;
 template <bool BACKWARD>
-__global__ void __launch_bounds__(1024) k_recur_join(int64_t tiles, int dim, float* carry, const float* factor, const uint8_t* open) {
+__global__ void __launch_bounds__(1024) k_recur_join(int64_t spans, int dim, float* carry, const float* factor, const uint8_t* open) {
     __shared__ float s_a[2][kParts][kChannels], s_b[2][kParts][kChannels];
     __shared__ int s_any;
     if (threadIdx.x == 0) s_any = 0;
     __syncthreads();
-    const int64_t n = tiles - 1;                            // carries that tiles have written
+    const int64_t n = spans - 1;                            // carries that spans have written
     auto at = [&](int64_t i) { return BACKWARD ? n - 1 - i : i + 1; };
     int any = 0;
     for (int64_t i = threadIdx.x; i < n; i += 1024) any |= open[at(i)];
@@ -465,10 +542,10 @@ __global__ void __launch_bounds__(1024) k_recur_join(int64_t tiles, int dim, flo
             const int64_t k = at(min(i + r, end - 1));
             is[r] = open[k];
             v[r] = carry[k * dim + c];
-            f[r] = factor[k * dim + c];                     // (whatever lies there if the tile was closed)
+            f[r] = factor[k * dim + c];                     // (whatever lies there if the span was closed)
         }
     };
-    float a = 1.0f, b = 0.0f;                               // what the part does to the carry that enters it: b alone once a tile was closed
+    float a = 1.0f, b = 0.0f;                               // what the part does to the carry that enters it: b alone once a span was closed
     bool all = true;
     for (int64_t i = begin; i < end; i += kAtOnce) {
         read(i);
@@ -496,7 +573,7 @@ __global__ void __launch_bounds__(1024) k_recur_join(int64_t tiles, int dim, flo
         s_b[from ^ 1][part][ch] = ob;
     }
     __syncthreads();
-    float enter = part ? s_b[from][part - 1][ch] : 0.0f;    // (the first tile written is never open: no list crosses the walk's ends)
+    float enter = part ? s_b[from][part - 1][ch] : 0.0f;    // (the first span is never open: no list crosses the walk's ends)
     for (int64_t i = begin; i < end; i += kAtOnce) {
         read(i);
 #pragma unroll
@@ -524,30 +601,33 @@ __device__ void fill_empty(const Lists<T>& l, int64_t first, const float* from, 
 }
 
 template <typename T, int V, bool DECAY>
-__global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, const float* carry, T* h_out, int64_t ld_h,
-                                                      float* last, float* saved) {
-    const int64_t wave = wave_id();
-    if (wave >= tiles * blocks) {
-        const int64_t first = (wave - tiles * blocks) * kWave;
+__global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Carries t, int blocks, T* h_out, int64_t ld_h, float* last, float* saved) {
+    const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
+    const int wave = uniform((int)(threadIdx.x >> 6));
+    if (blockIdx.x >= quads) {
+        const int64_t first = ((blockIdx.x - quads) * kWaves + wave) * kWave;
         if (last && first < l.S) fill_empty(l, first, l.h0, last);
         return;
     }
-    const Unit<V> w(l.dim, blocks, wave);
-    const int64_t total = l.total(), begin = w.tile * tile_rows, end = min(begin + tile_rows, total);
+    const Share share(blockIdx.x, blocks);
+    const int64_t tile = share.q * kWaves + wave;
+    const int c = channel_of<V>(l.dim, share.block);
+    const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
     if (begin >= end) return;
     Pack<T, V> u[kSaved], x[kSaved];
     const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total);
     const Along rows_h(l, h_out, ld_h, total);
-    read_rows<T, V>(u, rows_u, total, begin, w.c);
-    read_rows<T, V>(x, rows_x, total, begin, w.c);
+    read_rows<T, V>(u, rows_u, total, begin, c);
+    read_rows<T, V>(x, rows_x, total, begin, c);
     float rate[V], h[V];
-    rates<V, DECAY>(l, w.c, rate);
-    const int j = find_list(l, total, begin);
+    rates<V, DECAY>(l, c, rate);
+    const int j = tile ? uniform(t.list[tile]) : find_list(l, total, 0);
     const bool fresh = uniform(l.begin_of(j, total)) == begin;
-    load_or_zero<V>(fresh ? nullptr : carry + w.tile * l.dim + w.c, h);
+    if (fresh) load_or_zero<V>(nullptr, h);
+    else carry_of<V>(t, tile, l.dim, c, h);
     Batch b = locate<true, DECAY>(l, total, look_ahead<true, DECAY>(l, total, begin, j), fresh, 0, DECAY ? l.ts[l.row(max(begin - 1, (int64_t)0), total)] : 0.0f);
     Edges<V> enter;
-    enter.template read<true>(l.h0, b, (uint32_t)b.starts & kGroupMask, 0, l.dim, w.c);
+    enter.template read<true>(l.h0, b, (uint32_t)b.starts & kGroupMask, 0, l.dim, c);
     Ahead ahead = look_ahead<true, DECAY>(l, total, begin + kBatch, b.edge);
     float time = DECAY ? l.ts[l.row(min(begin + kBatch - 1, total - 1), total)] : 0.0f;
     for (int64_t p = begin; p < end; p += kSaved) {
@@ -561,10 +641,10 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t 
         Pack<T, V> next_u[kSaved], next_x[kSaved];
         Edges<V> next_enter;
         if (more) {
-            read_rows<T, V>(next_u, rows_u, total, p + kSaved, w.c);
-            read_rows<T, V>(next_x, rows_x, total, p + kSaved, w.c);
+            read_rows<T, V>(next_u, rows_u, total, p + kSaved, c);
+            read_rows<T, V>(next_x, rows_x, total, p + kSaved, c);
             const int next_q = turn ? 0 : q + kSaved;
-            next_enter.template read<true>(l.h0, next, (uint32_t)(next.starts >> next_q) & kGroupMask, next_q, l.dim, w.c);
+            next_enter.template read<true>(l.h0, next, (uint32_t)(next.starts >> next_q) & kGroupMask, next_q, l.dim, c);
         }
         if (more && turn) {
             ahead = look_ahead<true, DECAY>(l, total, p + kSaved + kBatch, next.edge);
@@ -572,18 +652,18 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t 
         }
         const int n = (int)min(end - p, (int64_t)kSaved);
         const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
-        if (saved) store_floats<V>(saved + p / kSaved * l.dim + w.c, h);
+        if (saved) store_floats<V>(saved + p / kSaved * l.dim + c, h);
         Global to = rows_h.at(p);
         each_row(n, [&](int r) {
-            if (starts >> r & 1) enter.take(l.h0, b, q + r, l.dim, w.c, h);
+            if (starts >> r & 1) enter.take(l.h0, b, q + r, l.dim, c, h);
             float z[V], rest[V], f[V];
             gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z, rest, f);
 #pragma unroll
             for (int i = 0; i < V; ++i) h[i] = f[i] * h[i] + z[i] * x[r].get(i);
-            if (h_out) store_row<T, V>(to, (uint32_t)w.c * sizeof(T), h);
+            if (h_out) store_row<T, V>(to, (uint32_t)c * sizeof(T), h);
             to = rows_h.next(to);
             if (ends >> r & 1)
-                if (last) store_floats<V>(last + (Edges<V>::at(last, b, q + r, l.dim) - last) + w.c, h);
+                if (last) store_floats<V>(last + (Edges<V>::at(last, b, q + r, l.dim) - last) + c, h);
         });
 #pragma unroll
         for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; }
@@ -595,16 +675,19 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, int64_t 
 // ---- gradients -----------------------------------------------------------------------------------------
 
 template <typename T, int V, bool DECAY>
-__global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t tile_rows, int64_t tiles, int blocks, const float* carry, const float* saved, const T* dh,
-                                                     int64_t ld_dh, const float* dlast, T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
-    const int64_t wave = wave_id();
-    if (wave >= tiles * blocks) {
-        const int64_t first = (wave - tiles * blocks) * kWave;
+__global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Carries t, int blocks, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
+                                                     T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
+    const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
+    const int wave = uniform((int)(threadIdx.x >> 6));
+    if (blockIdx.x >= quads) {
+        const int64_t first = ((blockIdx.x - quads) * kWaves + wave) * kWave;
         if (dh0 && first < l.S) fill_empty(l, first, dlast, dh0);
         return;
     }
-    const Unit<V> w(l.dim, blocks, wave);
-    const int64_t total = l.total(), begin = w.tile * tile_rows, end = min(begin + tile_rows, total);
+    const Share share(blockIdx.x, blocks);
+    const int64_t tile = share.q * kWaves + wave;
+    const int c = channel_of<V>(l.dim, share.block);
+    const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
     float sum[V] = {};
     if (begin < end) {
         const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved, last_batch = begin + (end - 1 - begin) / kBatch * kBatch;
@@ -613,27 +696,28 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
         const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total), rows_d(l, dh, ld_dh, total);
         const Along rows_du(l, du, ld_du, total), rows_dx(l, dx, ld_dx, total);
         auto read_inputs = [&](int64_t p) {
-            read_rows<T, V>(u, rows_u, total, p, w.c);
-            read_rows<T, V>(x, rows_x, total, p, w.c);
-            load_floats<V>(saved + p / kSaved * l.dim + w.c, enter);
+            read_rows<T, V>(u, rows_u, total, p, c);
+            read_rows<T, V>(x, rows_x, total, p, c);
+            load_floats<V>(saved + p / kSaved * l.dim + c, enter);
         };
         auto read_grads = [&](int64_t p) {
-            if (dh) read_rows<T, V>(d, rows_d, total, p, w.c);
+            if (dh) read_rows<T, V>(d, rows_d, total, p, c);
         };
         read_inputs(last_group);
         read_grads(last_group);
         float rate[V], back[V];
-        rates<V, DECAY>(l, w.c, rate);
-        const int j = find_list(l, total, end - 1);
+        rates<V, DECAY>(l, c, rate);
+        const int j = end < total ? uniform(t.list[tile]) : find_list(l, total, end - 1);
         const bool over = uniform(l.begin_of((int64_t)j + 1, total)) <= end;
-        load_or_zero<V>(over ? nullptr : carry + w.tile * l.dim + w.c, back);
+        if (over) load_or_zero<V>(nullptr, back);
+        else carry_of<V>(t, tile, l.dim, c, back);
         auto time_before = [&](int64_t p) { return DECAY ? l.ts[l.row(max(p - 1, (int64_t)0), total)] : 0.0f; };
         Batch b = locate<false, DECAY>(l, total, look_ahead<false, DECAY>(l, total, last_batch, j), over, (int)(end - 1 - last_batch), time_before(last_batch));
         Edges<V> start, leave;
         auto part = [](uint64_t bits, int q) { return (uint32_t)(bits >> q) & kGroupMask; };
         int q = (int)(last_group - last_batch);
-        start.template read<true>(l.h0, b, part(b.starts, q), q, l.dim, w.c);
-        leave.template read<false>(dlast, b, part(b.ends, q), q, l.dim, w.c);
+        start.template read<true>(l.h0, b, part(b.starts, q), q, l.dim, c);
+        leave.template read<false>(dlast, b, part(b.ends, q), q, l.dim, c);
         Ahead ahead = look_ahead<false, DECAY>(l, total, last_batch - kBatch, b.edge);
         float time = time_before(last_batch - kBatch);
         for (int64_t p = last_group; p >= begin; p -= kSaved) {
@@ -650,7 +734,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
             // Forward through the group: dx = z back, du = slope back, and what the event keeps of the state before it.
             float z[kSaved][V], f[kSaved][V], slope[kSaved][V], kept[kSaved][V];
             each_row(n, [&](int r) {
-                if (starts >> r & 1) start.take(l.h0, b, q + r, l.dim, w.c, h);
+                if (starts >> r & 1) start.take(l.h0, b, q + r, l.dim, c, h);
                 float rest[V];
                 gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z[r], rest, f[r]);
 #pragma unroll
@@ -668,7 +752,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
             const int next_q = turn ? kBatch - kSaved : q - kSaved;
             if (more) {
                 read_inputs(p - kSaved);
-                start.template read<true>(l.h0, next, part(next.starts, next_q), next_q, l.dim, w.c);
+                start.template read<true>(l.h0, next, part(next.starts, next_q), next_q, l.dim, c);
             }
             if (more && turn) {
                 ahead = look_ahead<false, DECAY>(l, total, p - 2 * kBatch, next.edge);
@@ -676,7 +760,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
             }
             Global to_x = rows_dx.at(p + n - 1), to_u = rows_du.at(p + n - 1);
             each_row_back(n, [&](int r) {
-                if (ends >> r & 1) leave.take(dlast, b, q + r, l.dim, w.c, back);
+                if (ends >> r & 1) leave.take(dlast, b, q + r, l.dim, c, back);
                 const float g = DECAY ? read_lane(b.gap, q + r) : 0.0f;
                 float vu[V], vx[V];
 #pragma unroll
@@ -687,34 +771,44 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, int64_t t
                     if (DECAY) sum[i] -= kept[r][i] * back[i] * g;
                     back[i] *= f[r][i];
                 }
-                store_row<T, V>(to_x, (uint32_t)w.c * sizeof(T), vx);
-                store_row<T, V>(to_u, (uint32_t)w.c * sizeof(T), vu);
+                store_row<T, V>(to_x, (uint32_t)c * sizeof(T), vx);
+                store_row<T, V>(to_u, (uint32_t)c * sizeof(T), vu);
                 to_x = rows_dx.back(to_x);
                 to_u = rows_du.back(to_u);
                 if (starts >> r & 1)
-                    if (dh0) store_floats<V>(dh0 + (Edges<V>::at(dh0, b, q + r, l.dim) - dh0) + w.c, back);
+                    if (dh0) store_floats<V>(dh0 + (Edges<V>::at(dh0, b, q + r, l.dim) - dh0) + c, back);
             });
             if (more) {
                 read_grads(p - kSaved);
-                leave.template read<false>(dlast, next, part(next.ends, next_q), next_q, l.dim, w.c);
+                leave.template read<false>(dlast, next, part(next.ends, next_q), next_q, l.dim, c);
             }
             b = next;
             q = next_q;
         }
     }
-    if (DECAY && sums) store_floats<V>(sums + w.tile * l.dim + w.c, sum);
+    if (DECAY && sums) {                // the workgroup's share
+        __shared__ float s_sum[kWaves][kWave * V];
+        store_floats<V>(&s_sum[wave][(threadIdx.x & 63) * V], sum);
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += s_sum[k][(threadIdx.x & 63) * V + i];
+        if (share.q * kWaves < t.tiles) store_floats<V>(sums + share.q * l.dim + c, sum);
+    }
 }
 
-// Sums of the tiles' shares, kChannels channels a workgroup, in a fixed order.
-__global__ void __launch_bounds__(1024) k_recur_sums(const float* sums, int64_t tiles, int dim, float* out) {
+// Sums of the workgroups' shares, kChannels channels a workgroup, in a fixed order.
+__global__ void __launch_bounds__(1024) k_recur_sums(const float* sums, int64_t shares, int dim, float* out) {
     __shared__ float s_sum[kParts][kChannels];
     const int part = threadIdx.x / kChannels, ch = threadIdx.x % kChannels, c = (int)blockIdx.x * kChannels + ch;
     float sum = 0.0f;
     if (c < dim)
-        for (int64_t k = part; k < tiles; k += kParts * kAtOnce) {
+        for (int64_t k = part; k < shares; k += kParts * kAtOnce) {
             float v[kAtOnce];
 #pragma unroll
-            for (int r = 0; r < kAtOnce; ++r) v[r] = k + r * kParts < tiles ? sums[(k + r * kParts) * dim + c] : 0.0f;
+            for (int r = 0; r < kAtOnce; ++r) v[r] = k + r * kParts < shares ? sums[(k + r * kParts) * dim + c] : 0.0f;
 #pragma unroll
             for (int r = 0; r < kAtOnce; ++r) sum += v[r];
         }
@@ -778,32 +872,45 @@ int check_workspace(const void* p, size_t have, size_t need) {
     return TNS_OK;
 }
 
-// Rows of a tile: as many as leave a wave for every place of the chip (1024 SIMDs, four waves each and more), 16 to 1024.
+// Rows of a tile.  A wave takes a tile's rows one after the other, so a small call is as long as its tiles; the fewer waves a large one
+// has, the less their reads overlap and the more unevenly they fill the chip; and every tile has its carry to find.
+// (A launch has fewer than 2^32 threads: tiles grow where there would be more than 2^20 workgroups of a span.)
 int64_t tile_rows_of(int64_t rows, int dim) {
     const int64_t blocks = (dim + kWave - 1) / kWave;
-    int64_t n = kSaved;
-    while (n < 1024 && rows / n * blocks > 8192) n *= 2;
+    int64_t n = rows / 64 * blocks < 2048 ? 32 : 64;
+    while ((rows / (n * kSpan) + 1) * blocks > 1 << 20) n *= 2;
     return n;
 }
 
 size_t aligned(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
-struct Workspace {                      // carries and factors of the tiles, which of them are open; sums in the factors' place
-    int64_t tile_rows, tiles;
-    float *carry, *factor;
-    uint8_t* open;
+struct Workspace {
+    Carries t;
+    int64_t spans;
+    float* sums;                        // [workgroups of a gradient, dim]
     size_t bytes;
 };
 Workspace carve(const tns_recur& r, void* base) {
     Workspace w{};
-    w.tile_rows = tile_rows_of(r.rows, r.dim);
-    w.tiles = (r.rows + w.tile_rows - 1) / w.tile_rows;
-    const size_t rows = aligned((size_t)w.tiles * r.dim * 4);
-    char* const p = static_cast<char*>(base);
-    w.carry = reinterpret_cast<float*>(p);
-    w.factor = reinterpret_cast<float*>(p + rows);
-    w.open = reinterpret_cast<uint8_t*>(p + 2 * rows);
-    w.bytes = 2 * rows + aligned((size_t)w.tiles);
+    w.t.tile_rows = tile_rows_of(r.rows, r.dim);
+    w.t.tiles = (r.rows + w.t.tile_rows - 1) / w.t.tile_rows;
+    w.spans = (w.t.tiles + kSpan - 1) / kSpan;
+    char* p = static_cast<char*>(base);
+    auto take = [&](size_t bytes) {
+        void* const at = p;
+        p += aligned(bytes);
+        w.bytes += aligned(bytes);
+        return at;
+    };
+    const size_t row = (size_t)r.dim * 4;
+    w.t.b = static_cast<float*>(take(w.t.tiles * row));
+    w.t.a = static_cast<float*>(take(w.t.tiles * row));
+    w.t.span_b = static_cast<float*>(take(w.spans * row));
+    w.t.span_a = static_cast<float*>(take(w.spans * row));
+    w.t.open = static_cast<uint8_t*>(take(w.t.tiles));
+    w.t.span_open = static_cast<uint8_t*>(take(w.spans));
+    w.t.list = static_cast<int32_t*>(take(w.t.tiles * 4));
+    w.sums = static_cast<float*>(take((w.t.tiles + kWaves - 1) / kWaves * row));
     return w;
 }
 size_t saved_bytes(const tns_recur& r) { return (size_t)((r.rows + kSaved - 1) / kSaved) * r.dim * 4; }
@@ -814,46 +921,47 @@ Lists<T> typed(const tns_recur& r) {
             r.d_ts, r.d_decay, r.d_h0, r.d_t0, r.dim, (r.flags & TNS_NEWEST_FIRST) != 0};
 }
 
-// Grid of the kernels that have a wave for every tile and block of channels, and for every 64 lists where `lists` is set.
-struct Grid {
-    int blocks;
-    unsigned tails, all;
-};
-Grid grid_of(const tns_recur& r, const Workspace& w, int V, bool lists) {
-    const int blocks = (r.dim + kWave * V - 1) / (kWave * V);
-    auto groups = [](int64_t waves) { return (unsigned)((waves + kWaves - 1) / kWaves); };
-    return {blocks, w.tiles > 1 ? groups((w.tiles - 1) * blocks) : 0, groups(w.tiles * blocks + (lists ? (r.S + kWave - 1) / kWave : 0))};
+// Workgroups: of the kernels with one for every four tiles and block of channels, and every 256 lists where `lists` is set.
+unsigned groups_of(const tns_recur& r, const Workspace& w, int blocks, bool lists) {
+    return (unsigned)(workgroups_of((w.t.tiles + kWaves - 1) / kWaves, blocks) + (lists ? (r.S + kWaves * kWave - 1) / (kWaves * kWave) : 0));
+}
+template <int V> int blocks_of(const tns_recur& r) { return (r.dim + kWave * V - 1) / (kWave * V); }
+
+template <bool BACKWARD>
+void launch_join(const tns_recur& r, const Workspace& w, hipStream_t stream) {
+    if (w.spans > 1)
+        hipLaunchKernelGGL((k_recur_join<BACKWARD>), dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.spans, r.dim, w.t.span_b, w.t.span_a, w.t.span_open);
 }
 
 template <typename T, int V, bool DECAY>
 void launch_run(const tns_recur& r, void* h, int64_t ld_h, float* last, void* saved, void* workspace, hipStream_t stream) {
     const Workspace w = carve(r, workspace);
-    const Grid g = grid_of(r, w, V, last != nullptr);
+    const int blocks = blocks_of<V>(r);
     const Lists<T> l = typed<T>(r);
-    if (g.tails) {
-        hipLaunchKernelGGL((k_recur_tails<T, V, DECAY>), dim3(g.tails), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, w.carry, w.factor, w.open);
-        hipLaunchKernelGGL((k_recur_join<false>), dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.tiles, r.dim, w.carry, w.factor, w.open);
+    if (w.t.tiles > 1) {
+        hipLaunchKernelGGL((k_recur_tails<T, V, DECAY>), dim3((unsigned)workgroups_of(w.spans, blocks)), dim3(kSpan * kWave), 0, stream, l, w.t, blocks);
+        launch_join<false>(r, w, stream);
     }
-    if (g.all)
-        hipLaunchKernelGGL((k_recur_states<T, V, DECAY>), dim3(g.all), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, w.carry, static_cast<T*>(h), ld_h, last,
-                           static_cast<float*>(saved));
+    if (const unsigned groups = groups_of(r, w, blocks, last != nullptr))
+        hipLaunchKernelGGL((k_recur_states<T, V, DECAY>), dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<T*>(h), ld_h, last, static_cast<float*>(saved));
 }
 
 template <typename T, int V, bool DECAY>
 void launch_grad(const tns_recur& r, const void* saved, const void* dh, int64_t ld_dh, const float* dlast, void* du, int64_t ld_du, void* dx,
                  int64_t ld_dx, float* ddecay, float* dh0, void* workspace, hipStream_t stream) {
     const Workspace w = carve(r, workspace);
-    const Grid g = grid_of(r, w, V, dh0 != nullptr);
+    const int blocks = blocks_of<V>(r);
     const Lists<T> l = typed<T>(r);
     const T* const d = static_cast<const T*>(dh);
-    if (g.tails) {
-        hipLaunchKernelGGL((k_recur_heads<T, V, DECAY>), dim3(g.tails), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, d, ld_dh, dlast, w.carry, w.factor, w.open);
-        hipLaunchKernelGGL((k_recur_join<true>), dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.tiles, r.dim, w.carry, w.factor, w.open);
+    if (w.t.tiles > 1) {
+        hipLaunchKernelGGL((k_recur_heads<T, V, DECAY>), dim3((unsigned)workgroups_of(w.spans, blocks)), dim3(kSpan * kWave), 0, stream, l, w.t, blocks, d, ld_dh, dlast);
+        launch_join<true>(r, w, stream);
     }
-    if (g.all)
-        hipLaunchKernelGGL((k_recur_grads<T, V, DECAY>), dim3(g.all), dim3(256), 0, stream, l, w.tile_rows, w.tiles, g.blocks, w.carry, static_cast<const float*>(saved), d,
-                           ld_dh, dlast, static_cast<T*>(du), ld_du, static_cast<T*>(dx), ld_dx, dh0, ddecay ? w.factor : nullptr);
-    if (ddecay) hipLaunchKernelGGL(k_recur_sums, dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.factor, w.tiles, r.dim, ddecay);
+    if (const unsigned groups = groups_of(r, w, blocks, dh0 != nullptr))
+        hipLaunchKernelGGL((k_recur_grads<T, V, DECAY>), dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<const float*>(saved), d, ld_dh, dlast,
+                           static_cast<T*>(du), ld_du, static_cast<T*>(dx), ld_dx, dh0, ddecay ? w.sums : nullptr);
+    if (ddecay)
+        hipLaunchKernelGGL(k_recur_sums, dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.sums, (w.t.tiles + kWaves - 1) / kWaves, r.dim, ddecay);
 }
 
 // Calls `go` with the type, the channels a lane has and whether there is a decay.  Two channels in 16 bits where every row allows reads of
