@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/tns_train.h"
@@ -38,6 +39,7 @@ struct Tensor {
     int64_t n;
     uint64_t word0;                   // number of the random word of its first four weights
     float decay;
+    int32_t aligned;                  // four weights of every buffer can be read at once
 };
 
 struct Tile {
@@ -49,12 +51,25 @@ struct Step {                         // factors of one step, rounded to fp32 on
     float beta1, rest1, beta2, rest2, lr, rate, root, eps;
     uint64_t key;
 };
+__device__ __forceinline__ float step_keep(const Step& s, const Tensor& t) {
+#pragma clang fp contract(off)
+    return 1.0f - s.lr * t.decay;
+}
 
-// Largest of the wave's values, as the bits of magnitudes (a NaN is larger than everything).
+// Largest of the wave's values, as the bits of magnitudes (a NaN is larger than everything): four steps within the rows of sixteen
+// lanes, part of the vector instruction, then the rows' ends.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t max_with(uint32_t v) {
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-    for (int by = 32; by; by >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, by));
-    return v;
+    v = max_with<0x111, 0xf>(v);
+    v = max_with<0x112, 0xf>(v);
+    v = max_with<0x114, 0xf>(v);
+    v = max_with<0x118, 0xf>(v);
+    v = max_with<0x142, 0xa>(v);
+    v = max_with<0x143, 0xc>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // Four codes and their values.
@@ -63,15 +78,14 @@ __device__ __forceinline__ void from_codes(uint32_t codes, float scale, float (&
     v[0] = lo[0] * scale; v[1] = lo[1] * scale; v[2] = hi[0] * scale; v[3] = hi[1] * scale;
 }
 
-// The wave's 256 values as codes; `valid`: how many of the lane's four exist (the others are 0 and stay 0).
+// The wave's 256 values as codes and their scale.
 template <bool SIGNED>
 __device__ __forceinline__ uint32_t to_codes(const float (&v)[4], uint64_t random, float& scale) {
 #pragma clang fp contract(off)
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-    top = wave_max(top);
-    float t = __uint_as_float(top);
+    const float t = __uint_as_float(wave_max(top));
     if (t < 0x1p-100f) { scale = 0.0f; return 0; }
     scale = t * (1.0f / 448.0f);
     const float by = 448.0f / t;
@@ -88,68 +102,151 @@ __device__ __forceinline__ uint32_t to_codes(const float (&v)[4], uint64_t rando
     return codes;
 }
 
+// Four weights of a lane, as they lie in memory, and their step.
 template <int BITS, typename G>
-__global__ void __launch_bounds__(256) k_adamw(const Tensor* __restrict__ tensors, const Tile* __restrict__ tiles, const Step s, const float* __restrict__ grad_scale) {
-#pragma clang fp contract(off)
-    const float gs = grad_scale ? *grad_scale : 1.0f;
-    if (gs == 0.0f || !(fabsf(gs) <= 3.402823466e+38f)) return;
-    const Tile tile = tiles[blockIdx.x];
-    const Tensor t = tensors[tile.tensor];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float keep = 1.0f - s.lr * t.decay;
-    for (int j = 0; j < kTile / kBlock / 4; ++j) {
-        const int64_t block = (int64_t)tile.index * (kTile / kBlock) + wave * (kTile / kBlock / 4) + j, i0 = block * kBlock + lane * 4;
-        if (block * kBlock >= t.n) return;
-        const int n = (int)min(max(t.n - i0, (int64_t)0), (int64_t)4);
-        float g[4] = {}, m[4] = {}, v[4] = {}, r[4], p[4] = {};
-        uint32_t mc = 0, vc = 0;
+struct Four {
+    using Grads = typename std::conditional<std::is_same<G, float>::value, float4, uint2>::type;
+    float p[4], m[4], v[4];             // (32 bits)
+    float g[4];
+    uint32_t mc, vc;                    // (8 bits)
+    float m_scale, v_scale;
+
+    // All of them, from aligned addresses.
+    __device__ void read(const Tensor& t, int64_t block, int64_t i0) {
+        const float4 q = *reinterpret_cast<const float4*>(t.param + i0);
+        p[0] = q.x; p[1] = q.y; p[2] = q.z; p[3] = q.w;
+        const Grads r = *reinterpret_cast<const Grads*>(static_cast<const G*>(t.grad) + i0);
+        if constexpr (std::is_same<G, float>::value) {
+            g[0] = r.x; g[1] = r.y; g[2] = r.z; g[3] = r.w;
+        } else {
+            g[0] = __uint_as_float(r.x << 16); g[1] = __uint_as_float(r.x & 0xffff0000u);
+            g[2] = __uint_as_float(r.y << 16); g[3] = __uint_as_float(r.y & 0xffff0000u);
+        }
+        if (BITS == 32) {
+            const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(t.m) + i0), b = *reinterpret_cast<const float4*>(static_cast<const float*>(t.v) + i0);
+            m[0] = a.x; m[1] = a.y; m[2] = a.z; m[3] = a.w;
+            v[0] = b.x; v[1] = b.y; v[2] = b.z; v[3] = b.w;
+        } else {
+            mc = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.m) + i0);
+            vc = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.v) + i0);
+            m_scale = t.m_scale[block];
+            v_scale = t.v_scale[block];
+        }
+    }
+    __device__ void write(const Tensor& t, int64_t block, int64_t i0) const {
+        *reinterpret_cast<float4*>(t.param + i0) = make_float4(p[0], p[1], p[2], p[3]);
+        if (t.copy) {
+            bf16 c[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k < n) {
-                g[k] = as_float(static_cast<const G*>(t.grad)[i0 + k]) * gs;
-                p[k] = t.param[i0 + k];
-                if (BITS == 32) {
-                    m[k] = static_cast<const float*>(t.m)[i0 + k];
-                    v[k] = static_cast<const float*>(t.v)[i0 + k];
-                } else {
-                    mc |= (uint32_t)static_cast<const uint8_t*>(t.m)[i0 + k] << (8 * k);
-                    vc |= (uint32_t)static_cast<const uint8_t*>(t.v)[i0 + k] << (8 * k);
-                }
+            for (int k = 0; k < 4; ++k) c[k] = as_value<bf16>(p[k]);
+            *reinterpret_cast<uint2*>(t.copy + i0) = __builtin_bit_cast(uint2, c);
+        }
+        if (BITS == 32) {
+            *reinterpret_cast<float4*>(static_cast<float*>(t.m) + i0) = make_float4(m[0], m[1], m[2], m[3]);
+            *reinterpret_cast<float4*>(static_cast<float*>(t.v) + i0) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.m) + i0) = mc;
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + i0) = vc;
+            if ((threadIdx.x & 63) == 0) { t.m_scale[block] = m_scale; t.v_scale[block] = v_scale; }
+        }
+    }
+    // The first n of them, one by one; the others are zero.
+    __device__ void read(const Tensor& t, int64_t block, int64_t i0, int n) {
+        mc = vc = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool is = k < n;
+            g[k] = is ? as_float(static_cast<const G*>(t.grad)[i0 + k]) : 0.0f;
+            p[k] = is ? t.param[i0 + k] : 0.0f;
+            if (BITS == 32) {
+                m[k] = is ? static_cast<const float*>(t.m)[i0 + k] : 0.0f;
+                v[k] = is ? static_cast<const float*>(t.v)[i0 + k] : 0.0f;
+            } else if (is) {
+                mc |= (uint32_t)static_cast<const uint8_t*>(t.m)[i0 + k] << (8 * k);
+                vc |= (uint32_t)static_cast<const uint8_t*>(t.v)[i0 + k] << (8 * k);
             }
+        }
         if (BITS == 8) {
-            from_codes(mc, t.m_scale[block], m);
-            from_codes(vc, t.v_scale[block], r);
+            m_scale = t.m_scale[block];
+            v_scale = t.v_scale[block];
+        }
+    }
+    __device__ void write(const Tensor& t, int64_t block, int64_t i0, int n) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k >= n) continue;
+            t.param[i0 + k] = p[k];
+            if (t.copy) t.copy[i0 + k] = as_value<bf16>(p[k]);
+            if (BITS == 32) {
+                static_cast<float*>(t.m)[i0 + k] = m[k];
+                static_cast<float*>(t.v)[i0 + k] = v[k];
+            } else {
+                static_cast<uint8_t*>(t.m)[i0 + k] = (uint8_t)(mc >> (8 * k));
+                static_cast<uint8_t*>(t.v)[i0 + k] = (uint8_t)(vc >> (8 * k));
+            }
+        }
+        if (BITS == 8 && (threadIdx.x & 63) == 0) { t.m_scale[block] = m_scale; t.v_scale[block] = v_scale; }
+    }
+
+    // n of the lane's four exist (the others stay zero).  The weight's change is divided by the reciprocal of one unit in the last place;
+    // what is kept for the next step is rounded operation by operation, so that it is the same wherever it is computed.
+    __device__ void step(const Step& s, float keep, float gs, uint64_t word, int n) {
+#pragma clang fp contract(off)
+        float r[4];
+        if (BITS == 8) {
+            from_codes(mc, m_scale, m);
+            from_codes(vc, v_scale, r);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = r[k] * r[k];
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            m[k] = s.beta1 * m[k] + s.rest1 * g[k];
-            v[k] = s.beta2 * v[k] + s.rest2 * (g[k] * g[k]);
+            const float a = g[k] * gs;
+            m[k] = s.beta1 * m[k] + s.rest1 * a;
+            v[k] = s.beta2 * v[k] + s.rest2 * (a * a);
             r[k] = sqrtf(v[k]);
-            p[k] = p[k] * keep - (s.rate * m[k]) / (r[k] * s.root + s.eps);
-            if (k >= n) m[k] = r[k] = 0.0f;
+            p[k] = p[k] * keep - (s.rate * m[k]) * __builtin_amdgcn_rcpf(r[k] * s.root + s.eps);
+            if (BITS == 8 && k >= n) m[k] = r[k] = 0.0f;
         }
         if (BITS == 8) {
-            const uint64_t random = mix64(s.key + kGolden * (t.word0 + (uint64_t)(i0 >> 2) + 1));
-            float ms, vs;
-            mc = to_codes<true>(m, random, ms);
-            vc = to_codes<false>(r, random, vs);
-            if (lane == 0) { t.m_scale[block] = ms; t.v_scale[block] = vs; }
+            const uint64_t random = mix64(s.key + kGolden * (word + 1));
+            mc = to_codes<true>(m, random, m_scale);
+            vc = to_codes<false>(r, random, v_scale);
         }
+    }
+};
+
+// A workgroup per tile.  Bound by memory: what lies in it is read and written once; a wave reads its four blocks before it computes.
+template <int BITS, typename G>
+__global__ void __launch_bounds__(256) k_adamw(const Tensor* __restrict__ tensors, const Tile* __restrict__ tiles, const Step s, const float* __restrict__ grad_scale) {
+    const float gs = grad_scale ? *grad_scale : 1.0f;
+    if (gs == 0.0f || !(fabsf(gs) <= 3.402823466e+38f)) return;
+    const Tile tile = tiles[blockIdx.x];
+    const Tensor t = tensors[tile.tensor];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int kMine = kTile / kBlock / 4;                // blocks of a wave
+    const int64_t first = (int64_t)tile.index * (kTile / kBlock) + wave * kMine;
+    const float keep = step_keep(s, t);
+    if (t.aligned && (first + kMine) * kBlock <= t.n) {
+        Four<BITS, G> f[kMine];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k < n) {
-                t.param[i0 + k] = p[k];
-                if (t.copy) t.copy[i0 + k] = as_value<bf16>(p[k]);
-                if (BITS == 32) {
-                    static_cast<float*>(t.m)[i0 + k] = m[k];
-                    static_cast<float*>(t.v)[i0 + k] = v[k];
-                } else {
-                    static_cast<uint8_t*>(t.m)[i0 + k] = (uint8_t)(mc >> (8 * k));
-                    static_cast<uint8_t*>(t.v)[i0 + k] = (uint8_t)(vc >> (8 * k));
-                }
-            }
+        for (int j = 0; j < kMine; ++j) f[j].read(t, first + j, (first + j) * kBlock + lane * 4);
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+            const int64_t i0 = (first + j) * kBlock + lane * 4;
+            f[j].step(s, keep, gs, t.word0 + (uint64_t)(i0 >> 2), 4);
+            f[j].write(t, first + j, i0);
+        }
+        return;
+    }
+    for (int j = 0; j < kMine; ++j) {
+        const int64_t block = first + j, i0 = block * kBlock + lane * 4;
+        if (block * kBlock >= t.n) return;
+        const int n = (int)min(max(t.n - i0, (int64_t)0), (int64_t)4);
+        Four<BITS, G> f;
+        f.read(t, block, i0, n);
+        f.step(s, keep, gs, t.word0 + (uint64_t)(i0 >> 2), n);
+        f.write(t, block, i0, n);
     }
 }
 
@@ -198,7 +295,10 @@ int tns_adamw_create(const tns_adamw_config* cfg, int32_t count, const tns_adamw
         uint64_t word = 0;
         for (int32_t i = 0; i < count; ++i) {
             const tns_adamw_tensor& t = tensors[i];
-            ts.push_back({t.d_param, static_cast<bf16*>(t.d_copy), t.d_grad, t.d_m, t.d_v, t.d_m_scale, t.d_v_scale, t.n, word, (float)t.weight_decay});
+            auto at = [](const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; };
+            const size_t state = cfg->state_bits / 2, grad = cfg->grad_dtype == TNS_F32 ? 16 : 8;      // bytes of four values
+            const bool all = at(t.d_param, 16) && at(t.d_copy, 8) && at(t.d_grad, grad) && at(t.d_m, state) && at(t.d_v, state);
+            ts.push_back({t.d_param, static_cast<bf16*>(t.d_copy), t.d_grad, t.d_m, t.d_v, t.d_m_scale, t.d_v_scale, t.n, word, (float)t.weight_decay, all});
             for (int64_t k = 0; k * kTile < t.n; ++k) tiles.push_back({i, (uint32_t)k});
             word += (uint64_t)((t.n + kBlock - 1) / kBlock) * (kBlock / 4);
         }

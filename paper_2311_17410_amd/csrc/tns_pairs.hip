@@ -1,6 +1,7 @@
 // Paired log-ratio loss of true links against sampled ones, and its gradients (include/tns_train.h).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "../../include/tns_train.h"
@@ -25,9 +26,22 @@ struct Pairs {                        // tns_pairs with its types
     int dim;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
+constexpr int kWaves = 4;
+constexpr int64_t kMostGroups = 1 << 16;   // workgroups of a launch; they go round the events
+constexpr int kWide = 2048, kWideSingle = 512;      // channels that a wave holds at most, in vectors of four and one by one
+
+// Sum over the G lanes that share a row.
+template <int G>
+__device__ __forceinline__ float row_sum(float v) {
 #pragma unroll
-    for (int by = 32; by; by >>= 1) v += __shfl_xor(v, by);
+    for (int by = G / 2; by; by >>= 1) v += __shfl_xor(v, by);
+    return v;
+}
+// Sum over the rows of a wave, of values that are the same for the lanes of a row.
+template <int G>
+__device__ __forceinline__ float sum_of_rows(float v) {
+#pragma unroll
+    for (int by = 32; by >= G; by >>= 1) v += __shfl_xor(v, by);
     return v;
 }
 
@@ -39,65 +53,287 @@ __device__ __forceinline__ void loss_of(float m, float w, float scale, float smo
     if (m != m) loss = slope = m;
 }
 
-// A wave per event, its sampled links one after the other.
-template <typename T>
-__global__ void __launch_bounds__(64) k_pairs(const Pairs<T> p, float* losses, float* margin, T* danchor, T* dpos, T* dneg) {
-    const int64_t b = blockIdx.x;
-    const int lane = threadIdx.x;
-    const T* const a = p.anchor + b * p.ld_anchor;
-    const T* const q = p.pos + b * p.ld_pos;
-    float plus = 0.0f;
-    for (int c = lane; c < p.dim; c += 64) plus += as_float(a[c]) * as_float(q[c]);
-    plus = wave_sum(plus);
-    float total = 0.0f, csum = 0.0f;
-    bool any = false;
-    for (int64_t k = 0; k < p.K; ++k) {
-        const int64_t i = b * p.K + k;
-        const float w = p.weight ? p.weight[i] : 1.0f;
-        const T* const n = p.neg + i * p.dim;
-        float m = 0.0f, slope = 0.0f, loss = 0.0f;
-        if (w != 0.0f) {
-            float minus = 0.0f;
-            for (int c = lane; c < p.dim; c += 64) minus += as_float(a[c]) * as_float(n[c]);
-            minus = wave_sum(minus);
-            m = p.beta * (plus - minus - (p.ref ? p.ref[i] : 0.0f));
-            loss_of(m, w, p.scale, p.smoothing, loss, slope);
-            slope *= p.beta;
-            any = true;
-        }
-        total += loss;
-        csum += slope;
-        if (lane == 0 && margin) margin[i] = m;
-        if (danchor)
-            for (int c = lane; c < p.dim; c += 64) {
-                dneg[i * p.dim + c] = as_value<T>(w != 0.0f ? -slope * as_float(a[c]) : 0.0f);
-            }
+// VEC channels of a row as they lie in memory.
+template <typename T, int VEC>
+struct alignas(sizeof(T) * VEC) Vec {
+    T v[VEC];
+};
+template <typename T, int VEC>
+__device__ __forceinline__ void load(const T* p, bool there, float (&v)[VEC]) {
+    if (there) {
+        const Vec<T, VEC> raw = *reinterpret_cast<const Vec<T, VEC>*>(p);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = as_float(raw.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = 0.0f;
     }
-    if (lane == 0) losses[b] = total;
-    if (!danchor) return;
-    for (int c = lane; c < p.dim; c += 64) {
-        float da = 0.0f;
-        for (int64_t k = 0; k < p.K; ++k) {
-            const int64_t i = b * p.K + k;
-            const float w = p.weight ? p.weight[i] : 1.0f;
-            if (w != 0.0f) {
-                float minus = 0.0f;
-                for (int j = 0; j < p.dim; ++j) minus += as_float(a[j]) * as_float(p.neg[i * p.dim + j]);
-                float loss, slope;
-                loss_of(p.beta * (plus - minus - (p.ref ? p.ref[i] : 0.0f)), w, p.scale, p.smoothing, loss, slope);
-                da += slope * p.beta * (as_float(q[c]) - as_float(p.neg[i * p.dim + c]));
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store(T* p, const float (&v)[VEC]) {
+    Vec<T, VEC> raw;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) raw.v[i] = as_value<T>(v[i]);
+    *reinterpret_cast<Vec<T, VEC>*>(p) = raw;
+}
+
+struct Work {                         // how the links of an event are shared out
+    int64_t chunks, links;            // parts of an event that workgroups take, links of each
+    int waves;                        // of a workgroup on one part: 1 (four events a workgroup) or 4
+    float *losses, *parts, *sums;     // per workgroup; [B * chunks, dim] and [B * chunks, 2] where there are parts to join
+};
+
+// The loss and all gradients in one pass over the sampled links: G lanes hold a row, NV vectors of VEC channels each, and R rows are on
+// their way at a time; the anchor and the sum for its gradient stay in registers.  Bound by memory: (2 + K) rows read and written for
+// every event.
+template <typename T, int VEC, int G, int NV, bool GRADS>
+__global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, float* margin, T* danchor, T* dpos, T* dneg) {
+    constexpr int kRows = 64 / G, R = NV == 1 ? 4 : NV == 2 ? 2 : 1;
+    __shared__ float s_acc[kWaves - 1][GRADS ? G * VEC * NV : 1], s_sum[kWaves][3];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / G;
+    const int part_of = w.waves == 1 ? 0 : wave;             // which of the part's waves this is
+    int at[NV];
+    bool there[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        at[j] = (j * G + lane % G) * VEC;
+        there[j] = at[j] < p.dim;
+    }
+    float total = 0.0f;
+    const int64_t units = p.B * w.chunks, per = kWaves / w.waves;
+    for (int64_t first = (int64_t)blockIdx.x * per; first < units; first += (int64_t)gridDim.x * per) {
+        const int64_t unit = first + (w.waves == 1 ? wave : 0);
+        const bool real = unit < units;
+        const int64_t b = real ? unit / w.chunks : 0, k_begin = real ? unit % w.chunks * w.links : 0, k_end = real ? min(k_begin + w.links, p.K) : 0;
+        float a[NV][VEC], q[NV][VEC], acc[NV][VEC], dot = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            load<T, VEC>(p.anchor + b * p.ld_anchor + at[j], there[j], a[j]);
+            load<T, VEC>(p.pos + b * p.ld_pos + at[j], there[j], q[j]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                dot += a[j][i] * q[j][i];
+                acc[j][i] = 0.0f;
             }
         }
-        danchor[b * p.dim + c] = as_value<T>(da);
-        dpos[b * p.dim + c] = as_value<T>(any ? csum * as_float(a[c]) : 0.0f);
+        const float plus = row_sum<G>(dot);
+        float loss_sum = 0.0f, slope_sum = 0.0f, any = 0.0f;
+        for (int64_t k0 = k_begin + part_of * kRows * R; k0 < k_end; k0 += (int64_t)w.waves * kRows * R) {
+            float n[R][NV][VEC], weight[R], ref[R];
+            int64_t i[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int64_t k = k0 + r * kRows + row;
+                const bool is = k < k_end;
+                i[r] = b * p.K + (is ? k : k_begin);
+                weight[r] = is ? (p.weight ? p.weight[i[r]] : 1.0f) : 0.0f;
+                ref[r] = is && p.ref ? p.ref[i[r]] : 0.0f;
+                if (!is) i[r] = -1;
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < NV; ++j) load<T, VEC>(p.neg + i[r] * p.dim + at[j], there[j] && weight[r] != 0.0f, n[r][j]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float minus = 0.0f;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) minus += a[j][c] * n[r][j][c];
+                minus = row_sum<G>(minus);
+                float m = 0.0f, loss = 0.0f, slope = 0.0f;
+                if (weight[r] != 0.0f) {
+                    m = p.beta * (plus - minus - ref[r]);
+                    loss_of(m, weight[r], p.scale, p.smoothing, loss, slope);
+                    slope *= p.beta;
+                    any = 1.0f;
+                }
+                loss_sum += loss;
+                slope_sum += slope;
+                if (margin && i[r] >= 0 && lane % G == 0) margin[i[r]] = m;
+                if (GRADS) {
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) {
+                        float out[VEC];
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) {
+                            acc[j][c] -= slope * n[r][j][c];
+                            out[c] = weight[r] != 0.0f ? -slope * a[j][c] : 0.0f;
+                        }
+                        if (i[r] >= 0 && there[j]) store<T, VEC>(dneg + i[r] * p.dim + at[j], out);
+                    }
+                }
+            }
+        }
+        loss_sum = sum_of_rows<G>(loss_sum);
+        slope_sum = sum_of_rows<G>(slope_sum);
+        any = sum_of_rows<G>(any);
+        if (real) total += loss_sum;
+        if (GRADS) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) acc[j][c] = sum_of_rows<G>(acc[j][c]);
+            if (w.waves > 1) {                               // the waves' shares, in their order
+                __syncthreads();                             // (the part before has been read)
+                if (wave) {
+                    if (row == 0)
+#pragma unroll
+                        for (int j = 0; j < NV; ++j)
+#pragma unroll
+                            for (int c = 0; c < VEC; ++c) s_acc[wave - 1][at[j] + c] = acc[j][c];
+                    if (lane == 0) { s_sum[wave][0] = slope_sum; s_sum[wave][1] = any; }
+                }
+                __syncthreads();
+                if (wave == 0)
+                    for (int k = 1; k < kWaves; ++k) {
+                        slope_sum += s_sum[k][0];
+                        any += s_sum[k][1];
+#pragma unroll
+                        for (int j = 0; j < NV; ++j)
+#pragma unroll
+                            for (int c = 0; c < VEC; ++c) acc[j][c] += s_acc[k - 1][at[j] + c];
+                    }
+            }
+            if (real && part_of == 0 && row == 0) {
+                if (w.chunks > 1 && lane == 0) { w.sums[unit * 2] = slope_sum; w.sums[unit * 2 + 1] = any; }
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    if (!there[j]) continue;
+                    if (w.chunks > 1) {
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) w.parts[unit * p.dim + at[j] + c] = acc[j][c];
+                    } else {
+                        float da[VEC], dp[VEC];
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) {
+                            da[c] = any != 0.0f ? slope_sum * q[j][c] + acc[j][c] : 0.0f;
+                            dp[c] = any != 0.0f ? slope_sum * a[j][c] : 0.0f;
+                        }
+                        store<T, VEC>(danchor + b * p.dim + at[j], da);
+                        store<T, VEC>(dpos + b * p.dim + at[j], dp);
+                    }
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (lane == 0) s_sum[wave][2] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) w.losses[blockIdx.x] = (s_sum[0][2] + s_sum[1][2]) + (s_sum[2][2] + s_sum[3][2]);
+}
+
+// Rows too wide for a wave's registers: margins and slopes first, a wave for a part of an event's links ...
+template <typename T>
+__global__ void __launch_bounds__(256) k_pairs_wide(const Pairs<T> p, const Work w, float* margin, float* slopes) {
+    __shared__ float s_sum[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float total = 0.0f;
+    const int64_t units = p.B * w.chunks;
+    for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < units; unit += (int64_t)gridDim.x * kWaves) {
+        const int64_t b = unit / w.chunks, k_begin = unit % w.chunks * w.links, k_end = min(k_begin + w.links, p.K);
+        const T* const a = p.anchor + b * p.ld_anchor;
+        float plus = 0.0f;
+        for (int c = lane; c < p.dim; c += 64) plus += as_float(a[c]) * as_float(p.pos[b * p.ld_pos + c]);
+        plus = row_sum<64>(plus);
+        for (int64_t k = k_begin; k < k_end; ++k) {
+            const int64_t i = b * p.K + k;
+            const float weight = p.weight ? p.weight[i] : 1.0f;
+            float m = 0.0f, loss = 0.0f, slope = 0.0f;
+            if (weight != 0.0f) {
+                float minus = 0.0f;
+                for (int c = lane; c < p.dim; c += 64) minus += as_float(a[c]) * as_float(p.neg[i * p.dim + c]);
+                m = p.beta * (plus - row_sum<64>(minus) - (p.ref ? p.ref[i] : 0.0f));
+                loss_of(m, weight, p.scale, p.smoothing, loss, slope);
+            }
+            total += loss;
+            if (lane == 0 && margin) margin[i] = m;
+            if (lane == 0) slopes[i] = slope * p.beta;
+        }
+    }
+    if (lane == 0) s_sum[wave] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) w.losses[blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+}
+// ... and the gradients of 256 channels of an event a workgroup.
+template <typename T>
+__global__ void __launch_bounds__(256) k_pairs_wide_grads(const Pairs<T> p, const float* slopes, T* danchor, T* dpos, T* dneg) {
+    const int tiles = (p.dim + 255) / 256;
+    for (int64_t at = blockIdx.x; at < p.B * tiles; at += gridDim.x) {
+        const int64_t b = at / tiles;
+        const int c = (int)(at % tiles) * 256 + threadIdx.x;
+        if (c >= p.dim) continue;
+        const float a = as_float(p.anchor[b * p.ld_anchor + c]), q = as_float(p.pos[b * p.ld_pos + c]);
+        float acc = 0.0f, sum = 0.0f;
+        bool any = false;
+        for (int64_t i = b * p.K; i < (b + 1) * p.K; ++i) {
+            const bool is = !p.weight || p.weight[i] != 0.0f;
+            if (is) {
+                acc += slopes[i] * as_float(p.neg[i * p.dim + c]);
+                sum += slopes[i];
+                any = true;
+            }
+            dneg[i * p.dim + c] = as_value<T>(is ? -slopes[i] * a : 0.0f);
+        }
+        danchor[b * p.dim + c] = as_value<T>(any ? sum * q - acc : 0.0f);
+        dpos[b * p.dim + c] = as_value<T>(any ? sum * a : 0.0f);
     }
 }
 
-__global__ void __launch_bounds__(64) k_pairs_sum(const float* losses, int64_t n, float* out) {
-    float sum = 0.0f;
-    for (int64_t i = threadIdx.x; i < n; i += 64) sum += losses[i];
-    sum = wave_sum(sum);
-    if (threadIdx.x == 0) *out = sum;
+// Sum of the workgroups' losses (the first workgroup) and, where events were taken in parts, the gradients of anchor and pos from them:
+// kColumns channels of an event a workgroup, the parts shared by its threads.
+constexpr int kColumns = 64, kShares = 1024 / kColumns;
+template <typename T>
+__global__ void __launch_bounds__(1024) k_pairs_join(const Pairs<T> p, const Work w, int64_t groups, float* loss, T* danchor, T* dpos) {
+    __shared__ float s_v[1024], s_sum[kShares], s_any[kShares];
+    if (blockIdx.x == 0 && blockIdx.y == 0) {
+        float sum = 0.0f;
+        for (int64_t k = threadIdx.x; k < groups; k += 8 * 1024) {
+            float v[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] = k + r * 1024 < groups ? w.losses[k + r * 1024] : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) sum += v[r];
+        }
+        s_v[threadIdx.x] = sum;
+        for (int n = 512; n; n /= 2) {
+            __syncthreads();
+            if ((int)threadIdx.x < n) s_v[threadIdx.x] += s_v[threadIdx.x + n];
+        }
+        if (threadIdx.x == 0) *loss = s_v[0];
+        __syncthreads();
+    }
+    if (!danchor) return;
+    const int64_t b = blockIdx.y;
+    const int share = threadIdx.x / kColumns, c = blockIdx.x * kColumns + threadIdx.x % kColumns;
+    float acc = 0.0f, sum = 0.0f, any = 0.0f;
+    for (int64_t k = share; k < w.chunks; k += 8 * kShares) {
+        float v[8], s[8], n[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const int64_t unit = b * w.chunks + min(k + r * kShares, w.chunks - 1);
+            const bool is = k + r * kShares < w.chunks;
+            v[r] = is && c < p.dim ? w.parts[unit * p.dim + c] : 0.0f;
+            s[r] = is ? w.sums[unit * 2] : 0.0f;
+            n[r] = is ? w.sums[unit * 2 + 1] : 0.0f;
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) { acc += v[r]; sum += s[r]; any += n[r]; }
+    }
+    s_v[threadIdx.x] = acc;
+    if (threadIdx.x % kColumns == 0) { s_sum[share] = sum; s_any[share] = any; }
+    __syncthreads();
+    if (share || c >= p.dim) return;
+    acc = sum = any = 0.0f;
+    for (int k = 0; k < kShares; ++k) {
+        acc += s_v[k * kColumns + threadIdx.x];
+        sum += s_sum[k];
+        any += s_any[k];
+    }
+    const float a = as_float(p.anchor[b * p.ld_anchor + c]), q = as_float(p.pos[b * p.ld_pos + c]);
+    danchor[b * p.dim + c] = as_value<T>(any != 0.0f ? sum * q + acc : 0.0f);
+    dpos[b * p.dim + c] = as_value<T>(any != 0.0f ? sum * a : 0.0f);
 }
 
 int check(int64_t B, int64_t K, int32_t dim) {
@@ -107,7 +343,83 @@ int check(int64_t B, int64_t K, int32_t dim) {
     return TNS_OK;
 }
 
-size_t workspace_bytes_of(int64_t B, int64_t, int32_t) { return (size_t)B * 4; }
+size_t aligned(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+// Few events are cut into parts, so that there are some 2048 workgroups of four waves (two for every wave's place of the chip); a part
+// has 64 links at least.  An event of few links is one wave's.
+struct Workspace {
+    Work w;
+    float* slopes;                    // [B, K], of rows that may be too wide for a wave
+    size_t bytes;
+};
+Workspace carve(int64_t B, int64_t K, int32_t dim, void* base) {
+    Workspace s{};
+    const int64_t most = std::max<int64_t>((K + 63) / 64, 1), want = B ? (2048 + B - 1) / B : 1;
+    s.w.chunks = std::min(most, want);
+    s.w.links = std::max<int64_t>((K + s.w.chunks - 1) / s.w.chunks, 1);
+    s.w.chunks = std::max<int64_t>((K + s.w.links - 1) / s.w.links, 1);
+    s.w.waves = s.w.links <= 16 ? 1 : kWaves;
+    char* p = static_cast<char*>(base);
+    auto take = [&](size_t floats) {
+        void* const at = p;
+        p += aligned(floats * 4);
+        s.bytes += aligned(floats * 4);
+        return static_cast<float*>(at);
+    };
+    const int64_t units = B * s.w.chunks;
+    s.w.losses = take(std::min(units, kMostGroups));
+    if (s.w.chunks > 1) {
+        s.w.parts = take(units * dim);
+        s.w.sums = take(units * 2);
+    }
+    if (dim > kWideSingle) s.slopes = take(B * K);
+    return s;
+}
+
+template <typename T>
+struct Out {
+    float *loss, *margin;
+    T *danchor, *dpos, *dneg;
+};
+
+template <typename T, int VEC, int G, int NV>
+int64_t launch(const Pairs<T>& p, const Work& w, const Out<T>& o, hipStream_t stream) {
+    const int64_t per = kWaves / w.waves, groups = std::min((p.B * w.chunks + per - 1) / per, kMostGroups);
+    if (o.danchor) hipLaunchKernelGGL((k_pairs<T, VEC, G, NV, true>), dim3((unsigned)groups), dim3(256), 0, stream, p, w, o.margin, o.danchor, o.dpos, o.dneg);
+    else hipLaunchKernelGGL((k_pairs<T, VEC, G, NV, false>), dim3((unsigned)groups), dim3(256), 0, stream, p, w, o.margin, o.danchor, o.dpos, o.dneg);
+    return groups;
+}
+
+// Vectors of four channels where every row begins at a multiple of them, else one by one; as few lanes to a row as hold it.
+template <typename T>
+void run(const Pairs<T>& p, const Workspace& s, const Out<T>& o, hipStream_t stream) {
+    const Work& w = s.w;
+    auto fits = [](const void* at) { return (reinterpret_cast<uintptr_t>(at) & (4 * sizeof(T) - 1)) == 0; };
+    const bool four = p.dim % 4 == 0 && p.ld_anchor % 4 == 0 && p.ld_pos % 4 == 0 && fits(p.anchor) && fits(p.pos) && fits(p.neg) && fits(o.danchor) && fits(o.dpos) && fits(o.dneg);
+    int64_t groups = 0;
+    bool joined = w.chunks == 1;
+    if (p.B > 0) {
+        const int d = p.dim;
+        if (d > (four ? kWide : kWideSingle)) {
+            groups = std::min((p.B * w.chunks + kWaves - 1) / kWaves, kMostGroups);
+            hipLaunchKernelGGL((k_pairs_wide<T>), dim3((unsigned)groups), dim3(256), 0, stream, p, w, o.margin, s.slopes);
+            if (o.danchor)
+                hipLaunchKernelGGL((k_pairs_wide_grads<T>), dim3((unsigned)std::min<int64_t>(p.B * ((d + 255) / 256), kMostGroups)), dim3(256), 0, stream, p, s.slopes,
+                                   o.danchor, o.dpos, o.dneg);
+            joined = true;
+        } else if (four) {
+            groups = d <= 32 ? launch<T, 4, 8, 1>(p, w, o, stream) : d <= 64 ? launch<T, 4, 16, 1>(p, w, o, stream) : d <= 128 ? launch<T, 4, 32, 1>(p, w, o, stream)
+                     : d <= 256 ? launch<T, 4, 64, 1>(p, w, o, stream) : d <= 512 ? launch<T, 4, 64, 2>(p, w, o, stream)
+                     : d <= 1024 ? launch<T, 4, 64, 4>(p, w, o, stream) : launch<T, 4, 64, 8>(p, w, o, stream);
+        } else {
+            groups = d <= 64 ? launch<T, 1, 64, 1>(p, w, o, stream) : d <= 128 ? launch<T, 1, 64, 2>(p, w, o, stream)
+                     : d <= 256 ? launch<T, 1, 64, 4>(p, w, o, stream) : launch<T, 1, 64, 8>(p, w, o, stream);
+        }
+    }
+    T* const da = joined ? nullptr : o.danchor;
+    const dim3 grid = da ? dim3((p.dim + kColumns - 1) / kColumns, (unsigned)p.B) : dim3(1);
+    hipLaunchKernelGGL((k_pairs_join<T>), grid, dim3(1024), 0, stream, p, w, groups, o.loss, da, o.dpos);
+}
 
 }  // namespace
 
@@ -117,7 +429,7 @@ int tns_pair_loss_workspace(int64_t B, int64_t K, int32_t dim, size_t* bytes) {
     tns::clear_error();
     if (!bytes) return fail(TNS_EINVAL, "null output pointer");
     if (int e = check(B, K, dim)) return e;
-    *bytes = workspace_bytes_of(B, K, dim);
+    *bytes = carve(B, K, dim, nullptr).bytes;
     return TNS_OK;
 }
 
@@ -131,24 +443,20 @@ int tns_pair_loss(const tns_pairs* p, float* d_loss, float* d_margin, void* d_da
     if (p->ld_anchor < p->dim || p->ld_pos < p->dim) return fail(TNS_EINVAL, "rows of anchor or pos overlap");
     if (!(p->smoothing >= 0.0 && p->smoothing <= 1.0)) return fail(TNS_EINVAL, "smoothing must be in [0, 1]");
     if (!d_danchor != !d_dpos || (p->K > 0 && !d_danchor != !d_dneg)) return fail(TNS_EINVAL, "gradients come together");
-    const size_t need = workspace_bytes_of(p->B, p->K, p->dim);
+    const Workspace s = carve(p->B, p->K, p->dim, d_workspace);
+    const size_t need = s.bytes;
     if (need && !d_workspace) return fail(TNS_EINVAL, "null workspace");
     if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return fail(TNS_EINVAL, "workspace must be 256-byte aligned");
     if (workspace_bytes < need) return fail(TNS_ESIZE, "workspace smaller than tns_pair_loss_workspace()");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    float* const losses = static_cast<float*>(d_workspace);
-    auto launch = [&](auto value) {
+    auto go = [&](auto value) {
         using T = decltype(value);
-        const Pairs<T> t{p->B, p->K, static_cast<const T*>(p->d_anchor), static_cast<const T*>(p->d_pos), static_cast<const T*>(p->d_neg),
-                         p->ld_anchor, p->ld_pos, p->d_ref, p->d_weight, (float)p->beta, (float)p->smoothing, (float)p->scale, p->dim};
-        hipLaunchKernelGGL((k_pairs<T>), dim3((unsigned)p->B), dim3(64), 0, stream, t, losses, d_margin, static_cast<T*>(d_danchor),
-                           static_cast<T*>(d_dpos), static_cast<T*>(d_dneg));
+        run(Pairs<T>{p->B, p->K, static_cast<const T*>(p->d_anchor), static_cast<const T*>(p->d_pos), static_cast<const T*>(p->d_neg),
+                     p->ld_anchor, p->ld_pos, p->d_ref, p->d_weight, (float)p->beta, (float)p->smoothing, (float)p->scale, p->dim},
+            s, Out<T>{d_loss, d_margin, static_cast<T*>(d_danchor), static_cast<T*>(d_dpos), static_cast<T*>(d_dneg)}, stream);
     };
-    if (p->B > 0) {
-        if (p->dtype == TNS_F32) launch(float{});
-        else launch(bf16{});
-    }
-    hipLaunchKernelGGL(k_pairs_sum, dim3(1), dim3(64), 0, stream, losses, p->B, d_loss);
+    if (p->dtype == TNS_F32) go(float{});
+    else go(bf16{});
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? (int)TNS_OK : fail_hip(e, "tns_pair_loss");
 }
