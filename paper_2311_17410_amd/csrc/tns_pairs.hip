@@ -30,19 +30,41 @@ constexpr int kWaves = 4;
 constexpr int64_t kMostGroups = 1 << 16;   // workgroups of a launch; they go round the events
 constexpr int kWide = 2048, kWideSingle = 512;      // channels that a wave holds at most, in vectors of four and one by one
 
+// Sums over lanes as vector instructions (a shuffle through the LDS unit is some sixty cycles, and every row of a product waits for one
+// sum).  Lanes that have the same sum read each other's in mirrored order, so all of them add the same two values.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float add_row16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add_row32(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 // Sum over the G lanes that share a row.
 template <int G>
 __device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-    for (int by = G / 2; by; by >>= 1) v += __shfl_xor(v, by);
+    static_assert(G >= 8);
+    v += moved<0xB1>(v);               // quad_perm 1, 0, 3, 2
+    v += moved<0x4E>(v);               // quad_perm 2, 3, 0, 1
+    v += moved<0x141>(v);              // the other four of eight
+    if (G >= 16) v += moved<0x140>(v); // the other eight of sixteen
+    if (G >= 32) v = add_row16(v);
+    if (G >= 64) v = add_row32(v);
     return v;
 }
 // Sum over the rows of a wave, of values that are the same for the lanes of a row.
 template <int G>
 __device__ __forceinline__ float sum_of_rows(float v) {
-#pragma unroll
-    for (int by = 32; by >= G; by >>= 1) v += __shfl_xor(v, by);
+    if (G <= 8) v += __shfl_xor(v, 8);
+    if (G <= 16) v = add_row16(v);
+    if (G <= 32) v = add_row32(v);
     return v;
+}
+// Lane r's of every four lanes.
+__device__ __forceinline__ float of_quad(float v, int r) {
+    return r == 0 ? moved<0x00>(v) : r == 1 ? moved<0x55>(v) : r == 2 ? moved<0xAA>(v) : moved<0xFF>(v);
 }
 
 // Loss of a margin and its slope, both times scale and weight.
@@ -58,10 +80,11 @@ template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Vec {
     T v[VEC];
 };
+// (`p` is the same for the wave, `bytes` the lane's part of the address: 32 bits.)
 template <typename T, int VEC>
-__device__ __forceinline__ void load(const T* p, bool there, float (&v)[VEC]) {
+__device__ __forceinline__ void load(const T* p, uint32_t bytes, bool there, float (&v)[VEC]) {
     if (there) {
-        const Vec<T, VEC> raw = *reinterpret_cast<const Vec<T, VEC>*>(p);
+        const Vec<T, VEC> raw = *reinterpret_cast<const Vec<T, VEC>*>(reinterpret_cast<const char*>(p) + bytes);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) v[i] = as_float(raw.v[i]);
     } else {
@@ -70,105 +93,142 @@ __device__ __forceinline__ void load(const T* p, bool there, float (&v)[VEC]) {
     }
 }
 template <typename T, int VEC>
-__device__ __forceinline__ void store(T* p, const float (&v)[VEC]) {
+__device__ __forceinline__ void store(T* p, uint32_t bytes, const float (&v)[VEC]) {
     Vec<T, VEC> raw;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) raw.v[i] = as_value<T>(v[i]);
-    *reinterpret_cast<Vec<T, VEC>*>(p) = raw;
+    *reinterpret_cast<Vec<T, VEC>*>(reinterpret_cast<char*>(p) + bytes) = raw;
 }
 
 struct Work {                         // how the links of an event are shared out
     int64_t chunks, links;            // parts of an event that workgroups take, links of each
-    int waves;                        // of a workgroup on one part: 1 (four events a workgroup) or 4
+    int waves;                        // of a workgroup on one part: 1 or 4 (and so four parts a workgroup, or one)
     float *losses, *parts, *sums;     // per workgroup; [B * chunks, dim] and [B * chunks, 2] where there are parts to join
 };
 
-// The loss and all gradients in one pass over the sampled links: G lanes hold a row, NV vectors of VEC channels each, and R rows are on
-// their way at a time; the anchor and the sum for its gradient stay in registers.  Bound by memory: (2 + K) rows read and written for
-// every event.
+// The loss and all gradients in one pass over the sampled links: G lanes hold a row, NV vectors of VEC channels each, and the next R rows
+// are on their way while R are computed; the anchor and the sum for its gradient stay in registers.  The margins' losses and slopes, a
+// hundred instructions each, are computed for R rows at once, by a lane of every four each.  Bound by memory: (2 + K) rows read and written
+// for every event.
 template <typename T, int VEC, int G, int NV, bool GRADS>
 __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, float* margin, T* danchor, T* dpos, T* dneg) {
     constexpr int kRows = 64 / G, R = NV == 1 ? 4 : NV == 2 ? 2 : 1;
-    __shared__ float s_acc[kWaves - 1][GRADS ? G * VEC * NV : 1], s_sum[kWaves][3];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / G;
-    const int part_of = w.waves == 1 ? 0 : wave;             // which of the part's waves this is
+    __shared__ float s_acc[kWaves][GRADS ? G * VEC * NV : 1], s_sum[kWaves][3];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), row = lane / G;
+    const int part_of = wave % w.waves;                      // which of the part's waves this is
     int at[NV];
     bool there[NV];
+    uint32_t col[NV], mine_at[NV];     // bytes of the lane's vectors from a row's begin, and from the begin of the rows side by side
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         at[j] = (j * G + lane % G) * VEC;
         there[j] = at[j] < p.dim;
+        col[j] = (uint32_t)at[j] * sizeof(T);
+        mine_at[j] = ((uint32_t)row * (uint32_t)p.dim + (uint32_t)at[j]) * sizeof(T);
     }
     float total = 0.0f;
     const int64_t units = p.B * w.chunks, per = kWaves / w.waves;
     for (int64_t first = (int64_t)blockIdx.x * per; first < units; first += (int64_t)gridDim.x * per) {
-        const int64_t unit = first + (w.waves == 1 ? wave : 0);
+        const int64_t unit = first + wave / w.waves;
         const bool real = unit < units;
         const int64_t b = real ? unit / w.chunks : 0, k_begin = real ? unit % w.chunks * w.links : 0, k_end = real ? min(k_begin + w.links, p.K) : 0;
-        float a[NV][VEC], q[NV][VEC], acc[NV][VEC], dot = 0.0f;
+        float a[NV][VEC], acc[NV][VEC], dot = 0.0f;
+        // Links of an iteration: row r of this lane's is k0 + r * kRows + row; the lane sees to the weight and the loss of one of them.
+        const int r_mine = lane % 4 % R;
+        const int64_t by = (int64_t)w.waves * kRows * R, base = b * p.K;
+        auto weight_of = [&](int64_t k0) {                   // (read by every lane: what lanes read of each other is never behind a branch)
+            const int64_t k = k0 + r_mine * kRows + row;
+            const float v = p.weight && k_begin < k_end ? p.weight[base + min(k, k_end - 1)] : 1.0f;
+            return k < k_end ? v : 0.0f;
+        };
+        auto read = [&](int64_t k0, float weight, float (&n)[R][NV][VEC]) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bool is = of_quad(weight, r) != 0.0f;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) load<T, VEC>(p.neg + (base + k0 + r * kRows) * p.dim, mine_at[j], there[j] && is, n[r][j]);
+            }
+        };
+        const int64_t k_first = k_begin + part_of * kRows * R;
+        float weight = weight_of(k_first), weight_next = weight_of(k_first + by);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            load<T, VEC>(p.anchor + b * p.ld_anchor + at[j], there[j], a[j]);
-            load<T, VEC>(p.pos + b * p.ld_pos + at[j], there[j], q[j]);
+            float q[VEC];
+            load<T, VEC>(p.anchor + b * p.ld_anchor, col[j], there[j], a[j]);
+            load<T, VEC>(p.pos + b * p.ld_pos, col[j], there[j], q);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                dot += a[j][i] * q[j][i];
+                dot += a[j][i] * q[i];
                 acc[j][i] = 0.0f;
             }
         }
+        float n[R][NV][VEC];
+        read(k_first, weight, n);
         const float plus = row_sum<G>(dot);
         float loss_sum = 0.0f, slope_sum = 0.0f, any = 0.0f;
-        for (int64_t k0 = k_begin + part_of * kRows * R; k0 < k_end; k0 += (int64_t)w.waves * kRows * R) {
-            float n[R][NV][VEC], weight[R], ref[R];
-            int64_t i[R];
+        for (int64_t k0 = k_first; k0 < k_end; k0 += by) {
+            const int64_t k_mine = k0 + r_mine * kRows + row;
+            const bool mine = k_mine < k_end;
+            const float ref = p.ref ? p.ref[base + min(k_mine, k_end - 1)] : 0.0f;
+            const float weight_after = weight_of(k0 + 2 * by);
+            float next[R][NV][VEC];
+            read(k0 + by, weight_next, next);
+            float minus = 0.0f;                              // of the lane's row
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const int64_t k = k0 + r * kRows + row;
-                const bool is = k < k_end;
-                i[r] = b * p.K + (is ? k : k_begin);
-                weight[r] = is ? (p.weight ? p.weight[i[r]] : 1.0f) : 0.0f;
-                ref[r] = is && p.ref ? p.ref[i[r]] : 0.0f;
-                if (!is) i[r] = -1;
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int j = 0; j < NV; ++j) load<T, VEC>(p.neg + i[r] * p.dim + at[j], there[j] && weight[r] != 0.0f, n[r][j]);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float minus = 0.0f;
+                float sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
-                    for (int c = 0; c < VEC; ++c) minus += a[j][c] * n[r][j][c];
-                minus = row_sum<G>(minus);
-                float m = 0.0f, loss = 0.0f, slope = 0.0f;
-                if (weight[r] != 0.0f) {
-                    m = p.beta * (plus - minus - ref[r]);
-                    loss_of(m, weight[r], p.scale, p.smoothing, loss, slope);
-                    slope *= p.beta;
-                    any = 1.0f;
-                }
-                loss_sum += loss;
-                slope_sum += slope;
-                if (margin && i[r] >= 0 && lane % G == 0) margin[i[r]] = m;
-                if (GRADS) {
+                    for (int c = 0; c < VEC; ++c) sum += a[j][c] * n[r][j][c];
+                sum = row_sum<G>(sum);
+                if (r == r_mine) minus = sum;
+            }
+            float m = 0.0f, loss = 0.0f, slope = 0.0f;
+            if (weight != 0.0f) {
+                m = p.beta * (plus - minus - ref);
+                loss_of(m, weight, p.scale, p.smoothing, loss, slope);
+                slope *= p.beta;
+                any = 1.0f;
+            }
+            loss_sum += loss;
+            slope_sum += slope;
+            if (margin && mine && lane % G < R) margin[base + k_mine] = m;
+            if (GRADS) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float s = of_quad(slope, r);
+                    const bool is = of_quad(weight, r) != 0.0f;
+                    const bool real_row = row < k_end - k0 - r * kRows;
 #pragma unroll
                     for (int j = 0; j < NV; ++j) {
                         float out[VEC];
 #pragma unroll
                         for (int c = 0; c < VEC; ++c) {
-                            acc[j][c] -= slope * n[r][j][c];
-                            out[c] = weight[r] != 0.0f ? -slope * a[j][c] : 0.0f;
+                            acc[j][c] -= s * n[r][j][c];
+                            out[c] = is ? -s * a[j][c] : 0.0f;
                         }
-                        if (i[r] >= 0 && there[j]) store<T, VEC>(dneg + i[r] * p.dim + at[j], out);
+                        if (real_row && there[j]) store<T, VEC>(dneg + (base + k0 + r * kRows) * p.dim, mine_at[j], out);
                     }
                 }
             }
+            weight = weight_next;
+            weight_next = weight_after;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) n[r][j][c] = next[r][j][c];
         }
-        loss_sum = sum_of_rows<G>(loss_sum);
-        slope_sum = sum_of_rows<G>(slope_sum);
-        any = sum_of_rows<G>(any);
+        auto sum_up = [&](float v) {                         // over the lanes' rows, and the rows side by side
+            if (R >= 2) v += moved<0xB1>(v);
+            if (R >= 4) v += moved<0x4E>(v);
+            return sum_of_rows<G>(v);
+        };
+        loss_sum = sum_up(loss_sum);
+        slope_sum = sum_up(slope_sum);
+        any = sum_up(any);
         if (real) total += loss_sum;
         if (GRADS) {
 #pragma unroll
@@ -177,23 +237,23 @@ __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, f
                 for (int c = 0; c < VEC; ++c) acc[j][c] = sum_of_rows<G>(acc[j][c]);
             if (w.waves > 1) {                               // the waves' shares, in their order
                 __syncthreads();                             // (the part before has been read)
-                if (wave) {
+                if (part_of) {
                     if (row == 0)
 #pragma unroll
                         for (int j = 0; j < NV; ++j)
 #pragma unroll
-                            for (int c = 0; c < VEC; ++c) s_acc[wave - 1][at[j] + c] = acc[j][c];
+                            for (int c = 0; c < VEC; ++c) s_acc[wave][at[j] + c] = acc[j][c];
                     if (lane == 0) { s_sum[wave][0] = slope_sum; s_sum[wave][1] = any; }
                 }
                 __syncthreads();
-                if (wave == 0)
-                    for (int k = 1; k < kWaves; ++k) {
+                if (part_of == 0)
+                    for (int k = wave + 1; k < wave + w.waves; ++k) {
                         slope_sum += s_sum[k][0];
                         any += s_sum[k][1];
 #pragma unroll
                         for (int j = 0; j < NV; ++j)
 #pragma unroll
-                            for (int c = 0; c < VEC; ++c) acc[j][c] += s_acc[k - 1][at[j] + c];
+                            for (int c = 0; c < VEC; ++c) acc[j][c] += s_acc[k][at[j] + c];
                     }
             }
             if (real && part_of == 0 && row == 0) {
@@ -205,14 +265,15 @@ __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, f
 #pragma unroll
                         for (int c = 0; c < VEC; ++c) w.parts[unit * p.dim + at[j] + c] = acc[j][c];
                     } else {
-                        float da[VEC], dp[VEC];
+                        float q[VEC], da[VEC], dp[VEC];
+                        load<T, VEC>(p.pos + b * p.ld_pos, col[j], true, q);
 #pragma unroll
                         for (int c = 0; c < VEC; ++c) {
-                            da[c] = any != 0.0f ? slope_sum * q[j][c] + acc[j][c] : 0.0f;
+                            da[c] = any != 0.0f ? slope_sum * q[c] + acc[j][c] : 0.0f;
                             dp[c] = any != 0.0f ? slope_sum * a[j][c] : 0.0f;
                         }
-                        store<T, VEC>(danchor + b * p.dim + at[j], da);
-                        store<T, VEC>(dpos + b * p.dim + at[j], dp);
+                        store<T, VEC>(danchor + b * p.dim, col[j], da);
+                        store<T, VEC>(dpos + b * p.dim, col[j], dp);
                     }
                 }
             }
@@ -346,7 +407,8 @@ int check(int64_t B, int64_t K, int32_t dim) {
 size_t aligned(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 // Few events are cut into parts, so that there are some 2048 workgroups of four waves (two for every wave's place of the chip); a part
-// has 64 links at least.  An event of few links is one wave's.
+// has 64 links at least.  A part of few links is one wave's where there are enough of them (4000 events of 50 links, 172 channels in 16
+// bits: 54 us, four waves a part 66; 200 events of 10000, 128 channels in 32 bits: 483 us, four waves 426).
 struct Workspace {
     Work w;
     float* slopes;                    // [B, K], of rows that may be too wide for a wave
@@ -358,7 +420,7 @@ Workspace carve(int64_t B, int64_t K, int32_t dim, void* base) {
     s.w.chunks = std::min(most, want);
     s.w.links = std::max<int64_t>((K + s.w.chunks - 1) / s.w.chunks, 1);
     s.w.chunks = std::max<int64_t>((K + s.w.links - 1) / s.w.links, 1);
-    s.w.waves = s.w.links <= 16 ? 1 : kWaves;
+    s.w.waves = s.w.links <= (B * s.w.chunks >= 2048 ? 64 : 16) ? 1 : kWaves;
     char* p = static_cast<char*>(base);
     auto take = [&](size_t floats) {
         void* const at = p;

@@ -6,6 +6,7 @@ enqueue on its current stream.  Strides other than those of the last dimension a
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 from .binding import TnsError, _check, lib as _lib  # noqa: F401
 
@@ -117,9 +118,9 @@ def tns_adamw_destroy(opt) -> None:
 
 def _dtype_of(t):
     import torch
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return TNS_F32
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return TNS_BF16
     raise ValueError(f"float32 or bfloat16 is wanted, not {t.dtype}")
 
@@ -128,9 +129,9 @@ def _want(name, t, shape, dtype, device, dense=True):
     """The address of a tensor of that shape and type, 0 for None; rows of a matrix may lie apart where it need not be dense."""
     if t is None:
         return 0
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
-        raise ValueError(f"{name}: {dtype} of shape {shape} on {device} is wanted, not {t.dtype} of {tuple(t.shape)} on {t.device}")
-    if not (t.is_contiguous() if dense else t.stride(-1) == 1 or t.shape[-1] <= 1 or t.numel() == 0):
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        raise ValueError(f"{name}: {dtype} of shape {tuple(shape)} on {device} is wanted, not {t.dtype} of {tuple(t.shape)} on {t.device}")
+    if not t.is_contiguous() and (dense or not (t.stride(-1) == 1 or t.shape[-1] <= 1)):
         raise ValueError(f"{name}: " + ("a contiguous tensor is wanted" if dense else "the channels of a row have to lie side by side"))
     return t.data_ptr()
 
@@ -139,22 +140,45 @@ def _ld(t, dim):
     return dim if t is None or t.shape[0] <= 1 else t.stride(0)
 
 
+class _Here:
+    """Leaves the current device as it is."""
+
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *_):
+        pass
+
+
+_HERE = _Here()
+
+
 def _on(t):
-    """Device and current stream of a tensor's GPU."""
+    """A context in which a tensor's GPU is the current one, and its current stream."""
     import torch
     if not t.is_cuda:
         raise ValueError("tensors on the GPU are wanted")
-    return torch.cuda.device(t.device), torch.cuda.current_stream(t.device).cuda_stream
+    index = t.device.index
+    return _HERE if torch.cuda.current_device() == index else torch.cuda.device(index), torch.cuda.current_stream(index).cuda_stream
+
+
+@functools.lru_cache(maxsize=1024)
+def _recur_bytes(S, rows, dim, dtype):
+    return tns_recur_workspace(tns_recur(S, rows, dim, dtype))
+
+
+_pair_bytes = functools.lru_cache(maxsize=1024)(tns_pair_loss_workspace)
 
 
 def _lists(rowptr, u, x, ts, decay, h0, t0, newest_first):
     import torch
     if u.dim() != 2 or rowptr.dim() != 1 or rowptr.shape[0] < 1:
         raise ValueError("u has the shape [rows, dim], rowptr [lists + 1]")
-    (rows, dim), S, dev, f32 = u.shape, rowptr.shape[0] - 1, u.device, torch.float32
+    shape, S, dev, f32 = u.shape, rowptr.shape[0] - 1, u.device, torch.float32
+    rows, dim = shape
     dtype = _dtype_of(u)
     return tns_recur(S, rows, dim, dtype, TNS_NEWEST_FIRST if newest_first else 0, 0, _want("rowptr", rowptr, (S + 1,), torch.int64, dev),
-                     _want("u", u, (rows, dim), u.dtype, dev, False), _want("x", x, (rows, dim), u.dtype, dev, False), _ld(u, dim), _ld(x, dim),
+                     _want("u", u, shape, u.dtype, dev, False), _want("x", x, shape, u.dtype, dev, False), _ld(u, dim), _ld(x, dim),
                      _want("ts", ts, (rows,), f32, dev), _want("decay", decay, (dim,), f32, dev), _want("h0", h0, (S, dim), f32, dev),
                      _want("t0", t0, (S,), f32, dev))
 
@@ -165,10 +189,10 @@ def recur_run(rowptr, u, x, ts=None, decay=None, h0=None, t0=None, newest_first=
     import torch
     on, stream = _on(u)
     r = _lists(rowptr, u, x, ts, decay, h0, t0, newest_first)
-    run, _, saved = tns_recur_workspace(r)
-    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=u.device)      # noqa: E731
-    out = dict(h=new((r.rows, r.dim), u.dtype) if states else None, last=new((r.S, r.dim), torch.float32), saved=new(saved, torch.uint8) if save else None)
-    ws = new(run, torch.uint8)
+    run, _, saved = _recur_bytes(r.S, r.rows, r.dim, r.dtype)
+    out = dict(h=u.new_empty((r.rows, r.dim)) if states else None, last=u.new_empty((r.S, r.dim), dtype=torch.float32),
+               saved=u.new_empty(saved, dtype=torch.uint8) if save else None)
+    ws = u.new_empty(run, dtype=torch.uint8)
     with on:
         tns_recur_run(r, out["h"].data_ptr() if states else 0, r.dim, out["last"].data_ptr(), out["saved"].data_ptr() if save else 0, ws.data_ptr(), run, stream)
     return out
@@ -180,16 +204,15 @@ def recur_grad(rowptr, u, x, saved, ts=None, decay=None, h0=None, t0=None, newes
     import torch
     on, stream = _on(u)
     r = _lists(rowptr, u, x, ts, decay, h0, t0, newest_first)
-    _, grad, size = tns_recur_workspace(r)
+    _, grad, size = _recur_bytes(r.S, r.rows, r.dim, r.dtype)
     if saved is None:
         raise ValueError("saved: recur_run(save=True) returns it")
-    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=u.device)      # noqa: E731
     p_saved = _want("saved", saved, (size,), torch.uint8, u.device)
-    p_dh = _want("dh", dh, (r.rows, r.dim), u.dtype, u.device, False)
+    p_dh = _want("dh", dh, u.shape, u.dtype, u.device, False)
     p_dlast = _want("dlast", dlast, (r.S, r.dim), torch.float32, u.device)
-    out = dict(du=new((r.rows, r.dim), u.dtype), dx=new((r.rows, r.dim), u.dtype), ddecay=new((r.dim,), torch.float32) if decay is not None else None,
-               dh0=new((r.S, r.dim), torch.float32) if h0 is not None else None)
-    ws = new(grad, torch.uint8)
+    out = dict(du=u.new_empty((r.rows, r.dim)), dx=u.new_empty((r.rows, r.dim)), ddecay=u.new_empty(r.dim, dtype=torch.float32) if decay is not None else None,
+               dh0=u.new_empty((r.S, r.dim), dtype=torch.float32) if h0 is not None else None)
+    ws = u.new_empty(grad, dtype=torch.uint8)
     p = lambda t: 0 if t is None else t.data_ptr()      # noqa: E731
     with on:
         tns_recur_grad(r, p_saved, p_dh, _ld(dh, r.dim), p_dlast, p(out["du"]), r.dim, p(out["dx"]), r.dim, p(out["ddecay"]), p(out["dh0"]), ws.data_ptr(),
@@ -204,11 +227,12 @@ def recur_step(ids, u, x, state, ts=None, decay=None, state_ts=None):
     on, stream = _on(u)
     if u.dim() != 2 or state.dim() != 2:
         raise ValueError("u has the shape [events, dim], state [nodes, dim]")
-    (B, dim), n, dev, f32 = u.shape, state.shape[0], u.device, torch.float32
+    shape, n, dev, f32 = u.shape, state.shape[0], u.device, torch.float32
+    B, dim = shape
     dtype = _dtype_of(u)
-    out = torch.empty((B, dim), dtype=u.dtype, device=dev)
-    args = (_want("ids", ids, (B,), torch.int32, dev), _want("u", u, (B, dim), u.dtype, dev, False), _ld(u, dim),
-            _want("x", x, (B, dim), u.dtype, dev, False), _ld(x, dim), _want("ts", ts, (B,), f32, dev), _want("decay", decay, (dim,), f32, dev),
+    out = u.new_empty((B, dim))
+    args = (_want("ids", ids, (B,), torch.int32, dev), _want("u", u, shape, u.dtype, dev, False), _ld(u, dim),
+            _want("x", x, shape, u.dtype, dev, False), _ld(x, dim), _want("ts", ts, (B,), f32, dev), _want("decay", decay, (dim,), f32, dev),
             _want("state", state, (n, dim), f32, dev), _want("state_ts", state_ts, (n,), f32, dev))
     with on:
         tns_recur_step(B, n, dim, dtype, *args, out.data_ptr(), dim, stream)
@@ -222,20 +246,17 @@ def pair_loss(anchor, pos, neg, ref=None, weight=None, beta=1.0, smoothing=0.0, 
     on, stream = _on(anchor)
     if neg.dim() != 3:
         raise ValueError("neg has the shape [events, links, dim]")
-    (B, K, dim), dev, dt = neg.shape, anchor.device, anchor.dtype
-    dtype = _dtype_of(anchor)
-    p = tns_pairs(B, K, dim, dtype, _want("anchor", anchor, (B, dim), dt, dev, False), _want("pos", pos, (B, dim), dt, dev, False),
-                  _want("neg", neg, (B, K, dim), dt, dev), _ld(anchor, dim), _ld(pos, dim), _want("ref", ref, (B, K), torch.float32, dev),
-                  _want("weight", weight, (B, K), torch.float32, dev), beta, smoothing, scale)
-    need = tns_pair_loss_workspace(B, K, dim)
-    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=dev)      # noqa: E731
-    out = dict(loss=new((), torch.float32), margin=new((B, K), torch.float32))
-    out.update({n: new(t.shape, dt) if grads else None for n, t in (("danchor", anchor), ("dpos", pos), ("dneg", neg))})
-    ws = new(need, torch.uint8)
-    g = [0 if out[n] is None else out[n].data_ptr() for n in ("danchor", "dpos", "dneg")]
+    (B, K, dim), dev, dt, f32 = neg.shape, anchor.device, anchor.dtype, torch.float32
+    p = tns_pairs(B, K, dim, _dtype_of(anchor), _want("anchor", anchor, (B, dim), dt, dev, False), _want("pos", pos, (B, dim), dt, dev, False),
+                  _want("neg", neg, neg.shape, dt, dev), _ld(anchor, dim), _ld(pos, dim), _want("ref", ref, (B, K), f32, dev),
+                  _want("weight", weight, (B, K), f32, dev), beta, smoothing, scale)
+    need = _pair_bytes(B, K, dim)
+    loss, margin, ws = anchor.new_empty((), dtype=f32), anchor.new_empty((B, K), dtype=f32), anchor.new_empty(need, dtype=torch.uint8)
+    da, dp, dn = (anchor.new_empty((B, dim)), anchor.new_empty((B, dim)), anchor.new_empty((B, K, dim))) if grads else (None,) * 3
+    g = (da.data_ptr(), dp.data_ptr(), dn.data_ptr()) if grads else (0, 0, 0)
     with on:
-        tns_pair_loss(p, out["loss"].data_ptr(), out["margin"].data_ptr(), *g, ws.data_ptr(), need, stream)
-    return out
+        tns_pair_loss(p, loss.data_ptr(), margin.data_ptr(), *g, ws.data_ptr(), need, stream)
+    return dict(loss=loss, margin=margin, danchor=da, dpos=dp, dneg=dn)
 
 
 class AdamW:
