@@ -820,25 +820,43 @@ __global__ void __launch_bounds__(1024) k_recur_sums(const float* sums, int64_t 
     if (part == 0 && c < dim) out[c] = s_sum[0][ch];
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_recur_step(int64_t num_ids, int dim, const int32_t* ids, const T* u, int64_t ld_u, const T* x, int64_t ld_x,
-                                                    const float* ts, const float* decay, float* state, float* state_ts, T* out, int64_t ld_out) {
-    const int64_t b = blockIdx.x;
-    const int64_t id = ids[b];
-    const bool held = id >= 0 && id < num_ids;
-    const float gap = held && ts ? gap_of(ts[b], state_ts[id]) : 0.0f;
-    __syncthreads();                  // every wave has read the time before one writes it
-    if (held && ts && threadIdx.x == 0) state_ts[id] = ts[b];
-    for (int c = threadIdx.x; c < dim; c += 256) {
-        float h = 0.0f;
-        if (held) {
-            float z, f;
-            gate_of(as_float(u[b * ld_u + c]), z, f);
-            if (ts) f *= __builtin_amdgcn_exp2f(-kLog2e * decay[c] * gap);
-            h = f * state[id * dim + c] + z * as_float(x[b * ld_x + c]);
-            state[id * dim + c] = h;
+// ---- one event per node ----------------------------------------------------------------------------------
+
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Vec {
+    T v[N];
+};
+// G lanes to an event, VEC channels a lane at a time.  Bound by memory; the states lie anywhere, so a row of them is read in as few
+// requests as there are.
+template <typename T, int VEC, int G>
+__global__ void __launch_bounds__(256) k_recur_step(int64_t B, int64_t num_ids, int dim, const int32_t* __restrict__ ids, const T* __restrict__ u, int64_t ld_u,
+                                                    const T* __restrict__ x, int64_t ld_x, const float* __restrict__ ts, const float* __restrict__ decay, float* state,
+                                                    float* state_ts, T* __restrict__ out, int64_t ld_out) {
+    for (int64_t b = ((int64_t)blockIdx.x * 256 + threadIdx.x) / G; b < B; b += (int64_t)gridDim.x * (256 / G)) {
+        const int64_t id = ids[b];
+        const bool held = id >= 0 && id < num_ids;
+        float gap = 0.0f;
+        if (held && ts) {
+            gap = gap_of(ts[b], state_ts[id]);
+            if (threadIdx.x % G == 0) state_ts[id] = ts[b];      // (the lanes of an event are in one wave: all have read it)
         }
-        if (out) out[b * ld_out + c] = as_value<T>(h);
+        for (int c = threadIdx.x % G * VEC; c < dim; c += G * VEC) {
+            const Vec<T, VEC> vu = *reinterpret_cast<const Vec<T, VEC>*>(u + b * ld_u + c), vx = *reinterpret_cast<const Vec<T, VEC>*>(x + b * ld_x + c);
+            Vec<float, VEC> h = {}, rate = {};
+            if (held) h = *reinterpret_cast<const Vec<float, VEC>*>(state + id * dim + c);
+            if (ts) rate = *reinterpret_cast<const Vec<float, VEC>*>(decay + c);
+            Vec<T, VEC> to;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                float z, f;
+                gate_of(as_float(vu.v[i]), z, f);
+                if (ts) f *= __builtin_amdgcn_exp2f(-kLog2e * rate.v[i] * gap);
+                h.v[i] = held ? f * h.v[i] + z * as_float(vx.v[i]) : 0.0f;
+                to.v[i] = as_value<T>(h.v[i]);
+            }
+            if (held) *reinterpret_cast<Vec<float, VEC>*>(state + id * dim + c) = h;
+            if (out) *reinterpret_cast<Vec<T, VEC>*>(out + b * ld_out + c) = to;
+        }
     }
 }
 
@@ -1047,13 +1065,28 @@ int tns_recur_step(int64_t B, int64_t num_ids, int32_t dim, int32_t dtype, const
     if (!d_ts != !d_decay || (num_ids > 0 && !d_ts != !d_state_ts)) return fail(TNS_EINVAL, "ts, decay and state_ts come together");
     if (!d_ids || !d_u || !d_x || (num_ids > 0 && !d_state)) return fail(TNS_EINVAL, "null ids, u, x or state");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    auto launch = [&](auto value) {
+    auto launch = [&](auto value, auto vec, auto lanes) {
         using T = decltype(value);
-        hipLaunchKernelGGL((k_recur_step<T>), dim3((unsigned)B), dim3(256), 0, stream, num_ids, dim, d_ids, static_cast<const T*>(d_u), ld_u,
+        const int64_t groups = std::min<int64_t>((B + 256 / lanes() - 1) / (256 / lanes()), 1 << 20);
+        hipLaunchKernelGGL((k_recur_step<T, vec(), lanes()>), dim3((unsigned)groups), dim3(256), 0, stream, B, num_ids, dim, d_ids, static_cast<const T*>(d_u), ld_u,
                            static_cast<const T*>(d_x), ld_x, d_ts, d_decay, d_state, d_state_ts, static_cast<T*>(d_out), ld_out);
     };
-    if (dtype == TNS_F32) launch(float{});
-    else launch(bf16{});
+    // Four channels at a time where all rows allow it, and as few lanes to an event as hold it at once.
+    auto choose_step = [&](auto value) {
+        using T = decltype(value);
+        auto fits = [](const void* p, size_t to) { return !misaligned(p, to); };
+        const bool four = dim % 4 == 0 && ld_u % 4 == 0 && ld_x % 4 == 0 && (!d_out || ld_out % 4 == 0) && fits(d_u, 4 * sizeof(T)) && fits(d_x, 4 * sizeof(T)) &&
+                          fits(d_out, 4 * sizeof(T)) && fits(d_state, 16) && fits(d_decay, 16);
+        using One = std::integral_constant<int, 1>;
+        using Four = std::integral_constant<int, 4>;
+        if (!four) launch(value, One{}, std::integral_constant<int, 64>{});
+        else if (dim <= 32) launch(value, Four{}, std::integral_constant<int, 8>{});
+        else if (dim <= 64) launch(value, Four{}, std::integral_constant<int, 16>{});
+        else if (dim <= 128) launch(value, Four{}, std::integral_constant<int, 32>{});
+        else launch(value, Four{}, std::integral_constant<int, 64>{});
+    };
+    if (dtype == TNS_F32) choose_step(float{});
+    else choose_step(bf16{});
     return launched("tns_recur_step");
 }
 
