@@ -610,10 +610,10 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
         return;
     }
     const Share share(blockIdx.x, blocks);
-    const int64_t tile = share.q * kWaves + wave;
+    const int64_t tile = ((t.tiles + kWaves - 1) / kWaves - 1 - share.q) * kWaves + wave;
     const int c = channel_of<V>(l.dim, share.block);
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
-    if (begin >= end) return;
+    if (tile < 0 || begin >= end) return;
     Pack<T, V> u[kSaved], x[kSaved];
     const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total);
     const Along rows_h(l, h_out, ld_h, total);
@@ -685,11 +685,11 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
         return;
     }
     const Share share(blockIdx.x, blocks);
-    const int64_t tile = share.q * kWaves + wave;
+    const int64_t tile = ((t.tiles + kWaves - 1) / kWaves - 1 - share.q) * kWaves + wave;
     const int c = channel_of<V>(l.dim, share.block);
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
     float sum[V] = {};
-    if (begin < end) {
+    if (tile >= 0 && begin < end) {
         const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved, last_batch = begin + (end - 1 - begin) / kBatch * kBatch;
         Pack<T, V> u[kSaved], x[kSaved], d[kSaved] = {};      // (d stays zero without dh)
         float enter[V];                                     // state before the group
