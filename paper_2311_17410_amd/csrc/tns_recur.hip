@@ -90,16 +90,21 @@ struct Lists {
 // (What a ballot votes on is computed without branches here and below: behind a load that some lanes skipped, the compiler folded the
 // skipping lanes' vote away and the two sides saw different results.)
 template <typename T>
-__device__ int find_list(const Lists<T>& l, int64_t total, int64_t p) {
+__device__ int find_list(const Lists<T>& l, int64_t total, int64_t p, int64_t* begin = nullptr) {
     const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = l.S;
+    int64_t lo = 0, hi = l.S, first = 0;
     while (hi - lo > 1) {
         const int64_t by = (hi - lo + kWave - 1) / kWave, j = lo + (lane + 1) * by;
         const int64_t at = l.begin_of(min(j, hi), total);
-        const int64_t c = __popcll(__ballot((j < hi) & (at <= p)));
+        const int c = __popcll(__ballot((j < hi) & (at <= p)));
+        if (c) {
+            const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, c - 1), high = (uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)at >> 32), c - 1);
+            first = (int64_t)((uint64_t)high << 32 | low);
+        }
         lo += c * by;
         hi = min(lo + by, hi);
     }
+    if (begin) *begin = first;                // of the list (the walk's first one begins at 0)
     return uniform((int)lo);
 }
 
@@ -348,17 +353,18 @@ struct Share {
 __host__ __device__ constexpr int64_t workgroups_of(int64_t groups, int blocks) { return (groups + kXcds - 1) / kXcds * kXcds * blocks; }
 
 // ---- carries -------------------------------------------------------------------------------------------
-// The walk is cut into tiles, sixteen tiles to a span.  What enters a tile is the state before its first event, or (backward) what the
+// The walk is cut into tiles, eight tiles to a span.  What enters a tile is the state before its first event, or (backward) what the
 // events after its last one send back.  A tile whose part of the crossing list begins (ends) inside it knows what it hands on, B (closed);
 // one that lies inside a list altogether hands on A * what enters + B (open).  A workgroup of a wave for every tile of a span finds both
 // and puts them together: for every tile what its span's entering carry becomes on the way to it, and what it becomes behind the span;
 // k_recur_join then goes along the spans.  All in a fixed order, so that a result does not depend on which wave was first.
-constexpr int kSpan = 16;
+constexpr int kSpan = 8;
+constexpr uint32_t kCrosses = 0x80000000u;
 struct Carries {
     float *b, *a;                       // [tiles, dim]: what enters a tile is b, or a * (what enters its span) + b where `open`
     float *span_b, *span_a;             // [spans, dim]: what the span before hands on; after the join, span_b is what enters
     uint8_t *open, *span_open;
-    int32_t* list;                      // list of a tile's first place, or (backward) its last one
+    uint32_t* list;                     // list of a tile's first place, or (backward) its last one; kCrosses: it reaches into the tile beside
     int64_t tile_rows, tiles;
 };
 
@@ -409,17 +415,23 @@ __device__ __forceinline__ void join_span(const Carries& t, const Effect<V>& min
         if (lead) t.span_open[to] = e.open;
     }
 }
-// What enters a tile that its list reaches into.
+// What enters a tile, where its list crosses the border: read before that is known (whatever lies there then), so that it is no request more to wait for.
 template <int V>
-__device__ __forceinline__ void carry_of(const Carries& t, int64_t tile, int dim, int c, float (&v)[V]) {
+struct Entering {
     float a[V], b[V], e[V];
-    const bool open = uniform((int)t.open[tile]);
-    load_floats<V>(t.b + tile * dim + c, b);
-    load_floats<V>(t.a + tile * dim + c, a);             // (whatever lies there where it is not open)
-    load_floats<V>(t.span_b + tile / kSpan * dim + c, e);
+    int open;
+    __device__ Entering(const Carries& t, int64_t tile, int dim, int c) {
+        open = t.open[tile];
+        load_floats<V>(t.b + tile * dim + c, b);
+        load_floats<V>(t.a + tile * dim + c, a);
+        load_floats<V>(t.span_b + tile / kSpan * dim + c, e);
+    }
+    __device__ void take(bool crosses, float (&v)[V]) const {
+        const bool all = uniform(open);
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = open ? a[i] * e[i] + b[i] : b[i];
-}
+        for (int i = 0; i < V; ++i) v[i] = !crosses ? 0.0f : all ? a[i] * e[i] + b[i] : b[i];
+    }
+};
 
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l, const Carries t, int blocks) {
@@ -431,9 +443,9 @@ __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l,
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = begin + t.tile_rows;
     Effect<V> e = {};
     if (end < total) {
-        const int j = find_list(l, total, end);
-        if (lead) t.list[tile + 1] = j;
-        const int64_t first = uniform(l.begin_of(j, total));
+        int64_t first;
+        const int j = find_list(l, total, end, &first);
+        if (lead) t.list[tile + 1] = (uint32_t)j | (first < end ? kCrosses : 0u);
         if (first < end) {
             e.open = first < begin;
             float rate[V];
@@ -479,8 +491,8 @@ __global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l,
     Effect<V> e = {};
     if (begin > 0 && begin < total) {
         const int j = find_list(l, total, begin - 1);
-        if (lead) t.list[tile - 1] = j;
         const int64_t last = uniform(l.begin_of((int64_t)j + 1, total)), end = min(last, begin + t.tile_rows);
+        if (lead) t.list[tile - 1] = (uint32_t)j | (last > begin ? kCrosses : 0u);
         if (last > begin) {
             e.open = end < last;
             float rate[V];
@@ -612,8 +624,11 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
     const Share share(blockIdx.x, blocks);
     const int64_t tile = ((t.tiles + kWaves - 1) / kWaves - 1 - share.q) * kWaves + wave;
     const int c = channel_of<V>(l.dim, share.block);
+    if (tile < 0) return;
+    const Entering<V> entering(t, tile, l.dim, c);
+    const uint32_t known = tile ? t.list[tile] : 0u;
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
-    if (tile < 0 || begin >= end) return;
+    if (begin >= end) return;
     Pack<T, V> u[kSaved], x[kSaved];
     const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total);
     const Along rows_h(l, h_out, ld_h, total);
@@ -621,10 +636,9 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
     read_rows<T, V>(x, rows_x, total, begin, c);
     float rate[V], h[V];
     rates<V, DECAY>(l, c, rate);
-    const int j = tile ? uniform(t.list[tile]) : find_list(l, total, 0);
-    const bool fresh = uniform(l.begin_of(j, total)) == begin;
-    if (fresh) load_or_zero<V>(nullptr, h);
-    else carry_of<V>(t, tile, l.dim, c, h);
+    const int j = tile ? uniform((int)(known & ~kCrosses)) : find_list(l, total, 0);
+    const bool fresh = !uniform((int)(known & kCrosses));
+    entering.take(!fresh, h);
     Batch b = locate<true, DECAY>(l, total, look_ahead<true, DECAY>(l, total, begin, j), fresh, 0, DECAY ? l.ts[l.row(max(begin - 1, (int64_t)0), total)] : 0.0f);
     Edges<V> enter;
     enter.template read<true>(l.h0, b, (uint32_t)b.starts & kGroupMask, 0, l.dim, c);
@@ -690,6 +704,8 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
     float sum[V] = {};
     if (tile >= 0 && begin < end) {
+        const Entering<V> entering(t, tile, l.dim, c);
+        const uint32_t known = end < total ? t.list[tile] : 0u;
         const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved, last_batch = begin + (end - 1 - begin) / kBatch * kBatch;
         Pack<T, V> u[kSaved], x[kSaved], d[kSaved] = {};      // (d stays zero without dh)
         float enter[V];                                     // state before the group
@@ -707,10 +723,9 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
         read_grads(last_group);
         float rate[V], back[V];
         rates<V, DECAY>(l, c, rate);
-        const int j = end < total ? uniform(t.list[tile]) : find_list(l, total, end - 1);
-        const bool over = uniform(l.begin_of((int64_t)j + 1, total)) <= end;
-        if (over) load_or_zero<V>(nullptr, back);
-        else carry_of<V>(t, tile, l.dim, c, back);
+        const int j = end < total ? uniform((int)(known & ~kCrosses)) : find_list(l, total, end - 1);
+        const bool over = end == total || !uniform((int)(known & kCrosses));
+        entering.take(!over, back);
         auto time_before = [&](int64_t p) { return DECAY ? l.ts[l.row(max(p - 1, (int64_t)0), total)] : 0.0f; };
         Batch b = locate<false, DECAY>(l, total, look_ahead<false, DECAY>(l, total, last_batch, j), over, (int)(end - 1 - last_batch), time_before(last_batch));
         Edges<V> start, leave;
@@ -927,7 +942,7 @@ Workspace carve(const tns_recur& r, void* base) {
     w.t.span_a = static_cast<float*>(take(w.spans * row));
     w.t.open = static_cast<uint8_t*>(take(w.t.tiles));
     w.t.span_open = static_cast<uint8_t*>(take(w.spans));
-    w.t.list = static_cast<int32_t*>(take(w.t.tiles * 4));
+    w.t.list = static_cast<uint32_t*>(take(w.t.tiles * 4));
     w.sums = static_cast<float*>(take((w.t.tiles + kWaves - 1) / kWaves * row));
     return w;
 }
