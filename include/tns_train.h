@@ -136,7 +136,7 @@ TNS_API int tns_pair_loss(const tns_pairs *p, float *d_loss, float *d_margin, vo
  * States that are not finite poison their 256 weights, as they would poison single ones in 32 bits.
  */
 typedef struct {
-    int64_t n;                 /* weights, 0 .. 2^40                                                       */
+    int64_t n;                 /* weights, 0 .. 2^36; fewer than 2^36 in all tensors, each rounded up to 4096 */
     float *d_param;            /* fp32                                                                     */
     void *d_copy;              /* bf16 [n], may be NULL: receives the new weights, rounded to nearest       */
     const void *d_grad;        /* of the configuration's grad_dtype                                         */

@@ -1,6 +1,7 @@
 // AdamW over all tensors of a model in one launch, states in 32 or in 8 bits (include/tns_train.h).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -30,28 +31,24 @@ __host__ __device__ inline uint64_t mix64(uint64_t z) {        // output functio
     return z ^ (z >> 31);
 }
 
-struct Tensor {
+// A workgroup's tile of a tensor, whole in itself: one request, and the addresses of everything else are known.
+struct Part {
     float* param;
     bf16* copy;
     const void* grad;
     void *m, *v;
     float *m_scale, *v_scale;
-    int64_t n;
     uint64_t word0;                   // number of the random word of its first four weights
-    float decay;
+    int32_t n;                        // weights, kTile at most
     int32_t aligned;                  // four weights of every buffer can be read at once
-};
-
-struct Tile {
-    int32_t tensor;
-    uint32_t index;                   // of the tile in its tensor
+    float decay;
 };
 
 struct Step {                         // factors of one step, rounded to fp32 once
     float beta1, rest1, beta2, rest2, lr, rate, root, eps;
     uint64_t key;
 };
-__device__ __forceinline__ float step_keep(const Step& s, const Tensor& t) {
+__device__ __forceinline__ float step_keep(const Step& s, const Part& t) {
 #pragma clang fp contract(off)
     return 1.0f - s.lr * t.decay;
 }
@@ -112,7 +109,7 @@ struct Four {
     float m_scale, v_scale;
 
     // All of them, from aligned addresses.
-    __device__ void read(const Tensor& t, int64_t block, int64_t i0) {
+    __device__ void read(const Part& t, int block, int i0) {
         const float4 q = *reinterpret_cast<const float4*>(t.param + i0);
         p[0] = q.x; p[1] = q.y; p[2] = q.z; p[3] = q.w;
         const Grads r = *reinterpret_cast<const Grads*>(static_cast<const G*>(t.grad) + i0);
@@ -133,7 +130,7 @@ struct Four {
             v_scale = t.v_scale[block];
         }
     }
-    __device__ void write(const Tensor& t, int64_t block, int64_t i0) const {
+    __device__ void write(const Part& t, int block, int i0) const {
         *reinterpret_cast<float4*>(t.param + i0) = make_float4(p[0], p[1], p[2], p[3]);
         if (t.copy) {
             bf16 c[4];
@@ -151,7 +148,7 @@ struct Four {
         }
     }
     // The first n of them, one by one; the others are zero.
-    __device__ void read(const Tensor& t, int64_t block, int64_t i0, int n) {
+    __device__ void read(const Part& t, int block, int i0, int n) {
         mc = vc = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -171,7 +168,7 @@ struct Four {
             v_scale = t.v_scale[block];
         }
     }
-    __device__ void write(const Tensor& t, int64_t block, int64_t i0, int n) const {
+    __device__ void write(const Part& t, int block, int i0, int n) const {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (k >= n) continue;
@@ -218,35 +215,39 @@ struct Four {
 
 // A workgroup per tile.  Bound by memory: what lies in it is read and written once; a wave reads its four blocks before it computes.
 template <int BITS, typename G>
-__global__ void __launch_bounds__(256) k_adamw(const Tensor* __restrict__ tensors, const Tile* __restrict__ tiles, const Step s, const float* __restrict__ grad_scale) {
+__global__ void __launch_bounds__(256) k_adamw(const Part* __restrict__ tiles, const Step s, const float* __restrict__ grad_scale) {
+    const Part t = tiles[blockIdx.x];
     const float gs = grad_scale ? *grad_scale : 1.0f;
     if (gs == 0.0f || !(fabsf(gs) <= 3.402823466e+38f)) return;
-    const Tile tile = tiles[blockIdx.x];
-    const Tensor t = tensors[tile.tensor];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr int kMine = kTile / kBlock / 4;                // blocks of a wave
-    const int64_t first = (int64_t)tile.index * (kTile / kBlock) + wave * kMine;
+    const int first = wave * kMine;
     const float keep = step_keep(s, t);
-    if (t.aligned && (first + kMine) * kBlock <= t.n) {
-        Four<BITS, G> f[kMine];
+    Four<BITS, G> f[kMine];
+    auto at = [&](int j) { return (first + j) * kBlock + lane * 4; };
+    auto whole = [&](int j) { return t.aligned && (first + j + 1) * kBlock <= t.n; };
+    auto count = [&](int j) { return min(max(t.n - at(j), 0), 4); };
+    if (whole(kMine - 1)) {
 #pragma unroll
-        for (int j = 0; j < kMine; ++j) f[j].read(t, first + j, (first + j) * kBlock + lane * 4);
+        for (int j = 0; j < kMine; ++j) f[j].read(t, first + j, at(j));
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
-            const int64_t i0 = (first + j) * kBlock + lane * 4;
-            f[j].step(s, keep, gs, t.word0 + (uint64_t)(i0 >> 2), 4);
-            f[j].write(t, first + j, i0);
+            f[j].step(s, keep, gs, t.word0 + (uint64_t)(at(j) >> 2), 4);
+            f[j].write(t, first + j, at(j));
         }
         return;
     }
+#pragma unroll
     for (int j = 0; j < kMine; ++j) {
-        const int64_t block = first + j, i0 = block * kBlock + lane * 4;
-        if (block * kBlock >= t.n) return;
-        const int n = (int)min(max(t.n - i0, (int64_t)0), (int64_t)4);
-        Four<BITS, G> f;
-        f.read(t, block, i0, n);
-        f.step(s, keep, gs, t.word0 + (uint64_t)(i0 >> 2), n);
-        f.write(t, block, i0, n);
+        if (whole(j)) f[j].read(t, first + j, at(j));
+        else if ((first + j) * kBlock < t.n) f[j].read(t, first + j, at(j), count(j));
+    }
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+        if ((first + j) * kBlock >= t.n) return;
+        f[j].step(s, keep, gs, t.word0 + (uint64_t)(at(j) >> 2), count(j));
+        if (whole(j)) f[j].write(t, first + j, at(j));
+        else f[j].write(t, first + j, at(j), count(j));
     }
 }
 
@@ -254,8 +255,7 @@ __global__ void __launch_bounds__(256) k_adamw(const Tensor* __restrict__ tensor
 
 struct tns_adamw {
     tns_adamw_config cfg;
-    Tensor* tensors = nullptr;
-    Tile* tiles = nullptr;
+    Part* tiles = nullptr;
     int64_t num_tiles = 0;
 };
 
@@ -274,12 +274,12 @@ int tns_adamw_create(const tns_adamw_config* cfg, int32_t count, const tns_adamw
     for (int32_t i = 0; i < count; ++i) {
         const tns_adamw_tensor& t = tensors[i];
         if (t.n < 0) return fail(TNS_EINVAL, "negative number of weights");
-        if (t.n > (int64_t)1 << 40) return fail(TNS_ESIZE, "more than 2^40 weights in one tensor");
+        if (t.n > (int64_t)1 << 36) return fail(TNS_ESIZE, "more than 2^36 weights in one tensor");
         if (t.n && (!t.d_param || !t.d_grad || !t.d_m || !t.d_v)) return fail(TNS_EINVAL, "null weights, gradient or state");
         if (t.n && cfg->state_bits == 8 && (!t.d_m_scale || !t.d_v_scale)) return fail(TNS_EINVAL, "null scales of a state of 8 bits");
         if (!std::isfinite(t.weight_decay)) return fail(TNS_EINVAL, "weight_decay must be finite");
         total += (t.n + kTile - 1) / kTile;
-        if (total > (int64_t)INT32_MAX) return fail(TNS_ESIZE, "more than 2^43 weights in all");
+        if (total >= (int64_t)1 << 24) return fail(TNS_ESIZE, "more than 2^36 weights in all");      // a launch has fewer than 2^32 threads
     }
     DeviceGuard guard(cfg->device);
     if (guard.error() != hipSuccess) return fail_hip(guard.error(), "selecting the optimizer's device");
@@ -288,9 +288,7 @@ int tns_adamw_create(const tns_adamw_config* cfg, int32_t count, const tns_adamw
         opt = new tns_adamw();
         opt->cfg = *cfg;
         opt->num_tiles = total;
-        std::vector<Tensor> ts;
-        std::vector<Tile> tiles;
-        ts.reserve(count);
+        std::vector<Part> tiles;
         tiles.reserve(total);
         uint64_t word = 0;
         for (int32_t i = 0; i < count; ++i) {
@@ -298,18 +296,20 @@ int tns_adamw_create(const tns_adamw_config* cfg, int32_t count, const tns_adamw
             auto at = [](const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; };
             const size_t state = cfg->state_bits / 2, grad = cfg->grad_dtype == TNS_F32 ? 16 : 8;      // bytes of four values
             const bool all = at(t.d_param, 16) && at(t.d_copy, 8) && at(t.d_grad, grad) && at(t.d_m, state) && at(t.d_v, state);
-            ts.push_back({t.d_param, static_cast<bf16*>(t.d_copy), t.d_grad, t.d_m, t.d_v, t.d_m_scale, t.d_v_scale, t.n, word, (float)t.weight_decay, all});
-            for (int64_t k = 0; k * kTile < t.n; ++k) tiles.push_back({i, (uint32_t)k});
+            for (int64_t k = 0; k < t.n; k += kTile) {
+                auto from = [&](const void* p, size_t bytes) { return p ? (void*)((char*)p + k * bytes) : nullptr; };
+                auto scales = [&](float* p) { return p ? p + k / kBlock : nullptr; };
+                tiles.push_back({(float*)from(t.d_param, 4), (bf16*)from(t.d_copy, 2), from(t.d_grad, grad / 4), from(t.d_m, state / 4), from(t.d_v, state / 4),
+                                 scales(t.d_m_scale), scales(t.d_v_scale), word + (uint64_t)k / 4, (int32_t)std::min<int64_t>(t.n - k, kTile), all, (float)t.weight_decay});
+            }
             word += (uint64_t)((t.n + kBlock - 1) / kBlock) * (kBlock / 4);
         }
         if (total) {
-            hipError_t e = tns::device_malloc((void**)&opt->tensors, ts.size() * sizeof(Tensor));
-            if (e == hipSuccess) e = tns::device_malloc((void**)&opt->tiles, tiles.size() * sizeof(Tile));
-            if (e == hipSuccess) e = hipMemcpy(opt->tensors, ts.data(), ts.size() * sizeof(Tensor), hipMemcpyHostToDevice);
-            if (e == hipSuccess) e = hipMemcpy(opt->tiles, tiles.data(), tiles.size() * sizeof(Tile), hipMemcpyHostToDevice);
+            hipError_t e = tns::device_malloc((void**)&opt->tiles, tiles.size() * sizeof(Part));
+            if (e == hipSuccess) e = hipMemcpy(opt->tiles, tiles.data(), tiles.size() * sizeof(Part), hipMemcpyHostToDevice);
             if (e != hipSuccess) {
                 tns_adamw_destroy(opt);
-                return fail_hip(e, "copying the optimizer's tables");
+                return fail_hip(e, "copying the optimizer's table");
             }
         }
     } catch (const std::bad_alloc&) {
@@ -333,7 +333,7 @@ int tns_adamw_step(tns_adamw* opt, double lr, int64_t t, const float* d_grad_sca
                  (float)(lr / (1.0 - std::pow(c.beta1, (double)t))), (float)(1.0 / std::sqrt(1.0 - std::pow(c.beta2, (double)t))), (float)c.eps,
                  mix64(c.seed + kGolden * (uint64_t)t)};
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)opt->num_tiles), dim3(256), 0, static_cast<hipStream_t>(hip_stream), opt->tensors, opt->tiles, s, d_grad_scale);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)opt->num_tiles), dim3(256), 0, static_cast<hipStream_t>(hip_stream), opt->tiles, s, d_grad_scale);
     };
     if (c.state_bits == 32) c.grad_dtype == TNS_F32 ? launch(k_adamw<32, float>) : launch(k_adamw<32, bf16>);
     else c.grad_dtype == TNS_F32 ? launch(k_adamw<8, float>) : launch(k_adamw<8, bf16>);
@@ -346,7 +346,6 @@ int tns_adamw_destroy(tns_adamw* opt) {
     DeviceGuard guard(opt->cfg.device);
     if (guard.error() == hipSuccess) {
         (void)hipDeviceSynchronize();
-        if (opt->tensors) (void)hipFree(opt->tensors);
         if (opt->tiles) (void)hipFree(opt->tiles);
     }
     delete opt;
