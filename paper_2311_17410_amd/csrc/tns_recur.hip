@@ -145,7 +145,8 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
     const int lane = threadIdx.x & 63;
     int passed = 0, more = 0;                   // borders between `from` and the lane's place; and the place after lane 63's (FORWARD), before lane 0's
     int at = a.border;
-    for (int64_t base = a.from;;) {
+    bool all = false;                           // every border looked at lies in the batch
+    for (int64_t base = a.from, window = 0;; ++window) {
         const uint64_t some = __ballot(FORWARD ? at <= kBatch : at >= 0);
         if (some) {                             // they come in order: how many lie at or before (beyond) the lane's place
             int n = 0;
@@ -159,15 +160,31 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
             passed += n;
             more += __popcll(some);
                     }
-        if (some != ~0ull) break;
+        all = some == ~0ull;
+        if (!all || window == 3) break;
         base += FORWARD ? kWave : -kWave;
         at = border_at<FORWARD>(l, total, a.p0, base);
     }
     Batch b;
-    const int list = (int)min(max(a.from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
+    int list = (int)min(max(a.from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
+    if (all) {                                  // many lists without events: every lane looks for its own
+        const int64_t p = max(a.p0 + lane, (int64_t)0);
+        int64_t lo = 0, hi = l.S;
+        for (int k = 0; k < 31; ++k) {
+            const int64_t mid = (lo + hi) >> 1;
+            const bool at_or_before = l.begin_of(mid, total) <= p, go = hi - lo > 1;
+            lo = (go & at_or_before) ? mid : lo;
+            hi = (go & !at_or_before) ? mid : hi;
+        }
+        list = (int)lo;
+    }
     b.edge = __builtin_amdgcn_readlane(list, FORWARD ? kBatch - 1 : 0);
     b.list = (int)l.list(list);
-    if (FORWARD) {
+    if (all) {
+        const int64_t p = a.p0 + lane, begin = l.begin_of(list, total), end = l.begin_of((int64_t)list + 1, total);
+        b.starts = __ballot((p >= 0) & (p < total) & (begin == p));
+        b.ends = __ballot((p >= 0) & (p < total) & (end == p + 1));
+    } else if (FORWARD) {
         const int prev = __shfl_up(passed, 1);
         b.starts = __ballot((lane != 0) & (passed != prev)) | (uint64_t)(edge | (uniform(passed) != 0));
         b.ends = b.starts >> 1 | (uint64_t)(more != __builtin_amdgcn_readlane(passed, 63)) << 63;

@@ -566,3 +566,27 @@ def test_refusals_of_tensors(T):
         T.recur_run(rp, u, u, ts=u[:, 0].contiguous())
     with pytest.raises(TnsError):
         T.recur_run(rp, u[:1].expand(4, 8), u)
+
+
+def test_adamw_offsets_beyond_32_bits(T):
+    """A tensor of more than 2^31 weights (2^33 bytes): its end equals the oracle's, the rest stays zero."""
+    import torch
+    n, tail = (1 << 31) + 1000, 4096 + 1000
+    rng = np.random.default_rng(7)
+    w = the_weights(rng, [tail], 8, BF16)[0]
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(-(-n // 256), device="cuda") for _ in range(2))
+    scales = -(-tail // 256)
+    p[-tail:], g[-tail:] = torch_of(w["param"]), torch_of(w["grad"], BF16)
+    for to, k, size in ((m, "m", tail), (v, "v", tail), (ms, "m_scale", scales), (vs, "v_scale", scales)):
+        to[-size:] = torch_of(w["state"][k])
+    e4m3 = torch.float8_e4m3fn
+    opt = T.AdamW([p], [g], bits=8, weight_decay=0.1, seed=3, states=([m.view(e4m3)], [v.view(e4m3)], [ms], [vs]))
+    opt.step(1e-3, 4)
+    new, off, state = O.adamw(w["param"], w["grad"], w["state"], 4, n - tail, weight_decay=0.1, seed=3)
+    close("param", p[-tail:], new, off)
+    for got, k, size in ((m, "m", tail), (v, "v", tail), (ms, "m_scale", scales), (vs, "v_scale", scales)):
+        assert np.array_equal(got[-size:].cpu().numpy(), state[k]), k
+    assert not p[:-tail].any() and not m[:-tail].any() and not v[:-tail].any()
+    opt.close()
