@@ -108,8 +108,9 @@ struct Work {                         // how the links of an event are shared ou
 
 // The loss and all gradients in one pass over the sampled links: G lanes hold a row, NV vectors of VEC channels each, and the next R rows
 // are on their way while R are computed; the anchor and the sum for its gradient stay in registers.  The margins' losses and slopes, a
-// hundred instructions each, are computed for R rows at once, by a lane of every four each.  Bound by memory: (2 + K) rows read and written
-// for every event.
+// hundred instructions each, are computed for R rows at once, by a lane of every four each.  Bound by memory, (2 + K) rows read and written
+// for every event: 200 events of 10000 links, 128 fp32 channels, 2.06 GB in 425 us (4.9 TB/s).  Where an event has few links its first and
+// last steps show: 4000 of 50, 172 bf16 channels, 146 MB in 54 us (2.7 TB/s); 600 of one: 5.4 us.
 template <typename T, int VEC, int G, int NV, bool GRADS>
 __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, float* margin, T* danchor, T* dpos, T* dneg) {
     constexpr int kRows = 64 / G, R = NV == 1 ? 4 : NV == 2 ? 2 : 1;
@@ -343,7 +344,7 @@ __global__ void __launch_bounds__(256) k_pairs_wide_grads(const Pairs<T> p, cons
 }
 
 // Sum of the workgroups' losses (the first workgroup) and, where events were taken in parts, the gradients of anchor and pos from them:
-// kColumns channels of an event a workgroup, the parts shared by its threads.
+// kColumns channels of an event a workgroup, the parts shared by its threads (2 us without parts, 5 with eleven parts of 200 events).
 constexpr int kColumns = 64, kShares = 1024 / kColumns;
 template <typename T>
 __global__ void __launch_bounds__(1024) k_pairs_join(const Pairs<T> p, const Work w, int64_t groups, float* loss, T* danchor, T* dpos) {

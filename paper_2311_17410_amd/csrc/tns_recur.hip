@@ -356,7 +356,7 @@ __device__ __forceinline__ void rates(const Lists<T>& l, int c, float (&rate)[V]
 
 // A workgroup's share: block of channels and the q-th group of tiles.  Workgroups go round the eight XCDs; those of one group of tiles come
 // eight apart and so meet in one L2, as their blocks of channels share cache lines wherever rows are no multiple of them (172 channels of
-// fp32, 1.35 M rows: states 452 -> 338 us, gradients 776 -> 599 us).
+// fp32, 0.8 M rows: states 452 -> 338 us, gradients 776 -> 599 us).
 constexpr int kXcds = 8;
 struct Share {
     int64_t q;
@@ -450,6 +450,10 @@ struct Entering {
     }
 };
 
+// First pass of the states: reads the rows of every list that crosses the end of a tile, from the list's begin or the tile's on.  For short
+// lists that is half a list a tile (1.14 M rows of 128 bf16 channels in lists of ten: 30 us), for long ones all rows, and then bound by memory
+// (0.79 M rows of 256 bf16 channels: 0.80 GB in 182 us, 4.4 TB/s).  Sixteen tiles a workgroup took 213: two workgroups fill a compute unit,
+// and their waves wait for each other.
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l, const Carries t, int blocks) {
     const Share share(blockIdx.x, blocks);
@@ -497,6 +501,8 @@ __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l,
     join_span<V, true>(t, e, span, tile, l.dim, c, lead);
 }
 
+// First pass of the gradients: what the rows behind a tile's begin send back over it, from u and dh.  As k_recur_tails (0.79 M rows of 256
+// bf16 channels: 179 us).
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l, const Carries t, int blocks, const T* dh, int64_t ld_dh, const float* dlast) {
     const Share share(blockIdx.x, blocks);
@@ -545,7 +551,8 @@ __global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l,
 }
 
 // Puts the open spans' carries together, from span 1 on or (BACKWARD) from the last but one down: kChannels channels a workgroup, each
-// with kParts parts of the spans: every thread joins its part, the parts are scanned, every thread goes through its part again.
+// with kParts parts of the spans: every thread joins its part, the parts are scanned, every thread goes through its part again.  Bound by
+// how fast a few compute units read 32 bytes of a row each: 22 us for 1536 spans of 256 channels, 2 to 5 where no list is that long.
 constexpr int kChannels = 8, kParts = 1024 / kChannels, kAtOnce = 8;
 template <bool BACKWARD>
 __global__ void __launch_bounds__(1024) k_recur_join(int64_t spans, int dim, float* carry, const float* factor, const uint8_t* open) {
@@ -629,6 +636,11 @@ __device__ void fill_empty(const Lists<T>& l, int64_t first, const float* from, 
     }
 }
 
+// h = f h + z x along the rows of a tile, V channels a lane, 16 rows in registers and the next 16 on their way.  The list a row belongs to, and
+// the gap before it, lie in the lanes (64 rows at a time); what is the same for the wave (addresses, first and last rows) is the scalar
+// unit's.  Bound by memory: 0.79 M rows of 256 bf16 channels, all states written and saved, 1.23 GB in 223 us (5.5 TB/s); 0.80 M rows of
+// 172 fp32 channels, 1.70 GB in 331 us (5.1); 0.91 M of 128 fp32, 1.39 GB in 238 us (5.9); lists of ten, last states only, 1.14 M rows of 128
+// bf16: 0.69 GB in 150 us (4.6).
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Carries t, int blocks, T* h_out, int64_t ld_h, float* last, float* saved) {
     const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
@@ -705,6 +717,11 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
 
 // ---- gradients -----------------------------------------------------------------------------------------
 
+// The gradients of a tile's rows, group by group from the last one back.  A group's states are computed again from the one saved before it
+// (a sixteenth of what reading them all would cost, and they stay in fp32), then the group is walked back.  The next rows of u and x are on
+// their way during the walk back, those of dh during the walk forward: a second set of registers for them left one wave a SIMD instead of
+// two.  Bound by memory: 0.79 M rows of 256 bf16 channels, 2.06 GB in 397 us (5.2 TB/s); 0.80 M of 172 fp32, 2.78 GB in 602 us (4.6); lists
+// of ten, 1.14 M rows of 128 bf16, 1.28 GB in 266 us (4.8).
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Carries t, int blocks, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
                                                      T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
@@ -831,7 +848,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
     }
 }
 
-// Sums of the workgroups' shares, kChannels channels a workgroup, in a fixed order.
+// Sums of the workgroups' shares, kChannels channels a workgroup, in a fixed order (4469 shares of 128 channels: 13 us).
 __global__ void __launch_bounds__(1024) k_recur_sums(const float* sums, int64_t shares, int dim, float* out) {
     __shared__ float s_sum[kParts][kChannels];
     const int part = threadIdx.x / kChannels, ch = threadIdx.x % kChannels, c = (int)blockIdx.x * kChannels + ch;
@@ -859,7 +876,8 @@ struct alignas(sizeof(T) * N) Vec {
     T v[N];
 };
 // G lanes to an event, VEC channels a lane at a time.  Bound by memory; the states lie anywhere, so a row of them is read in as few
-// requests as there are.
+// requests as there are: 66600 events of 172 bf16 channels, 161 MB in 33 us (4.9 TB/s); a workgroup of 256 threads to an event, a channel
+// each, took 63.  600 events of 100: 3.4 us, the launch and three reads one after the other.
 template <typename T, int VEC, int G>
 __global__ void __launch_bounds__(256) k_recur_step(int64_t B, int64_t num_ids, int dim, const int32_t* __restrict__ ids, const T* __restrict__ u, int64_t ld_u,
                                                     const T* __restrict__ x, int64_t ld_x, const float* __restrict__ ts, const float* __restrict__ decay, float* state,
@@ -923,7 +941,9 @@ int check_workspace(const void* p, size_t have, size_t need) {
 }
 
 // Rows of a tile.  A wave takes a tile's rows one after the other, so a small call is as long as its tiles; the fewer waves a large one
-// has, the less their reads overlap and the more unevenly they fill the chip; and every tile has its carry to find.
+// has, the less their reads overlap and the more unevenly they fill the chip; and every tile has its carry to find.  Tiles of 16, 32 and 64
+// rows: 35 K rows of 100 fp32 channels, states 13.6, 12.2, 15.2 us, gradients 21.2, 19.3, 24.5.  Of 64, 128 and 256: 0.79 M rows of 256
+// bf16 channels, states 219, 238, 246, gradients 378, 399, 413.
 // (A launch has fewer than 2^32 threads: tiles grow where there would be more than 2^20 workgroups of a span.)
 int64_t tile_rows_of(int64_t rows, int dim) {
     const int64_t blocks = (dim + kWave - 1) / kWave;
