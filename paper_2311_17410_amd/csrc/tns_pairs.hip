@@ -67,11 +67,21 @@ __device__ __forceinline__ float of_quad(float v, int r) {
     return r == 0 ? moved<0x00>(v) : r == 1 ? moved<0x55>(v) : r == 2 ? moved<0xAA>(v) : moved<0xFF>(v);
 }
 
-// Loss of a margin and its slope, both times scale and weight.
+// Loss of a margin and its slope, both times scale and weight.  softplus(-m) = log(1 + e) + max(-m, 0) with e = exp(-|m|); the logarithm is
+// twice the inverse hyperbolic tangent of e / (2 + e), which is a third at most: nine terms of its series leave 1e-10 of it.
 __device__ __forceinline__ void loss_of(float m, float w, float scale, float smoothing, float& loss, float& slope) {
-    const float e = expf(-fabsf(m)), tail = log1pf(e);                      // softplus(-m) = tail + max(-m, 0)
+    const float e = __builtin_amdgcn_exp2f(-fabsf(m) * tns::kLog2e), t = e * __builtin_amdgcn_rcpf(2.0f + e), q = t * t;
+    float tail = 1.0f / 17;
+    tail = tail * q + 1.0f / 15;
+    tail = tail * q + 1.0f / 13;
+    tail = tail * q + 1.0f / 11;
+    tail = tail * q + 1.0f / 9;
+    tail = tail * q + 1.0f / 7;
+    tail = tail * q + 1.0f / 5;
+    tail = tail * q + 1.0f / 3;
+    tail = 2.0f * t * (tail * q + 1.0f);
     loss = scale * w * (tail + fmaxf(-m, 0.0f) * (1.0f - smoothing) + fmaxf(m, 0.0f) * smoothing);
-    slope = scale * w * (smoothing - (m > 0.0f ? e : 1.0f) / (1.0f + e));   // sigmoid(-m)
+    slope = scale * w * (smoothing - (m > 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e));      // sigmoid(-m)
     if (m != m) loss = slope = m;
 }
 
@@ -93,6 +103,11 @@ __device__ __forceinline__ void load(const T* p, uint32_t bytes, bool there, flo
     }
 }
 template <typename T, int VEC>
+__device__ __forceinline__ void load(const T* p, uint32_t bytes, bool there, Vec<T, VEC>& v) {
+    v = Vec<T, VEC>{};
+    if (there) v = *reinterpret_cast<const Vec<T, VEC>*>(reinterpret_cast<const char*>(p) + bytes);
+}
+template <typename T, int VEC>
 __device__ __forceinline__ void store(T* p, uint32_t bytes, const float (&v)[VEC]) {
     Vec<T, VEC> raw;
 #pragma unroll
@@ -110,7 +125,8 @@ struct Work {                         // how the links of an event are shared ou
 // are on their way while R are computed; the anchor and the sum for its gradient stay in registers.  The margins' losses and slopes, a
 // hundred instructions each, are computed for R rows at once, by a lane of every four each.  Bound by memory, (2 + K) rows read and written
 // for every event: 200 events of 10000 links, 128 fp32 channels, 2.06 GB in 425 us (4.9 TB/s).  Where an event has few links its first and
-// last steps show: 4000 of 50, 172 bf16 channels, 146 MB in 54 us (2.7 TB/s); 600 of one: 5.4 us.
+// last steps show: 4000 of 50, 172 bf16 channels, 146 MB in 34 us (4.3 TB/s; 54 with the
+// library's exponential and logarithm and 64-bit indices: bound by instructions); 600 of one: 5.0 us.
 template <typename T, int VEC, int G, int NV, bool GRADS>
 __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, float* margin, T* danchor, T* dpos, T* dneg) {
     constexpr int kRows = 64 / G, R = NV == 1 ? 4 : NV == 2 ? 2 : 1;
@@ -134,24 +150,28 @@ __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, f
         const bool real = unit < units;
         const int64_t b = real ? unit / w.chunks : 0, k_begin = real ? unit % w.chunks * w.links : 0, k_end = real ? min(k_begin + w.links, p.K) : 0;
         float a[NV][VEC], acc[NV][VEC], dot = 0.0f;
-        // Links of an iteration: row r of this lane's is k0 + r * kRows + row; the lane sees to the weight and the loss of one of them.
-        const int r_mine = lane % 4 % R;
-        const int64_t by = (int64_t)w.waves * kRows * R, base = b * p.K;
-        auto weight_of = [&](int64_t k0) {                   // (read by every lane: what lanes read of each other is never behind a branch)
-            const int64_t k = k0 + r_mine * kRows + row;
-            const float v = p.weight && k_begin < k_end ? p.weight[base + min(k, k_end - 1)] : 1.0f;
-            return k < k_end ? v : 0.0f;
+        // The part's links, fewer than 2^30.  Row r of an iteration is link k0 + r * kRows + row; the lane sees to the weight and the loss of
+        // one of the R.  (What lanes read of each other is computed without branches.)
+        const int count = (int)(k_end - k_begin), r_mine = lane % 4 % R, by = w.waves * kRows * R, of_mine = r_mine * kRows + row;
+        const int64_t base = b * p.K + k_begin;
+        const T* const neg = p.neg + base * p.dim;
+        T* const to = GRADS ? dneg + base * p.dim : nullptr;
+        auto weight_of = [&](int k0) {
+            const int k = k0 + of_mine;
+            const float v = p.weight && count > 0 ? p.weight[base + min(k, count - 1)] : 1.0f;
+            return k < count ? v : 0.0f;
         };
-        auto read = [&](int64_t k0, float weight, float (&n)[R][NV][VEC]) {
+        auto ref_of = [&](int k0) { return p.ref && count > 0 ? p.ref[base + min(k0 + of_mine, count - 1)] : 0.0f; };
+        auto read = [&](int k0, float weight, Vec<T, VEC> (&n)[R][NV]) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const bool is = of_quad(weight, r) != 0.0f;
 #pragma unroll
-                for (int j = 0; j < NV; ++j) load<T, VEC>(p.neg + (base + k0 + r * kRows) * p.dim, mine_at[j], there[j] && is, n[r][j]);
+                for (int j = 0; j < NV; ++j) load<T, VEC>(neg + (int64_t)(k0 + r * kRows) * p.dim, mine_at[j], there[j] && is, n[r][j]);
             }
         };
-        const int64_t k_first = k_begin + part_of * kRows * R;
-        float weight = weight_of(k_first), weight_next = weight_of(k_first + by);
+        const int k_first = part_of * kRows * R;
+        float weight = weight_of(k_first), weight_next = weight_of(k_first + by), ref = ref_of(k_first), ref_next = ref_of(k_first + by);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float q[VEC];
@@ -163,16 +183,13 @@ __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, f
                 acc[j][i] = 0.0f;
             }
         }
-        float n[R][NV][VEC];
+        Vec<T, VEC> n[R][NV];
         read(k_first, weight, n);
         const float plus = row_sum<G>(dot);
         float loss_sum = 0.0f, slope_sum = 0.0f, any = 0.0f;
-        for (int64_t k0 = k_first; k0 < k_end; k0 += by) {
-            const int64_t k_mine = k0 + r_mine * kRows + row;
-            const bool mine = k_mine < k_end;
-            const float ref = p.ref ? p.ref[base + min(k_mine, k_end - 1)] : 0.0f;
-            const float weight_after = weight_of(k0 + 2 * by);
-            float next[R][NV][VEC];
+        for (int k0 = k_first; k0 < count; k0 += by) {
+            const float weight_after = weight_of(k0 + 2 * by), ref_after = ref_of(k0 + 2 * by);
+            Vec<T, VEC> next[R][NV];
             read(k0 + by, weight_next, next);
             float minus = 0.0f;                              // of the lane's row
 #pragma unroll
@@ -181,46 +198,44 @@ __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, f
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
-                    for (int c = 0; c < VEC; ++c) sum += a[j][c] * n[r][j][c];
+                    for (int c = 0; c < VEC; ++c) sum += a[j][c] * as_float(n[r][j].v[c]);
                 sum = row_sum<G>(sum);
                 if (r == r_mine) minus = sum;
             }
-            float m = 0.0f, loss = 0.0f, slope = 0.0f;
-            if (weight != 0.0f) {
-                m = p.beta * (plus - minus - ref);
-                loss_of(m, weight, p.scale, p.smoothing, loss, slope);
-                slope *= p.beta;
-                any = 1.0f;
-            }
-            loss_sum += loss;
+            float m = p.beta * (plus - minus - ref), loss, slope;
+            loss_of(m, weight, p.scale, p.smoothing, loss, slope);
+            const bool read_it = weight != 0.0f;
+            m = read_it ? m : 0.0f;
+            slope = read_it ? slope * p.beta : 0.0f;
+            loss_sum += read_it ? loss : 0.0f;
+            any = read_it ? 1.0f : any;
             slope_sum += slope;
-            if (margin && mine && lane % G < R) margin[base + k_mine] = m;
+            if (margin && k0 + of_mine < count && lane % G < R) margin[base + k0 + of_mine] = m;
             if (GRADS) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const float s = of_quad(slope, r);
                     const bool is = of_quad(weight, r) != 0.0f;
-                    const bool real_row = row < k_end - k0 - r * kRows;
 #pragma unroll
                     for (int j = 0; j < NV; ++j) {
                         float out[VEC];
 #pragma unroll
                         for (int c = 0; c < VEC; ++c) {
-                            acc[j][c] -= s * n[r][j][c];
+                            acc[j][c] -= s * as_float(n[r][j].v[c]);
                             out[c] = is ? -s * a[j][c] : 0.0f;
                         }
-                        if (real_row && there[j]) store<T, VEC>(dneg + (base + k0 + r * kRows) * p.dim, mine_at[j], out);
+                        if (k0 + r * kRows + row < count && there[j]) store<T, VEC>(to + (int64_t)(k0 + r * kRows) * p.dim, mine_at[j], out);
                     }
                 }
             }
             weight = weight_next;
             weight_next = weight_after;
+            ref = ref_next;
+            ref_next = ref_after;
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int c = 0; c < VEC; ++c) n[r][j][c] = next[r][j][c];
+                for (int j = 0; j < NV; ++j) n[r][j] = next[r][j];
         }
         auto sum_up = [&](float v) {                         // over the lanes' rows, and the rows side by side
             if (R >= 2) v += moved<0xB1>(v);
@@ -409,7 +424,7 @@ size_t aligned(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 // Few events are cut into parts, so that there are some 2048 workgroups of four waves (two for every wave's place of the chip); a part
 // has 64 links at least.  A part of few links is one wave's where there are enough of them (4000 events of 50 links, 172 channels in 16
-// bits: 54 us, four waves a part 66; 200 events of 10000, 128 channels in 32 bits: 483 us, four waves 426).
+// bits: 34 us, four waves a part 39; 200 events of 10000, 128 channels in 32 bits: 474 us, four waves 423).
 struct Workspace {
     Work w;
     float* slopes;                    // [B, K], of rows that may be too wide for a wave
