@@ -40,7 +40,8 @@ enum { TNS_F32 = 0, TNS_BF16 = 1 };
  *   flags             TNS_NEWEST_FIRST: a list's first row is its newest event (tns_run's order under the
  *                     recent policy); otherwise its oldest
  *   d_u, d_x          T [rows, dim], ld_u / ld_x elements from one row to the next (>= dim); aligned to T
- *   d_ts [rows], d_decay [dim]   both or neither
+ *   d_ts [rows], d_decay [dim]   both or neither; decay >= 0 (with a negative one the state grows, and what rows do
+ *                     to a state, multiplied up over a long list, may overflow)
  *   d_h0 [S, dim], d_t0 [S]      may be NULL; d_t0 needs d_ts
  */
 enum { TNS_NEWEST_FIRST = 1 };
@@ -155,7 +156,7 @@ typedef struct tns_adamw tns_adamw;
 
 /* `tensors` (HOST, count entries) is copied; the buffers they name have to stay where they are.  Buffers of one optimizer must not overlap. */
 TNS_API int tns_adamw_create(const tns_adamw_config *cfg, int32_t count, const tns_adamw_tensor *tensors, tns_adamw **out);
-/* Step t >= 1.  d_grad_scale [1] may be NULL (1); where it is 0 or not finite nothing is changed: the step is left out. */
+/* Step t >= 1.  A captured step keeps its lr and t.  d_grad_scale [1] may be NULL (1); where it is 0 or not finite nothing is changed: the step is left out. */
 TNS_API int tns_adamw_step(tns_adamw *opt, double lr, int64_t t, const float *d_grad_scale, void *hip_stream);
 /* Waits for the device; opt may be NULL. */
 TNS_API int tns_adamw_destroy(tns_adamw *opt);

@@ -159,7 +159,7 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
             if (n == 63 && (FORWARD ? border <= lane : border > lane)) n = 64;
             passed += n;
             more += __popcll(some);
-                    }
+        }
         all = some == ~0ull;
         if (!all || window == 3) break;
         base += FORWARD ? kWave : -kWave;
@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
     const Share share(blockIdx.x, blocks);
     const int64_t tile = ((t.tiles + kWaves - 1) / kWaves - 1 - share.q) * kWaves + wave;
     const int c = channel_of<V>(l.dim, share.block);
-    if (tile < 0) return;
+    if (tile < 0 || tile >= t.tiles) return;
     const Entering<V> entering(t, tile, l.dim, c);
     const uint32_t known = tile ? t.list[tile] : 0u;
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
@@ -737,7 +737,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
     const int c = channel_of<V>(l.dim, share.block);
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
     float sum[V] = {};
-    if (tile >= 0 && begin < end) {
+    if (tile >= 0 && begin < end) {         // (and so tile < t.tiles)
         const Entering<V> entering(t, tile, l.dim, c);
         const uint32_t known = end < total ? t.list[tile] : 0u;
         const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved, last_batch = begin + (end - 1 - begin) / kBatch * kBatch;
