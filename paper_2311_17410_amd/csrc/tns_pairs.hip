@@ -129,7 +129,7 @@ struct Work {                         // how the links of an event are shared ou
 // library's exponential and logarithm and 64-bit indices: bound by instructions); 600 of one: 5.0 us.
 template <typename T, int VEC, int G, int NV, bool GRADS>
 __global__ void __launch_bounds__(256) k_pairs(const Pairs<T> p, const Work w, float* margin, T* danchor, T* dpos, T* dneg) {
-    constexpr int kRows = 64 / G, R = NV == 1 ? 4 : NV == 2 ? 2 : 1;
+    constexpr int kRows = 64 / G, R = NV * VEC <= 4 ? 4 : NV * VEC <= 8 ? 2 : 1;
     __shared__ float s_acc[kWaves][GRADS ? G * VEC * NV : 1], s_sum[kWaves][3];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), row = lane / G;
     const int part_of = wave % w.waves;                      // which of the part's waves this is
