@@ -305,16 +305,21 @@ __device__ __forceinline__ Pack<T, V> load_row(Global row, uint32_t bytes) {
     asm("" : "+v"(bytes));              // (stays 32 bits: address = scalar base + vector offset)
     return *(const TNS_GLOBAL Pack<T, V>*)(row + bytes);
 }
-template <typename T, int V>
+// STREAM: with the non-temporal hint (streams_out).
+template <bool STREAM, typename T, int V>
 __device__ __forceinline__ void store_row(Global row, uint32_t bytes, const float (&v)[V]) {
     asm("" : "+v"(bytes));
+    using Bits = std::conditional_t<sizeof(T) * V == 4, uint32_t, uint16_t>;
+    Bits bits;
     if constexpr (V == 2) {
         using Two = float __attribute__((ext_vector_type(2)));
         using Halves = __bf16 __attribute__((ext_vector_type(2)));
-        *(TNS_GLOBAL Halves*)(row + bytes) = __builtin_convertvector((Two{v[0], v[1]}), Halves);
+        bits = __builtin_bit_cast(Bits, __builtin_convertvector((Two{v[0], v[1]}), Halves));
     } else {
-        *(TNS_GLOBAL T*)(row + bytes) = as_value<T>(v[0]);
+        bits = __builtin_bit_cast(Bits, as_value<T>(v[0]));
     }
+    if constexpr (STREAM) __builtin_nontemporal_store(bits, (TNS_GLOBAL Bits*)(row + bytes));
+    else *(TNS_GLOBAL Bits*)(row + bytes) = bits;
 }
 // The kSaved rows from place p on, 0 <= p < total; the walk's last row again where there are no more.
 template <typename T, int V>
@@ -641,7 +646,7 @@ __device__ void fill_empty(const Lists<T>& l, int64_t first, const float* from, 
 // unit's.  Bound by memory: 0.79 M rows of 256 bf16 channels, all states written and saved, 1.23 GB in 223 us (5.5 TB/s); 0.80 M rows of
 // 172 fp32 channels, 1.70 GB in 331 us (5.1); 0.91 M of 128 fp32, 1.39 GB in 238 us (5.9); lists of ten, last states only, 1.14 M rows of 128
 // bf16: 0.69 GB in 150 us (4.6).
-template <typename T, int V, bool DECAY>
+template <typename T, int V, bool DECAY, bool STREAM>
 __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Carries t, int blocks, T* h_out, int64_t ld_h, float* last, float* saved) {
     const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
     const int wave = uniform((int)(threadIdx.x >> 6));
@@ -703,7 +708,7 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
             gates<V, DECAY>(u[r], rate, DECAY ? read_lane(b.gap, q + r) : 0.0f, z, rest, f);
 #pragma unroll
             for (int i = 0; i < V; ++i) h[i] = f[i] * h[i] + z[i] * x[r].get(i);
-            if (h_out) store_row<T, V>(to, (uint32_t)c * sizeof(T), h);
+            if (h_out) store_row<STREAM, T, V>(to, (uint32_t)c * sizeof(T), h);
             to = rows_h.next(to);
             if (ends >> r & 1)
                 if (last) store_floats<V>(last + (Edges<V>::at(last, b, q + r, l.dim) - last) + c, h);
@@ -722,7 +727,7 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
 // their way during the walk back, those of dh during the walk forward: a second set of registers for them left one wave a SIMD instead of
 // two.  Bound by memory: 0.79 M rows of 256 bf16 channels, 2.06 GB in 397 us (5.2 TB/s); 0.80 M of 172 fp32, 2.78 GB in 602 us (4.6); lists
 // of ten, 1.14 M rows of 128 bf16, 1.28 GB in 266 us (4.8).
-template <typename T, int V, bool DECAY>
+template <typename T, int V, bool DECAY, bool STREAM>
 __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Carries t, int blocks, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
                                                      T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
     const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
@@ -820,8 +825,8 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
                     if (DECAY) sum[i] -= kept[r][i] * back[i] * g;
                     back[i] *= f[r][i];
                 }
-                store_row<T, V>(to_x, (uint32_t)c * sizeof(T), vx);
-                store_row<T, V>(to_u, (uint32_t)c * sizeof(T), vu);
+                store_row<STREAM, T, V>(to_x, (uint32_t)c * sizeof(T), vx);
+                store_row<STREAM, T, V>(to_u, (uint32_t)c * sizeof(T), vu);
                 to_x = rows_dx.back(to_x);
                 to_u = rows_du.back(to_u);
                 if (starts >> r & 1)
@@ -997,6 +1002,16 @@ unsigned groups_of(const tns_recur& r, const Workspace& w, int blocks, bool list
 }
 template <int V> int blocks_of(const tns_recur& r) { return (r.dim + kWave * V - 1) / (kWave * V); }
 
+// Whether rows are written past the caches: where one call's rows of u and x alone are more than the last-level cache holds (256 MiB), so that
+// nothing written stays there for a later call anyway and what is read twice has the room, and only rows that are whole lines of 128
+// bytes (others come in parts, which would each go to memory).  0.79 M rows of 256 bf16 channels, both directions: 1011 -> 957 us; 1.14 M of 128 in
+// lists of ten: 484 -> 466; with rows of 688 bytes, 0.80 M of them: 1444 -> 1650.
+template <typename T>
+bool streams_out(const tns_recur& r, const void* out, int64_t ld) {
+    const size_t line = 128;
+    return 2 * (size_t)r.rows * r.dim * sizeof(T) > size_t(256) << 20 && r.dim * sizeof(T) % line == 0 && ld * sizeof(T) % line == 0 && !misaligned(out, line);
+}
+
 template <bool BACKWARD>
 void launch_join(const tns_recur& r, const Workspace& w, hipStream_t stream) {
     if (w.spans > 1)
@@ -1012,8 +1027,13 @@ void launch_run(const tns_recur& r, void* h, int64_t ld_h, float* last, void* sa
         hipLaunchKernelGGL((k_recur_tails<T, V, DECAY>), dim3((unsigned)workgroups_of(w.spans, blocks)), dim3(kSpan * kWave), 0, stream, l, w.t, blocks);
         launch_join<false>(r, w, stream);
     }
-    if (const unsigned groups = groups_of(r, w, blocks, last != nullptr))
-        hipLaunchKernelGGL((k_recur_states<T, V, DECAY>), dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<T*>(h), ld_h, last, static_cast<float*>(saved));
+    if (const unsigned groups = groups_of(r, w, blocks, last != nullptr)) {
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<T*>(h), ld_h, last, static_cast<float*>(saved));
+        };
+        if (streams_out<T>(r, h, ld_h)) go(k_recur_states<T, V, DECAY, true>);
+        else go(k_recur_states<T, V, DECAY, false>);
+    }
 }
 
 template <typename T, int V, bool DECAY>
@@ -1027,9 +1047,14 @@ void launch_grad(const tns_recur& r, const void* saved, const void* dh, int64_t 
         hipLaunchKernelGGL((k_recur_heads<T, V, DECAY>), dim3((unsigned)workgroups_of(w.spans, blocks)), dim3(kSpan * kWave), 0, stream, l, w.t, blocks, d, ld_dh, dlast);
         launch_join<true>(r, w, stream);
     }
-    if (const unsigned groups = groups_of(r, w, blocks, dh0 != nullptr))
-        hipLaunchKernelGGL((k_recur_grads<T, V, DECAY>), dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<const float*>(saved), d, ld_dh, dlast,
-                           static_cast<T*>(du), ld_du, static_cast<T*>(dx), ld_dx, dh0, ddecay ? w.sums : nullptr);
+    if (const unsigned groups = groups_of(r, w, blocks, dh0 != nullptr)) {
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<const float*>(saved), d, ld_dh, dlast,
+                               static_cast<T*>(du), ld_du, static_cast<T*>(dx), ld_dx, dh0, ddecay ? w.sums : nullptr);
+        };
+        if (streams_out<T>(r, du, ld_du) && streams_out<T>(r, dx, ld_dx)) go(k_recur_grads<T, V, DECAY, true>);
+        else go(k_recur_grads<T, V, DECAY, false>);
+    }
     if (ddecay)
         hipLaunchKernelGGL(k_recur_sums, dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.sums, (w.t.tiles + kWaves - 1) / kWaves, r.dim, ddecay);
 }

@@ -590,3 +590,30 @@ def test_adamw_offsets_beyond_32_bits(T):
         assert np.array_equal(got[-size:].cpu().numpy(), state[k]), k
     assert not p[:-tail].any() and not m[:-tail].any() and not v[:-tail].any()
     opt.close()
+
+
+@pytest.mark.parametrize("dtype, dim", [(F32, 128), (BF16, 128)])
+def test_recurrence_rows_written_past_the_caches(T, dtype, dim):
+    """More rows than the last-level cache holds, of whole cache lines: the lists at the end equal the oracle's."""
+    import torch
+    n, tail = 600_000, [40, 0, 300, 7, 1]
+    rng = np.random.default_rng(16)
+    a = the_lists(rng, tail, dim, dtype, True, False)
+    g = on_gpu(a, dtype)
+    rows = n + sum(tail)
+    u, x, dh = (torch.zeros((rows, dim), dtype=g["u"].dtype, device="cuda") for _ in range(3))
+    assert 2 * u.numel() * u.element_size() > 1 << 28
+    tail_dh = values(rng, (sum(tail), dim), dtype)
+    u[n:], x[n:], dh[n:] = g["u"], g["x"], torch_of(tail_dh, dtype)
+    ts = torch.cat((torch.zeros(n, device="cuda"), g["ts"]))
+    rowptr = torch.cat((torch.arange(0, n, 100), n + torch.from_numpy(a["rowptr"]))).cuda()
+    first = rowptr.shape[0] - 1 - len(tail)
+    want = O.recurrence(**a, dh=tail_dh)
+    r = T.recur_run(rowptr, u, x, ts=ts, decay=g["decay"], save=True)
+    got = T.recur_grad(rowptr, u, x, saved=r["saved"], ts=ts, decay=g["decay"], dh=dh)
+    close("h", r["h"][n:], want["h"], want["h_off"], dtype)
+    close("last", r["last"][first:], want["last"], want["last_off"])
+    for name in ("du", "dx"):
+        close(name, got[name][n:], want[name], want[name + "_off"], dtype)
+        assert not got[name][:n].any()
+    close("ddecay", got["ddecay"], want["ddecay"], want["ddecay_off"])
