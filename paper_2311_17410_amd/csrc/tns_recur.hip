@@ -456,8 +456,8 @@ struct Entering {
 };
 
 // First pass of the states: reads the rows of every list that crosses the end of a tile, from the list's begin or the tile's on.  For short
-// lists that is half a list a tile (1.14 M rows of 128 bf16 channels in lists of ten: 30 us), for long ones all rows, and then bound by memory
-// (0.79 M rows of 256 bf16 channels: 0.80 GB in 182 us, 4.4 TB/s).  Sixteen tiles a workgroup took 213: two workgroups fill a compute unit,
+// lists that is half a list a tile (1.14 M rows of 128 bf16 channels in lists of ten: 29 us), for long ones all rows, and then bound by memory
+// (0.79 M rows of 256 bf16 channels: 0.80 GB in 168 us, 4.8 TB/s).  Sixteen tiles a workgroup took a sixth more: two workgroups fill a compute unit,
 // and their waves wait for each other.
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l, const Carries t, int blocks) {
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l,
 }
 
 // First pass of the gradients: what the rows behind a tile's begin send back over it, from u and dh.  As k_recur_tails (0.79 M rows of 256
-// bf16 channels: 179 us).
+// bf16 channels: 171 us).
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l, const Carries t, int blocks, const T* dh, int64_t ld_dh, const float* dlast) {
     const Share share(blockIdx.x, blocks);
@@ -644,8 +644,8 @@ __device__ void fill_empty(const Lists<T>& l, int64_t first, const float* from, 
 // h = f h + z x along the rows of a tile, V channels a lane, 16 rows in registers and the next 16 on their way.  The list a row belongs to, and
 // the gap before it, lie in the lanes (64 rows at a time); what is the same for the wave (addresses, first and last rows) is the scalar
 // unit's.  Bound by memory: 0.79 M rows of 256 bf16 channels, all states written and saved, 1.23 GB in 223 us (5.5 TB/s); 0.80 M rows of
-// 172 fp32 channels, 1.70 GB in 331 us (5.1); 0.91 M of 128 fp32, 1.39 GB in 238 us (5.9); lists of ten, last states only, 1.14 M rows of 128
-// bf16: 0.69 GB in 150 us (4.6).
+// 172 fp32 channels, 1.70 GB in 331 us (5.1); 0.91 M of 128 fp32, 1.39 GB in 236 us (5.9); lists of ten, last states only, 1.14 M rows of 128
+// bf16: 0.69 GB in 142 us (4.9).
 template <typename T, int V, bool DECAY, bool STREAM>
 __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Carries t, int blocks, T* h_out, int64_t ld_h, float* last, float* saved) {
     const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
@@ -725,8 +725,8 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
 // The gradients of a tile's rows, group by group from the last one back.  A group's states are computed again from the one saved before it
 // (a sixteenth of what reading them all would cost, and they stay in fp32), then the group is walked back.  The next rows of u and x are on
 // their way during the walk back, those of dh during the walk forward: a second set of registers for them left one wave a SIMD instead of
-// two.  Bound by memory: 0.79 M rows of 256 bf16 channels, 2.06 GB in 397 us (5.2 TB/s); 0.80 M of 172 fp32, 2.78 GB in 602 us (4.6); lists
-// of ten, 1.14 M rows of 128 bf16, 1.28 GB in 266 us (4.8).
+// two.  Bound by memory: 0.79 M rows of 256 bf16 channels, 2.06 GB in 414 us (5.0 TB/s); 0.80 M of 172 fp32, 2.78 GB in 602 us (4.6); lists
+// of ten, 1.14 M rows of 128 bf16, 1.28 GB in 276 us (4.6).
 template <typename T, int V, bool DECAY, bool STREAM>
 __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Carries t, int blocks, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
                                                      T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
