@@ -97,6 +97,8 @@ TNS_API int tns_recur_step(int64_t B, int64_t num_ids, int32_t dim, int32_t dtyp
  * scores, the scalar products of their embeddings; with ref it is taken relative to a frozen model's:
  *     m = beta * (anchor . pos - anchor . neg_k - ref)
  *     loss = scale * sum weight * ((1 - smoothing) softplus(-m) + smoothing softplus(m))
+ * A term whose factor is 0 is left out: without smoothing a pair of margin +infinity (ref = -infinity: the frozen model rules the
+ * link out) adds nothing to the loss, as its gradients are 0.
  *
  *   B, K         events and sampled links of each; B * K < 2^40, dim 1 .. 2^16
  *   d_anchor, d_pos   T [B, dim] with ld; d_neg T [B, K, dim], dense

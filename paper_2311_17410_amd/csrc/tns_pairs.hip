@@ -68,7 +68,8 @@ __device__ __forceinline__ float of_quad(float v, int r) {
 }
 
 // Loss of a margin and its slope, both times scale and weight.  softplus(-m) = log(1 + e) + max(-m, 0) with e = exp(-|m|); the logarithm is
-// twice the inverse hyperbolic tangent of e / (2 + e), which is a third at most: nine terms of its series leave 1e-10 of it.
+// twice the inverse hyperbolic tangent of e / (2 + e), which is a third at most: nine terms of its series leave 1e-10 of it.  A side
+// whose factor is 0 is left out: its margin may be infinite.
 __device__ __forceinline__ void loss_of(float m, float w, float scale, float smoothing, float& loss, float& slope) {
     const float e = __builtin_amdgcn_exp2f(-fabsf(m) * tns::kLog2e), t = e * __builtin_amdgcn_rcpf(2.0f + e), q = t * t;
     float tail = 1.0f / 17;
@@ -80,7 +81,8 @@ __device__ __forceinline__ void loss_of(float m, float w, float scale, float smo
     tail = tail * q + 1.0f / 5;
     tail = tail * q + 1.0f / 3;
     tail = 2.0f * t * (tail * q + 1.0f);
-    loss = scale * w * (tail + fmaxf(-m, 0.0f) * (1.0f - smoothing) + fmaxf(m, 0.0f) * smoothing);
+    const float down = smoothing < 1.0f ? fmaxf(-m, 0.0f) : 0.0f, up = smoothing > 0.0f ? fmaxf(m, 0.0f) : 0.0f;
+    loss = scale * w * (tail + down * (1.0f - smoothing) + up * smoothing);
     slope = scale * w * (smoothing - (m > 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e));      // sigmoid(-m)
     if (m != m) loss = slope = m;
 }

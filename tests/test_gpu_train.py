@@ -617,3 +617,29 @@ def test_recurrence_rows_written_past_the_caches(T, dtype, dim):
         close(name, got[name][n:], want[name], want[name + "_off"], dtype)
         assert not got[name][:n].any()
     close("ddecay", got["ddecay"], want["ddecay"], want["ddecay_off"])
+
+
+@pytest.mark.parametrize("dtype, dim", [(F32, 64), (BF16, 33), (F32, 600), (BF16, 2500)])
+@pytest.mark.parametrize("smoothing, sign", [(0.0, 1), (1.0, -1), (0.0, -1), (1.0, 1), (0.25, 1), (0.25, -1)])
+def test_pair_loss_infinite_margins(T, smoothing, sign, dtype, dim):
+    """A margin of infinity on the side whose factor is 0 adds nothing, on another side the loss is infinite; either way the gradients are the
+    limit's, and the other pairs' are their own."""
+    rng = np.random.default_rng(17)
+    B, K = 5, 7
+    a, p, n = values(rng, (B, dim), dtype), values(rng, (B, dim), dtype), values(rng, (B, K, dim), dtype)
+    ref = rng.standard_normal((B, K)).astype(np.float32)
+    far = rng.random((B, K)) < 0.3
+    far[3] = True
+    kw = dict(beta=1.0 / np.sqrt(dim), scale=1.0 / (B * K), smoothing=smoothing)
+    got = T.pair_loss(torch_of(a, dtype), torch_of(p, dtype), torch_of(n, dtype), ref=torch_of(np.where(far, np.float32(-sign * np.inf), ref)), **kw)
+    limit = O.pair_loss(a, p, n, ref=np.where(far, np.float32(-sign * 1e6), ref), **kw)      # (a margin of thousands: the slopes are 0 and 1)
+    assert np.abs(limit["margin"][far]).min() > 1000
+    for k in ("danchor", "dpos", "dneg"):
+        close(k, got[k], limit[k], limit[k + "_off"], dtype)
+    margin = got["margin"].cpu().numpy()
+    assert (margin[far] == sign * np.inf).all()
+    if smoothing == (0.0 if sign > 0 else 1.0):
+        near = O.pair_loss(a, p, n, ref=ref, weight=np.where(far, 0.0, 1.0), **kw)
+        close("loss", got["loss"], np.float64(near["loss"]), near["loss_off"])
+    else:
+        assert float(got["loss"]) == np.inf
