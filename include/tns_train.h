@@ -35,16 +35,17 @@ enum { TNS_F32 = 0, TNS_BF16 = 1 };
  *
  *   S, d_rowptr[S+1]  lists; d_rowptr[0] = 0, non-decreasing, as tns_run writes it.  S < 2^31
  *   rows              rows that the arrays have room for, at least d_rowptr[S]; rows from d_rowptr[S] on are
- *                     neither read nor written.  rows < 2^40
+ *                     neither read nor, without TNS_ZERO_BEYOND, written.  rows < 2^40
  *   dim, dtype        channels per row, 1 .. 2^16; TNS_F32 | TNS_BF16
  *   flags             TNS_NEWEST_FIRST: a list's first row is its newest event (tns_run's order under the
- *                     recent policy); otherwise its oldest
+ *                     recent policy); otherwise its oldest.  TNS_ZERO_BEYOND: the rows from d_rowptr[S] on of d_h, d_du
+ *                     and d_dx are written as zeros, so that they can be summed over without reading d_rowptr[S] back
  *   d_u, d_x          T [rows, dim], ld_u / ld_x elements from one row to the next (>= dim); aligned to T
  *   d_ts [rows], d_decay [dim]   both or neither; decay >= 0 (with a negative one the state grows, and what rows do
  *                     to a state, multiplied up over a long list, may overflow)
  *   d_h0 [S, dim], d_t0 [S]      may be NULL; d_t0 needs d_ts
  */
-enum { TNS_NEWEST_FIRST = 1 };
+enum { TNS_NEWEST_FIRST = 1, TNS_ZERO_BEYOND = 4 };
 typedef struct {
     int64_t S, rows;
     int32_t dim, dtype, flags, reserved; /* reserved: 0 */

@@ -74,9 +74,9 @@ struct Lists {
     int64_t ld_u, ld_x;
     const float *ts, *decay, *h0, *t0;
     int dim;
-    bool newest_first;
+    bool newest_first, zero_beyond;
 
-    __device__ int64_t total() const { return uniform(min(max(rowptr[S], (int64_t)0), rows)); }
+    __device__ int64_t total() const { return S ? uniform(min(max(rowptr[S], (int64_t)0), rows)) : 0; }
     __device__ int64_t begin_of(int64_t j, int64_t total) const {         // 0 <= j <= S
         const int64_t at = min(max(rowptr[newest_first ? S - j : j], (int64_t)0), total);
         return newest_first ? total - at : at;
@@ -641,6 +641,15 @@ __device__ void fill_empty(const Lists<T>& l, int64_t first, const float* from, 
     }
 }
 
+// Zeros in the rows of a tile that belong to no list (the tile's rows along memory: they lie behind the walk in either order).
+template <typename T, int V>
+__device__ void zero_rows(const Lists<T>& l, T* out, int64_t ld, int64_t begin, int64_t end, int64_t total, int c) {
+    end = min(end, l.rows);
+    for (int64_t p = max(begin, total); p < end; ++p)
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[p * ld + c + i] = T{};
+}
+
 // h = f h + z x along the rows of a tile, V channels a lane, 16 rows in registers and the next 16 on their way.  The list a row belongs to, and
 // the gap before it, lie in the lanes (64 rows at a time); what is the same for the wave (addresses, first and last rows) is the scalar
 // unit's.  Bound by memory: 0.79 M rows of 256 bf16 channels, all states written and saved, 1.23 GB in 223 us (5.5 TB/s); 0.80 M rows of
@@ -662,6 +671,7 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
     const Entering<V> entering(t, tile, l.dim, c);
     const uint32_t known = tile ? t.list[tile] : 0u;
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
+    if (l.zero_beyond && h_out) zero_rows<T, V>(l, h_out, ld_h, begin, begin + t.tile_rows, total, c);
     if (begin >= end) return;
     Pack<T, V> u[kSaved], x[kSaved];
     const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total);
@@ -742,6 +752,10 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
     const int c = channel_of<V>(l.dim, share.block);
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
     float sum[V] = {};
+    if (l.zero_beyond && tile >= 0) {
+        zero_rows<T, V>(l, du, ld_du, begin, begin + t.tile_rows, total, c);
+        zero_rows<T, V>(l, dx, ld_dx, begin, begin + t.tile_rows, total, c);
+    }
     if (tile >= 0 && begin < end) {         // (and so tile < t.tiles)
         const Entering<V> entering(t, tile, l.dim, c);
         const uint32_t known = end < total ? t.list[tile] : 0u;
@@ -921,7 +935,7 @@ int check(const tns_recur* r) {
     if (r->S > (int64_t)INT32_MAX || r->rows > (int64_t)1 << 40) return fail(TNS_ESIZE, "more than 2^31-1 lists or 2^40 rows");
     if (r->dim < 1 || r->dim > 1 << 16) return fail(TNS_EINVAL, "dim must be in [1, 2^16]");
     if (r->dtype != TNS_F32 && r->dtype != TNS_BF16) return fail(TNS_EINVAL, "unknown dtype");
-    if ((r->flags & ~TNS_NEWEST_FIRST) || r->reserved) return fail(TNS_EINVAL, "unknown flag");
+    if ((r->flags & ~(TNS_NEWEST_FIRST | TNS_ZERO_BEYOND)) || r->reserved) return fail(TNS_EINVAL, "unknown flag");
     return TNS_OK;
 }
 
@@ -993,7 +1007,7 @@ size_t saved_bytes(const tns_recur& r) { return (size_t)((r.rows + kSaved - 1) /
 template <typename T>
 Lists<T> typed(const tns_recur& r) {
     return {r.S, r.rows, r.d_rowptr, static_cast<const T*>(r.d_u), static_cast<const T*>(r.d_x), r.ld_u, r.ld_x,
-            r.d_ts, r.d_decay, r.d_h0, r.d_t0, r.dim, (r.flags & TNS_NEWEST_FIRST) != 0};
+            r.d_ts, r.d_decay, r.d_h0, r.d_t0, r.dim, (r.flags & TNS_NEWEST_FIRST) != 0, (r.flags & TNS_ZERO_BEYOND) != 0};
 }
 
 // Workgroups: of the kernels with one for every four tiles and block of channels, and every 256 lists where `lists` is set.
@@ -1100,7 +1114,7 @@ int tns_recur_run(const tns_recur* r, void* d_h, int64_t ld_h, float* d_h_last, 
     if (d_h && ld_h < r->dim) return fail(TNS_EINVAL, "rows of h overlap");
     if (misaligned(d_saved, 256)) return fail(TNS_EINVAL, "saved states must be 256-byte aligned");
     if (int e = check_workspace(d_workspace, workspace_bytes, carve(*r, nullptr).bytes)) return e;
-    if (r->S == 0) return TNS_OK;
+    if (r->S == 0 && !(r->flags & TNS_ZERO_BEYOND)) return TNS_OK;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     choose(*r, ld_h % 2 == 0 && !misaligned(d_h, 4), [&](auto value, auto v, auto decay) {
         launch_run<decltype(value), v(), decay()>(*r, d_h, ld_h, d_h_last, d_saved, d_workspace, stream);
@@ -1118,7 +1132,7 @@ int tns_recur_grad(const tns_recur* r, const void* d_saved, const void* d_dh, in
     if (d_ddecay && !r->d_decay) return fail(TNS_EINVAL, "gradient of a decay that is not there");
     if (int e = check_workspace(d_workspace, workspace_bytes, carve(*r, nullptr).bytes)) return e;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (r->S == 0) {
+    if (r->S == 0 && !(r->flags & TNS_ZERO_BEYOND)) {
         if (d_ddecay) hipLaunchKernelGGL(k_recur_sums, dim3((r->dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, nullptr, 0, r->dim, d_ddecay);
         return launched("tns_recur_grad");
     }

@@ -11,7 +11,7 @@ import functools
 from .binding import TnsError, _check, lib as _lib  # noqa: F401
 
 TNS_F32, TNS_BF16 = 0, 1
-TNS_NEWEST_FIRST = 1
+TNS_NEWEST_FIRST, TNS_ZERO_BEYOND = 1, 4
 ADAMW_BLOCK = 256          # weights that share a scale of a state in 8 bits
 EXPORTS = ["tns_recur_workspace", "tns_recur_run", "tns_recur_grad", "tns_recur_step", "tns_pair_loss_workspace", "tns_pair_loss",
            "tns_adamw_create", "tns_adamw_step", "tns_adamw_destroy"]
@@ -185,10 +185,11 @@ def _lists(rowptr, u, x, ts, decay, h0, t0, newest_first):
 
 def recur_run(rowptr, u, x, ts=None, decay=None, h0=None, t0=None, newest_first=False, states=True, save=False) -> dict:
     """The recurrence over the lists of ``rowptr`` (tns_recur_run): ``h`` (None without ``states``), ``last`` and, with ``save``,
-    what recur_grad needs (``saved``)."""
+    what recur_grad needs (``saved``).  u and x may have more rows than the lists hold: those of ``h`` are zero."""
     import torch
     on, stream = _on(u)
     r = _lists(rowptr, u, x, ts, decay, h0, t0, newest_first)
+    r.flags |= TNS_ZERO_BEYOND
     run, _, saved = _recur_bytes(r.S, r.rows, r.dim, r.dtype)
     out = dict(h=u.new_empty((r.rows, r.dim)) if states else None, last=u.new_empty((r.S, r.dim), dtype=torch.float32),
                saved=u.new_empty(saved, dtype=torch.uint8) if save else None)
@@ -200,10 +201,12 @@ def recur_run(rowptr, u, x, ts=None, decay=None, h0=None, t0=None, newest_first=
 
 def recur_grad(rowptr, u, x, saved, ts=None, decay=None, h0=None, t0=None, newest_first=False, dh=None, dlast=None) -> dict:
     """Gradients ``du``, ``dx``, ``ddecay`` (None without decay) and ``dh0`` (None without h0), given those by the states (``dh``)
-    and by the last states (``dlast``); the other arguments as given to recur_run, ``saved`` from its result."""
+    and by the last states (``dlast``); the other arguments as given to recur_run, ``saved`` from its result.  Rows of du and dx that
+    no list holds are zero."""
     import torch
     on, stream = _on(u)
     r = _lists(rowptr, u, x, ts, decay, h0, t0, newest_first)
+    r.flags |= TNS_ZERO_BEYOND
     _, grad, size = _recur_bytes(r.S, r.rows, r.dim, r.dtype)
     if saved is None:
         raise ValueError("saved: recur_run(save=True) returns it")

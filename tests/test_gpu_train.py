@@ -643,3 +643,47 @@ def test_pair_loss_infinite_margins(T, smoothing, sign, dtype, dim):
         close("loss", got["loss"], np.float64(near["loss"]), near["loss_off"])
     else:
         assert float(got["loss"]) == np.inf
+
+
+@pytest.mark.parametrize("newest_first", [False, True])
+@pytest.mark.parametrize("lens", [[], [0, 0], [3, 0, 10, 1], RAGGED], ids=["no_list", "empty_lists", "few", "ragged"])
+@pytest.mark.parametrize("dtype, dim, more", [(F32, 33, 1), (F32, 100, 700), (BF16, 128, 64), (BF16, 70, 5000), (BF16, 300, 31)])
+def test_recurrence_rows_of_no_list_are_zero(T, dtype, dim, more, lens, newest_first):
+    """u and x with more rows than the lists hold: h, du and dx are zero there, whatever lay in their memory, and the products that make the
+    gradients of weights can be taken over all rows."""
+    import torch
+    rng = np.random.default_rng(18)
+    a = the_lists(rng, lens, dim, dtype, True, False)
+    n = a["u"].shape[0]
+    dlast, dh = values(rng, (len(lens), dim), F32), values(rng, (n + more, dim), dtype)
+    want = O.recurrence(**a, newest_first=newest_first, dlast=dlast, dh=dh[:n])
+    g = on_gpu(a, dtype)
+    nan = lambda *s: torch.full(s, float("nan"), device="cuda")      # noqa: E731
+    for k in ("u", "x"):
+        g[k] = torch.cat((g[k], nan(more, dim).to(g[k].dtype)))
+    g["ts"] = torch.cat((g["ts"], nan(more)))
+    stale = [nan(n + more, dim).to(g["u"].dtype) for _ in range(8)]      # memory that the outputs are likely to get
+    del stale
+    r = T.recur_run(**g, newest_first=newest_first, save=True)
+    stale = [nan(n + more, dim).to(g["u"].dtype) for _ in range(8)]
+    del stale
+    got = T.recur_grad(**g, saved=r["saved"], newest_first=newest_first, dlast=torch_of(dlast), dh=torch_of(dh, dtype))
+    for k, v in (("h", r["h"]), ("du", got["du"]), ("dx", got["dx"])):
+        assert not v[n:].any(), k
+        close(k, v[:n], want[k][:n], want[k + "_off"][:n], dtype)
+        total, off = want[k].sum(0), want[k + "_off"].sum(0) + (n + 1) * 2.0 ** -24 * np.abs(want[k]).sum(0)
+        if dtype == F32:
+            close(f"sum of {k}", v.sum(0), total, off)
+        else:
+            assert bool(torch.isfinite(v.float().sum(0)).all())
+    close("ddecay", got["ddecay"], want["ddecay"], want["ddecay_off"])
+    # through the C interface, between guards
+    desc = T._lists(g["rowptr"], g["u"], g["x"], g["ts"], g["decay"], None, None, newest_first)
+    desc.flags |= T.TNS_ZERO_BEYOND
+    ld, rows = dim + 3, n + more
+    out = torch.full((rows * ld + 40,), 7.0, dtype=g["u"].dtype, device="cuda")
+    work = torch.empty(T.tns_recur_workspace(desc)[0], dtype=torch.uint8, device="cuda")
+    T.tns_recur_run(desc, out.data_ptr(), ld, 0, 0, work.data_ptr(), work.numel(), torch.cuda.current_stream().cuda_stream)
+    inside = out[: rows * ld].view(rows, ld)
+    assert not inside[n:, :dim].any() and bool((inside[:, dim:] == 7).all()) and bool((out[rows * ld:] == 7).all())
+    close("h", inside[:n, :dim], want["h"][:n], want["h_off"][:n], dtype)
