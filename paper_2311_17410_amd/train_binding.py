@@ -17,6 +17,7 @@ EXPORTS = ["tns_recur_workspace", "tns_recur_run", "tns_recur_grad", "tns_recur_
            "tns_adamw_create", "tns_adamw_step", "tns_adamw_destroy"]
 
 _vp, _i64, _i32, _f64 = C.c_void_p, C.c_int64, C.c_int32, C.c_double
+_at = C.c_size_t           # a device address or a stream: an integer (a c_void_p argument would take bytes, strings and arrays, as addresses of host memory)
 
 
 class tns_recur(C.Structure):
@@ -48,13 +49,13 @@ def lib():
     if not _ready:
         size_p = C.POINTER(C.c_size_t)
         L.tns_recur_workspace.argtypes = [C.POINTER(tns_recur), size_p, size_p, size_p]
-        L.tns_recur_run.argtypes = [C.POINTER(tns_recur), _vp, _i64, _vp, _vp, _vp, C.c_size_t, _vp]
-        L.tns_recur_grad.argtypes = [C.POINTER(tns_recur), _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, C.c_size_t, _vp]
-        L.tns_recur_step.argtypes = [_i64, _i64, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]
+        L.tns_recur_run.argtypes = [C.POINTER(tns_recur), _at, _i64, _at, _at, _at, C.c_size_t, _at]
+        L.tns_recur_grad.argtypes = [C.POINTER(tns_recur), _at, _at, _i64, _at, _at, _i64, _at, _i64, _at, _at, _at, C.c_size_t, _at]
+        L.tns_recur_step.argtypes = [_i64, _i64, _i32, _i32, _at, _at, _i64, _at, _i64, _at, _at, _at, _at, _at, _i64, _at]
         L.tns_pair_loss_workspace.argtypes = [_i64, _i64, _i32, size_p]
-        L.tns_pair_loss.argtypes = [C.POINTER(tns_pairs), _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]
+        L.tns_pair_loss.argtypes = [C.POINTER(tns_pairs), _at, _at, _at, _at, _at, _at, C.c_size_t, _at]
         L.tns_adamw_create.argtypes = [C.POINTER(tns_adamw_config), _i32, C.POINTER(tns_adamw_tensor), C.POINTER(_vp)]
-        L.tns_adamw_step.argtypes = [_vp, _f64, _i64, _vp, _vp]
+        L.tns_adamw_step.argtypes = [_vp, _f64, _i64, _at, _at]
         L.tns_adamw_destroy.argtypes = [_vp]
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
@@ -72,20 +73,20 @@ def tns_recur_workspace(r: tns_recur):
 
 
 def tns_recur_run(r: tns_recur, d_h, ld_h: int, d_h_last, d_saved, d_workspace, workspace_bytes: int, hip_stream: int = 0) -> None:
-    _check(lib().tns_recur_run(C.byref(r), d_h or None, ld_h, d_h_last or None, d_saved or None, d_workspace or None, workspace_bytes, hip_stream or None),
+    _check(lib().tns_recur_run(C.byref(r), d_h or 0, ld_h, d_h_last or 0, d_saved or 0, d_workspace or 0, workspace_bytes, hip_stream or 0),
            "tns_recur_run")
 
 
 def tns_recur_grad(r: tns_recur, d_saved, d_dh, ld_dh: int, d_dh_last, d_du, ld_du: int, d_dx, ld_dx: int, d_ddecay, d_dh0, d_workspace,
                    workspace_bytes: int, hip_stream: int = 0) -> None:
-    _check(lib().tns_recur_grad(C.byref(r), d_saved or None, d_dh or None, ld_dh, d_dh_last or None, d_du or None, ld_du, d_dx or None, ld_dx,
-                                d_ddecay or None, d_dh0 or None, d_workspace or None, workspace_bytes, hip_stream or None), "tns_recur_grad")
+    _check(lib().tns_recur_grad(C.byref(r), d_saved or 0, d_dh or 0, ld_dh, d_dh_last or 0, d_du or 0, ld_du, d_dx or 0, ld_dx,
+                                d_ddecay or 0, d_dh0 or 0, d_workspace or 0, workspace_bytes, hip_stream or 0), "tns_recur_grad")
 
 
 def tns_recur_step(B: int, num_ids: int, dim: int, dtype: int, d_ids, d_u, ld_u: int, d_x, ld_x: int, d_ts, d_decay, d_state, d_state_ts, d_out,
                    ld_out: int, hip_stream: int = 0) -> None:
-    _check(lib().tns_recur_step(B, num_ids, dim, dtype, d_ids or None, d_u or None, ld_u, d_x or None, ld_x, d_ts or None, d_decay or None,
-                                d_state or None, d_state_ts or None, d_out or None, ld_out, hip_stream or None), "tns_recur_step")
+    _check(lib().tns_recur_step(B, num_ids, dim, dtype, d_ids or 0, d_u or 0, ld_u, d_x or 0, ld_x, d_ts or 0, d_decay or 0,
+                                d_state or 0, d_state_ts or 0, d_out or 0, ld_out, hip_stream or 0), "tns_recur_step")
 
 
 def tns_pair_loss_workspace(B: int, K: int, dim: int) -> int:
@@ -95,8 +96,8 @@ def tns_pair_loss_workspace(B: int, K: int, dim: int) -> int:
 
 
 def tns_pair_loss(p: tns_pairs, d_loss, d_margin, d_danchor, d_dpos, d_dneg, d_workspace, workspace_bytes: int, hip_stream: int = 0) -> None:
-    _check(lib().tns_pair_loss(C.byref(p), d_loss or None, d_margin or None, d_danchor or None, d_dpos or None, d_dneg or None, d_workspace or None,
-                               workspace_bytes, hip_stream or None), "tns_pair_loss")
+    _check(lib().tns_pair_loss(C.byref(p), d_loss or 0, d_margin or 0, d_danchor or 0, d_dpos or 0, d_dneg or 0, d_workspace or 0,
+                               workspace_bytes, hip_stream or 0), "tns_pair_loss")
 
 
 def tns_adamw_create(cfg: tns_adamw_config, tensors):
@@ -107,7 +108,7 @@ def tns_adamw_create(cfg: tns_adamw_config, tensors):
 
 
 def tns_adamw_step(opt, lr: float, t: int, d_grad_scale=None, hip_stream: int = 0) -> None:
-    _check(lib().tns_adamw_step(opt, lr, t, d_grad_scale or None, hip_stream or None), "tns_adamw_step")
+    _check(lib().tns_adamw_step(opt, lr, t, d_grad_scale or 0, hip_stream or 0), "tns_adamw_step")
 
 
 def tns_adamw_destroy(opt) -> None:

@@ -208,3 +208,39 @@ p.close()
 fake.fake_fail_synchronize(0)
 assert fake.fake_host_blocks() == 0 and fake.fake_used() == 0
 """)
+
+
+def test_device_addresses_of_the_training_operators_are_integers(run):
+    run("""
+from paper_2311_17410_amd import train_binding as T
+r = T.tns_recur(2, 4, 8, 0, 0, 0, 256, 256, 256, 8, 8, 256, 256, None, None)
+p = T.tns_pairs(2, 3, 8, 0, 256, 256, 256, 8, 8, None, None, 1.0, 0.0, 1.0)
+opt = T.tns_adamw_create(T.tns_adamw_config(0.9, 0.999, 1e-8, 0, 32, 0, 0, 0), [T.tns_adamw_tensor(5, 256, None, 256, 256, 256, None, None, 0.0)])
+calls = [(T.tns_recur_run, [r, 256, 8, 256, 256, 256, 1 << 30, 0], (1, 3, 4, 5, 7)),
+         (T.tns_recur_grad, [r, 256, 256, 8, 256, 256, 8, 256, 8, 256, 256, 256, 1 << 30, 0], (1, 2, 4, 5, 7, 9, 10, 11, 13)),
+         (T.tns_recur_step, [2, 4, 8, 0, 256, 256, 8, 256, 8, 256, 256, 256, 256, 256, 8, 0], (4, 5, 7, 9, 10, 11, 12, 13, 15)),
+         (T.tns_pair_loss, [p, 256, 256, 256, 256, 256, 256, 1 << 30, 0], (1, 2, 3, 4, 5, 6, 8)),
+         (T.tns_adamw_step, [opt, 1e-3, 1, 256, 0], (3, 4))]
+for call, args, addresses in calls:
+    n = fake.fake_launches()
+    call(*args)
+    assert fake.fake_launches() > n
+    for i in addresses:
+        for other in (b"12345678", "12345678", C.create_string_buffer(8), C.c_void_p(256), (C.c_int64 * 2)(1, 2), 1.5):
+            try:
+                call(*args[:i], other, *args[i + 1:])
+            except (TypeError, C.ArgumentError):
+                continue
+            raise SystemExit(f"{call.__name__} takes {other!r} as argument {i}")
+T.tns_recur_run(r, None, 8, 256, None, 256, 1 << 30, None)      # NULL either way
+T.tns_adamw_step(opt, 1e-3, 1, None, None)
+for kind in (T.tns_recur, T.tns_pairs, T.tns_adamw_tensor):
+    for name in [n for n, _ in kind._fields_ if n.startswith("d_")]:
+        for other in (b"12345678", "12345678", C.create_string_buffer(8)):
+            try:
+                kind(**{name: other})
+            except TypeError:
+                continue
+            raise SystemExit(f"{kind.__name__}.{name} takes {other!r}")
+T.tns_adamw_destroy(opt)
+""")
