@@ -2,6 +2,8 @@
 
 The functions without the prefix take torch tensors: they check them, allocate what they return on the tensors' device and
 enqueue on its current stream.  Strides other than those of the last dimension are free where the C interface has them.
+They record nothing for autograd, and so refuse tensors that require gradients while it records (a torch.autograd.Function of the
+caller's may call them); what they change in place (a state table, weights) has its version raised, as by an operation of torch.
 """
 from __future__ import annotations
 
@@ -117,6 +119,15 @@ def tns_adamw_destroy(opt) -> None:
 
 # ---- the same on torch tensors ---------------------------------------------------------------------
 
+def _unrecorded(*tensors):
+    """Refuses what autograd would have to follow: the results would look like constants to it."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            import torch
+            if torch.is_grad_enabled():
+                raise ValueError("nothing is recorded for autograd here: call under torch.no_grad(), within a torch.autograd.Function, or on detached tensors")
+
+
 def _dtype_of(t):
     import torch
     if t.dtype is torch.float32:
@@ -188,6 +199,7 @@ def recur_run(rowptr, u, x, ts=None, decay=None, h0=None, t0=None, newest_first=
     """The recurrence over the lists of ``rowptr`` (tns_recur_run): ``h`` (None without ``states``), ``last`` and, with ``save``,
     what recur_grad needs (``saved``).  u and x may have more rows than the lists hold: those of ``h`` are zero."""
     import torch
+    _unrecorded(u, x, ts, decay, h0, t0)
     on, stream = _on(u)
     r = _lists(rowptr, u, x, ts, decay, h0, t0, newest_first)
     r.flags |= TNS_ZERO_BEYOND
@@ -205,6 +217,7 @@ def recur_grad(rowptr, u, x, saved, ts=None, decay=None, h0=None, t0=None, newes
     and by the last states (``dlast``); the other arguments as given to recur_run, ``saved`` from its result.  Rows of du and dx that
     no list holds are zero."""
     import torch
+    _unrecorded(u, x, ts, decay, h0, t0, dh, dlast)
     on, stream = _on(u)
     r = _lists(rowptr, u, x, ts, decay, h0, t0, newest_first)
     r.flags |= TNS_ZERO_BEYOND
@@ -228,6 +241,7 @@ def recur_step(ids, u, x, state, ts=None, decay=None, state_ts=None):
     """One event for each node of ``ids`` (int32, distinct): changes ``state`` (and ``state_ts``) in place, returns the new states
     in u's type, zero for ids that hold none."""
     import torch
+    _unrecorded(u, x, state, ts, decay, state_ts)
     on, stream = _on(u)
     if u.dim() != 2 or state.dim() != 2:
         raise ValueError("u has the shape [events, dim], state [nodes, dim]")
@@ -240,6 +254,7 @@ def recur_step(ids, u, x, state, ts=None, decay=None, state_ts=None):
             _want("state", state, (n, dim), f32, dev), _want("state_ts", state_ts, (n,), f32, dev))
     with on:
         tns_recur_step(B, n, dim, dtype, *args, out.data_ptr(), dim, stream)
+    torch.autograd.graph.increment_version([state] if state_ts is None else [state, state_ts])
     return out
 
 
@@ -247,6 +262,7 @@ def pair_loss(anchor, pos, neg, ref=None, weight=None, beta=1.0, smoothing=0.0, 
     """Paired log-ratio loss (tns_pair_loss): ``loss`` (a scalar tensor), ``margin`` [B, K] and the gradients ``danchor``, ``dpos``,
     ``dneg`` (None without ``grads``)."""
     import torch
+    _unrecorded(anchor, pos, neg, ref, weight)
     on, stream = _on(anchor)
     if neg.dim() != 3:
         raise ValueError("neg has the shape [events, links, dim]")
@@ -296,6 +312,8 @@ class AdamW:
                                           at("m_scale", self.m_scale, torch.float32, scales), at("v_scale", self.v_scale, torch.float32, scales), decays[i]))
         cfg = tns_adamw_config(betas[0], betas[1], eps, seed & (1 << 64) - 1, bits, _dtype_of(grads[0]), dev.index, 0)
         self._device = dev
+        changed = [t for many in (params, copies, self.m, self.v, self.m_scale, self.v_scale) if many is not None for t in many]
+        self._changed = list({id(t if t._base is None else t._base): t for t in changed}.values())      # (views of one tensor have one version)
         self._h = tns_adamw_create(cfg, table)
 
     def step(self, lr, t, grad_scale=None):
@@ -303,6 +321,7 @@ class AdamW:
         import torch
         scale = 0 if grad_scale is None else _want("grad_scale", grad_scale.reshape(-1), (1,), torch.float32, self._device)
         tns_adamw_step(self._h, lr, t, scale, torch.cuda.current_stream(self._device).cuda_stream)
+        torch.autograd.graph.increment_version(self._changed)
 
     def close(self):
         if getattr(self, "_h", None):

@@ -687,3 +687,55 @@ def test_recurrence_rows_of_no_list_are_zero(T, dtype, dim, more, lens, newest_f
     inside = out[: rows * ld].view(rows, ld)
     assert not inside[n:, :dim].any() and bool((inside[:, dim:] == 7).all()) and bool((out[rows * ld:] == 7).all())
     close("h", inside[:n, :dim], want["h"][:n], want["h_off"][:n], dtype)
+
+
+def test_within_autograd(T):
+    """A Function of the caller's around the operators; what they change in place is noticed by a graph that kept it."""
+    import torch
+    rng = np.random.default_rng(19)
+    a = the_lists(rng, [5, 0, 9], 12, F32, True, False)
+    g = on_gpu(a, F32)
+
+    class Last(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, u, x, decay):
+            r = T.recur_run(g["rowptr"], u, x, ts=g["ts"], decay=decay, save=True)
+            ctx.save_for_backward(u, x, decay, r["saved"])
+            return r["last"]
+
+        @staticmethod
+        def backward(ctx, dlast):
+            u, x, decay, saved = ctx.saved_tensors
+            d = T.recur_grad(g["rowptr"], u, x, saved, ts=g["ts"], decay=decay, dlast=dlast.contiguous())
+            return d["du"], d["dx"], d["ddecay"]
+
+    leaves = [g[k].requires_grad_() for k in ("u", "x", "decay")]
+    dlast = values(rng, (3, 12), F32)
+    (Last.apply(*leaves) * torch_of(dlast)).sum().backward()
+    want = O.recurrence(**a, dlast=dlast)
+    for t, k in zip(leaves, ("du", "dx", "ddecay")):
+        close(k, t.grad, want[k], want[k + "_off"])
+    with pytest.raises(ValueError, match="autograd"):
+        T.recur_run(g["rowptr"], *leaves[:2])
+
+    ids, state, state_ts = torch.arange(3, dtype=torch.int32, device="cuda"), torch.zeros((3, 12), device="cuda"), torch.zeros(3, device="cuda")
+    one, ts, x = torch.ones((3, 12), device="cuda"), torch.ones(3, device="cuda"), torch.ones((3, 12), device="cuda", requires_grad=True)
+    kept = x * state
+    versions = state._version, state_ts._version
+    T.recur_step(ids, one, one, state, ts, torch.ones(12, device="cuda"), state_ts)
+    assert state._version > versions[0] and state_ts._version > versions[1]
+    with pytest.raises(RuntimeError, match="inplace"):
+        kept.sum().backward()
+
+    w = torch.ones(12, device="cuda", requires_grad=True)
+    for bits in (32, 8):
+        copy = torch.zeros(12, dtype=torch.bfloat16, device="cuda")
+        opt = T.AdamW([w], [torch.ones(12, device="cuda")], copies=[copy], bits=bits)
+        changed = [w, copy, opt.m[0], opt.v[0]] + ([opt.m_scale[0], opt.v_scale[0]] if bits == 8 else [])
+        versions = [t._version for t in changed]
+        kept = (x * w).sum()
+        opt.step(1e-3, 1)
+        assert all(t._version > v for t, v in zip(changed, versions))
+        with pytest.raises(RuntimeError, match="inplace"):
+            kept.backward()
+        opt.close()

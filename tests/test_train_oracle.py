@@ -234,3 +234,18 @@ def test_tensors_off_the_gpu_are_refused():
                  lambda: T.pair_loss(v, v, torch.zeros(4, 1, 8)), lambda: T.AdamW([v], [v])):
         with pytest.raises(ValueError):
             call()
+
+
+def test_tensors_that_require_gradients_are_refused():
+    """Results that autograd takes for constants are no results for a caller who relies on it (off the GPU: it is looked at first)."""
+    import torch
+    rp, ids = torch.zeros(2, dtype=torch.int64), torch.zeros(4, dtype=torch.int32)
+    v, g, d, t, many = torch.zeros(4, 8), torch.zeros(4, 8, requires_grad=True), torch.zeros(8, requires_grad=True), torch.zeros(4), torch.zeros(4, 1, 8)
+    calls = [lambda: T.recur_run(rp, g, v), lambda: T.recur_run(rp, v, g), lambda: T.recur_run(rp, v, v, ts=t, decay=d), lambda: T.recur_run(rp, v, v, h0=g[:1]),
+             lambda: T.recur_grad(rp, g, v, v), lambda: T.recur_grad(rp, v, v, v, dh=g), lambda: T.recur_step(ids, g, v, v), lambda: T.recur_step(ids, v, v, g),
+             lambda: T.pair_loss(g, v, many), lambda: T.pair_loss(v, g, many), lambda: T.pair_loss(v, v, g[:, None]), lambda: T.pair_loss(v, v, many, weight=g[:, :1])]
+    for call in calls:
+        with pytest.raises(ValueError, match="autograd"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):
+            call()
