@@ -79,6 +79,72 @@ def recurrence(rowptr, u, x, ts=None, decay=None, h0=None, t0=None, newest_first
     return out
 
 
+def scan(a, b):
+    """h_i = a_i h_{i-1} + b_i along the first axis, in log2(rows) rounds."""
+    by = 1
+    while by < len(b):
+        b = np.concatenate((b[:by], b[by:] + a[by:] * b[:-by]))
+        a = np.concatenate((a[:by], a[by:] * a[:-by]))
+        by *= 2
+    return b
+
+
+def recurrence_scanned(rowptr, u, x, ts=None, decay=None, h0=None, t0=None, newest_first=False, dh=None, dlast=None, change=None):
+    """What recurrence() returns, for lists of many rows: all rows at once, by scans.  Times have to be finite and every list has to hold a row.
+    change(f): what a test has a mistake in the factors do (f in the order of the walk)."""
+    rowptr = np.asarray(rowptr, np.int64)
+    S, n = len(rowptr) - 1, int(rowptr[-1])
+    assert (rowptr[1:] > rowptr[:-1]).all()
+    flip = (lambda v: v[::-1]) if newest_first else (lambda v: v)
+    seq = flip(np.repeat(np.arange(S), np.diff(rowptr)))
+    u, x = (flip(v.astype(np.float64)) for v in (u, x))
+    first, last = (np.concatenate(([True], seq[1:] != seq[:-1]))[:, None], np.concatenate((seq[1:] != seq[:-1], [True]))[:, None])
+    gap, lam = np.zeros((n, 1)), np.zeros(u.shape[1]) if decay is None else decay.astype(np.float64)
+    if ts is not None:
+        t = flip(ts.astype(np.float32))
+        before = np.where(first[:, 0], t if t0 is None else t0.astype(np.float32)[seq], np.concatenate((t[:1], t[:-1])))
+        gap = np.maximum(t - before, np.float32(0)).astype(np.float64)[:, None]
+    at_first = np.zeros((n, u.shape[1])) if h0 is None else h0.astype(np.float64)[seq]
+    z, rest = sigmoid(u), sigmoid(-u)
+    f = rest * np.exp(-lam * gap)
+    if change is not None:
+        f = change(f)
+    ez = (1.5 * np.abs(u) + 6) * U
+    ef = ez + (3.5 * np.minimum(lam * gap, 200.0) + 3) * U
+    inner = np.where(first, 0.0, f)
+    shifted = lambda v: np.concatenate((v[:1], v[:-1]))      # noqa: E731
+    h = scan(inner, z * x + np.where(first, f * at_first, 0.0))
+    enters = np.where(first, at_first, shifted(h))
+    off = scan(inner, (ef + 4 * U) * f * np.abs(enters) + (ez + 4 * U) * z * np.abs(x))
+    enters_off = np.where(first, 0.0, shifted(off))
+    out = dict(h=flip(h), h_off=flip(2 * off))
+    ends, begins = np.flatnonzero(last[:, 0]), np.flatnonzero(first[:, 0])
+    for name, v in (("last", h), ("last_off", 2 * off)):
+        out[name] = np.zeros((S, u.shape[1]))
+        out[name][seq[ends]] = v[ends]
+    if dh is None and dlast is None:
+        return out
+    d = np.zeros(u.shape) if dh is None else flip(dh.astype(np.float64))
+    end = np.zeros(u.shape) if dlast is None else np.where(last, dlast.astype(np.float64)[seq], 0.0)
+    after = lambda v: np.concatenate((v[1:], v[:1]))         # noqa: E731
+    back = np.where(last, 0.0, after(f))
+    g = scan(back[::-1], (d + end)[::-1])[::-1]
+    sent = np.where(last, end, after(f * g))                 # what comes to a row from behind it
+    sent_off = np.where(last, 0.0, after((ef + 4 * U) * np.abs(f * g)))
+    off = scan(back[::-1], (sent_off + (0 if dh is None else U * (np.abs(sent) + np.abs(d))))[::-1])[::-1]
+    a, b = rest * x, f * enters
+    out["dx"], out["dx_off"] = flip(z * g), flip(2 * (z * off + (ez + 2 * U) * np.abs(z * g)))
+    out["du"] = flip(z * g * (a - b))
+    out["du_off"] = flip(2 * (z * off * (np.abs(a) + np.abs(b)) + np.abs(z * g) * ((2 * ez + 6 * U) * np.abs(a) + (ez + ef + 6 * U) * np.abs(b) + f * enters_off)))
+    term = g * b * gap
+    out["ddecay"] = -term.sum(0)
+    out["ddecay_off"] = 2 * (((ef + 4 * U) * np.abs(term) + gap * f * (np.abs(g) * enters_off + off * np.abs(enters))).sum(0) + n * U * np.abs(term).sum(0))
+    for name, v in (("dh0", f * g), ("dh0_off", 2 * (f * off + (ef + 4 * U) * np.abs(f * g)))):
+        out[name] = np.zeros((S, u.shape[1]))
+        out[name][seq[begins]] = v[begins]
+    return out
+
+
 def step(ids, u, x, state, ts=None, decay=None, state_ts=None):
     """(out, out_off, state, state_off, state_ts) after one event for each id."""
     out, off = np.zeros(u.shape), np.zeros(u.shape)

@@ -249,3 +249,63 @@ def test_tensors_that_require_gradients_are_refused():
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):
             call()
+
+
+LONG = {"one": [900], "cut": [300, 1, 70, 2, 256, 40, 1, 1, 230]}
+
+
+def slow(rng, lens, dim, decay=True, start=True):
+    """Gates and decays that carry a state over thousands of rows."""
+    a = lists(rng, lens, dim, decay, start)
+    a["u"] = (a["u"] - 8).astype(np.float32)
+    a["x"] = a["x"].astype(np.float32)
+    if decay:
+        a.update(decay=np.float32(rng.uniform(0, 2e-4, dim)), ts=np.float32(np.cumsum(rng.uniform(0, 2, len(a["u"])))))
+    if start:
+        a.update(h0=a["h0"].astype(np.float32))
+    return a
+
+
+@pytest.mark.parametrize("newest_first", [False, True])
+@pytest.mark.parametrize("decay, start, both", [(True, True, True), (False, True, False), (True, False, True), (False, False, False)])
+@pytest.mark.parametrize("lens", list(LONG))
+def test_recurrence_by_scans_is_the_same(lens, decay, start, both, newest_first):
+    rng = np.random.default_rng(20)
+    a = slow(rng, LONG[lens], 3, decay, start)
+    kw = dict(newest_first=newest_first, dh=rng.normal(size=a["u"].shape) if both else None, dlast=rng.normal(size=(len(LONG[lens]), 3)))
+    want, got = O.recurrence(**a, **kw), O.recurrence_scanned(**a, **kw)
+    for k, v in want.items():
+        if (decay or not k.startswith("ddecay")) and (start or not k.startswith("dh0")):
+            assert np.allclose(got[k], v, rtol=1e-9, atol=1e-12 * max(np.abs(v).max(), 1e-30)), k
+
+
+@pytest.mark.parametrize("newest_first", [False, True])
+@pytest.mark.parametrize("span, rows", [(256, 4000), (512, 9000)])
+def test_a_lost_or_repeated_carry_is_far_outside_the_bounds(span, rows, newest_first):
+    """Mistakes that a join of spans can make, in the factors of the 64-bit form: a carry lost at a border, a span's factor left out, one taken
+    twice.  Each is seen in the states and in the rows' gradients (the decay's is a sum over all rows, in whose bound one span hardly counts)."""
+    rng = np.random.default_rng(21)
+    a = slow(rng, [rows], 2)
+    kw = dict(newest_first=newest_first, dh=rng.normal(size=a["u"].shape), dlast=rng.normal(size=(1, 2)))
+    want = O.recurrence_scanned(**a, **kw)
+    at = rows // 2 // span * span
+
+    def lost(f):
+        f = f.copy()
+        f[at] = 0
+        return f
+
+    def left_out(f):
+        f = f.copy()
+        f[at] /= f[at: at + span].prod(0)
+        return f
+
+    def twice(f):
+        f = f.copy()
+        f[at] *= f[at: at + span].prod(0)
+        return f
+
+    for mistake in (lost, left_out, twice):
+        bad = O.recurrence_scanned(**a, **kw, change=mistake)
+        for k in ("h", "dx", "du"):
+            assert (np.abs(bad[k] - want[k]) > 4 * want[k + "_off"]).any(), (mistake.__name__, k)
