@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kWave = 64, kWaves = 4;  // lanes of a wave, waves of a workgroup
 constexpr int kSaved = 16;             // rows from one saved state to the next, and rows that a wave has in its registers
-constexpr int kBatch = 64;             // rows whose lists and gaps the lanes of a wave hold
+constexpr int kBatch = 64;             // rows whose lists and gaps the lanes of a wave hold, and rows of a tile at most
 constexpr uint32_t kGroupMask = (1u << kSaved) - 1;
 
 // Values of the V channels of a lane, as they lie in memory.
@@ -108,21 +108,15 @@ __device__ int find_list(const Lists<T>& l, int64_t total, int64_t p, int64_t* b
     return uniform((int)lo);
 }
 
-// What the lanes know of the 64 places from p0 on: lane i the list of place p0 + i and the gap before its event; bit i of `starts` and
-// `ends`, whether that place is the first and the last of its list.  A walk through a tile reads what it needs for the next 64 (a window of
-// the borders between lists, the times) while it is busy with these.
+// What the lanes know of the 64 places from a tile's first one on: lane i the list of the i-th and the gap before its event; bit i of
+// `starts` and `ends`, whether that place is the first and the last of its list.
 struct Batch {
     int list;
-    int edge;                           // the last place's list (FORWARD), or the first one's, counted along the walk
     float gap;
     uint64_t starts, ends;
 };
-struct Ahead {                          // of the batch at p0, as it was read
-    int64_t p0, from;                   // `from`: the list of the place before (FORWARD) or after the batch, or of its first (last) one
-    int border;                         // of lane i: list from + 1 + i begins at that place of the batch (FORWARD), or list from - i
-    float time;
-};
 
+// Of lane i: list base + 1 + i begins at that place of the 64 from p0 on (FORWARD), or list base - i.
 template <bool FORWARD, typename T>
 __device__ __forceinline__ int border_at(const Lists<T>& l, int64_t total, int64_t p0, int64_t base) {
     const int lane = threadIdx.x & 63;
@@ -132,21 +126,16 @@ __device__ __forceinline__ int border_at(const Lists<T>& l, int64_t total, int64
     return (int)min(max(rel, (int64_t)(FORWARD ? 0 : -1)), (int64_t)(kBatch + (FORWARD ? 1 : 0)));
 }
 
+// The tile at p0, 0 <= p0 < total.  FORWARD: `from` is its first place's list, `edge` whether that place is the list's first; backward: its
+// last place's (the place `last` of the tile), and whether that place is the list's last.
 template <bool FORWARD, bool DECAY, typename T>
-__device__ __forceinline__ Ahead look_ahead(const Lists<T>& l, int64_t total, int64_t p0, int64_t from) {
-    const int64_t p = min(max(p0 + (int)(threadIdx.x & 63), (int64_t)0), total - 1);
-    return {p0, from, border_at<FORWARD>(l, total, p0, from), DECAY ? l.ts[l.row(p, total)] : 0.0f};
-}
-
-// The batch.  FORWARD: `edge`, whether the first place is the first of `from` (a batch that begins a walk); backward: whether the place
-// `last` (the last one of the walk that the batch holds) is the last of its list.  `before`: the time of the event before the batch.
-template <bool FORWARD, bool DECAY, typename T>
-__device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const Ahead& a, bool edge, int last, float before) {
+__device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, int64_t p0, int64_t from, bool edge, int last) {
     const int lane = threadIdx.x & 63;
     int passed = 0, more = 0;                   // borders between `from` and the lane's place; and the place after lane 63's (FORWARD), before lane 0's
-    int at = a.border;
+    int at = border_at<FORWARD>(l, total, p0, from);
+    const float time = DECAY ? l.ts[l.row(min(p0 + lane, total - 1), total)] : 0.0f, before = DECAY ? l.ts[l.row(max(p0 - 1, (int64_t)0), total)] : 0.0f;
     bool all = false;                           // every border looked at lies in the batch
-    for (int64_t base = a.from, window = 0;; ++window) {
+    for (int64_t base = from, window = 0;; ++window) {
         const uint64_t some = __ballot(FORWARD ? at <= kBatch : at >= 0);
         if (some) {                             // they come in order: how many lie at or before (beyond) the lane's place
             int n = 0;
@@ -163,12 +152,12 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
         all = some == ~0ull;
         if (!all || window == 3) break;
         base += FORWARD ? kWave : -kWave;
-        at = border_at<FORWARD>(l, total, a.p0, base);
+        at = border_at<FORWARD>(l, total, p0, base);
     }
     Batch b;
-    int list = (int)min(max(a.from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
+    int list = (int)min(max(from + (FORWARD ? passed : -passed), (int64_t)0), l.S - 1);
     if (all) {                                  // many lists without events: every lane looks for its own
-        const int64_t p = max(a.p0 + lane, (int64_t)0);
+        const int64_t p = p0 + lane;
         int64_t lo = 0, hi = l.S;
         for (int k = 0; k < 31; ++k) {
             const int64_t mid = (lo + hi) >> 1;
@@ -178,12 +167,11 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
         }
         list = (int)lo;
     }
-    b.edge = __builtin_amdgcn_readlane(list, FORWARD ? kBatch - 1 : 0);
     b.list = (int)l.list(list);
     if (all) {
-        const int64_t p = a.p0 + lane, begin = l.begin_of(list, total), end = l.begin_of((int64_t)list + 1, total);
-        b.starts = __ballot((p >= 0) & (p < total) & (begin == p));
-        b.ends = __ballot((p >= 0) & (p < total) & (end == p + 1));
+        const int64_t p = p0 + lane, begin = l.begin_of(list, total), end = l.begin_of((int64_t)list + 1, total);
+        b.starts = __ballot((p < total) & (begin == p));
+        b.ends = __ballot((p < total) & (end == p + 1));
     } else if (FORWARD) {
         const int prev = __shfl_up(passed, 1);
         b.starts = __ballot((lane != 0) & (passed != prev)) | (uint64_t)(edge | (uniform(passed) != 0));
@@ -195,10 +183,10 @@ __device__ __forceinline__ Batch locate(const Lists<T>& l, int64_t total, const 
     }
     b.gap = 0.0f;
     if (DECAY) {
-        float t = __shfl_up(a.time, 1);
+        float t = __shfl_up(time, 1);
         if (lane == 0) t = before;
-        if (b.starts >> lane & 1) t = l.t0 ? l.t0[b.list] : a.time;
-        b.gap = gap_of(a.time, t);
+        if (b.starts >> lane & 1) t = l.t0 ? l.t0[b.list] : time;
+        b.gap = gap_of(time, t);
     }
     return b;
 }
@@ -372,7 +360,14 @@ struct Share {
         block = (int)(at / kXcds);
     }
 };
-__host__ __device__ constexpr int64_t workgroups_of(int64_t groups, int blocks) { return (groups + kXcds - 1) / kXcds * kXcds * blocks; }
+constexpr int64_t workgroups_of(int64_t groups, int blocks) { return (groups + kXcds - 1) / kXcds * kXcds * blocks; }
+// One of the launches that a walk takes (a launch has fewer than 2^32 threads): the groups of tiles from `first` on; workgroups from
+// `workgroups` on have no share of the walk.
+struct Piece {
+    int64_t first;
+    unsigned workgroups;
+    int blocks;
+};
 
 // ---- carries -------------------------------------------------------------------------------------------
 // The walk is cut into tiles, eight tiles to a span.  What enters a tile is the state before its first event, or (backward) what the
@@ -460,9 +455,9 @@ struct Entering {
 // (0.79 M rows of 256 bf16 channels: 0.80 GB in 168 us, 4.8 TB/s).  Sixteen tiles a workgroup took a sixth more: two workgroups fill a compute unit,
 // and their waves wait for each other.
 template <typename T, int V, bool DECAY>
-__global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l, const Carries t, int blocks) {
-    const Share share(blockIdx.x, blocks);
-    const int64_t span = share.q, tile = span * kSpan + uniform((int)(threadIdx.x >> 6));
+__global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l, const Carries t, const Piece piece) {
+    const Share share(blockIdx.x, piece.blocks);
+    const int64_t span = piece.first + share.q, tile = span * kSpan + uniform((int)(threadIdx.x >> 6));
     if (span * kSpan >= t.tiles) return;
     const int c = channel_of<V>(l.dim, share.block);
     const bool lead = share.block == 0 && (threadIdx.x & 63) == 0;
@@ -509,9 +504,9 @@ __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l,
 // First pass of the gradients: what the rows behind a tile's begin send back over it, from u and dh.  As k_recur_tails (0.79 M rows of 256
 // bf16 channels: 171 us).
 template <typename T, int V, bool DECAY>
-__global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l, const Carries t, int blocks, const T* dh, int64_t ld_dh, const float* dlast) {
-    const Share share(blockIdx.x, blocks);
-    const int64_t span = share.q, tile = span * kSpan + uniform((int)(threadIdx.x >> 6));
+__global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l, const Carries t, const Piece piece, const T* dh, int64_t ld_dh, const float* dlast) {
+    const Share share(blockIdx.x, piece.blocks);
+    const int64_t span = piece.first + share.q, tile = span * kSpan + uniform((int)(threadIdx.x >> 6));
     if (span * kSpan >= t.tiles) return;
     const int c = channel_of<V>(l.dim, share.block);
     const bool lead = share.block == 0 && (threadIdx.x & 63) == 0;
@@ -654,18 +649,18 @@ __device__ void zero_rows(const Lists<T>& l, T* out, int64_t ld, int64_t begin, 
 // the gap before it, lie in the lanes (64 rows at a time); what is the same for the wave (addresses, first and last rows) is the scalar
 // unit's.  Bound by memory: 0.79 M rows of 256 bf16 channels, all states written and saved, 1.23 GB in 223 us (5.5 TB/s); 0.80 M rows of
 // 172 fp32 channels, 1.70 GB in 331 us (5.1); 0.91 M of 128 fp32, 1.39 GB in 236 us (5.9); lists of ten, last states only, 1.14 M rows of 128
-// bf16: 0.69 GB in 142 us (4.9).
+// bf16: 0.69 GB in 141 us (4.9).  Four waves a SIMD: with the fifth that the registers have room for, the walk met less of what the first pass left
+// in the caches (0.80 M rows of 172 fp32: 348 us instead of 333; the others the same or 1 % more).
 template <typename T, int V, bool DECAY, bool STREAM>
-__global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Carries t, int blocks, T* h_out, int64_t ld_h, float* last, float* saved) {
-    const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))) k_recur_states(const Lists<T> l, const Carries t, const Piece piece, T* h_out, int64_t ld_h, float* last, float* saved) {
     const int wave = uniform((int)(threadIdx.x >> 6));
-    if (blockIdx.x >= quads) {
-        const int64_t first = ((blockIdx.x - quads) * kWaves + wave) * kWave;
+    if (blockIdx.x >= piece.workgroups) {
+        const int64_t first = ((int64_t)(blockIdx.x - piece.workgroups) * kWaves + wave) * kWave;
         if (last && first < l.S) fill_empty(l, first, l.h0, last);
         return;
     }
-    const Share share(blockIdx.x, blocks);
-    const int64_t tile = ((t.tiles + kWaves - 1) / kWaves - 1 - share.q) * kWaves + wave;
+    const Share share(blockIdx.x, piece.blocks);
+    const int64_t quad = piece.first + share.q, tile = ((t.tiles + kWaves - 1) / kWaves - 1 - quad) * kWaves + wave;
     const int c = channel_of<V>(l.dim, share.block);
     if (tile < 0 || tile >= t.tiles) return;
     const Entering<V> entering(t, tile, l.dim, c);
@@ -683,30 +678,21 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
     const int j = tile ? uniform((int)(known & ~kCrosses)) : find_list(l, total, 0);
     const bool fresh = !uniform((int)(known & kCrosses));
     entering.take(!fresh, h);
-    Batch b = locate<true, DECAY>(l, total, look_ahead<true, DECAY>(l, total, begin, j), fresh, 0, DECAY ? l.ts[l.row(max(begin - 1, (int64_t)0), total)] : 0.0f);
+    const Batch b = locate<true, DECAY>(l, total, begin, j, fresh, 0);
     Edges<V> enter;
     enter.template read<true>(l.h0, b, (uint32_t)b.starts & kGroupMask, 0, l.dim, c);
-    Ahead ahead = look_ahead<true, DECAY>(l, total, begin + kBatch, b.edge);
-    float time = DECAY ? l.ts[l.row(min(begin + kBatch - 1, total - 1), total)] : 0.0f;
     for (int64_t p = begin; p < end; p += kSaved) {
-        const int q = (int)(p - begin) & (kBatch - 1);
-        const bool more = p + kSaved < end, turn = q + kSaved == kBatch;
+        const int q = (int)(p - begin);
+        const bool more = p + kSaved < end;
         arrive(u);
         arrive(x);
         arrive(enter.v);
-        Batch next = b;
-        if (more && turn) next = locate<true, DECAY>(l, total, ahead, false, 0, time);
         Pack<T, V> next_u[kSaved], next_x[kSaved];
         Edges<V> next_enter;
         if (more) {
             read_rows<T, V>(next_u, rows_u, total, p + kSaved, c);
             read_rows<T, V>(next_x, rows_x, total, p + kSaved, c);
-            const int next_q = turn ? 0 : q + kSaved;
-            next_enter.template read<true>(l.h0, next, (uint32_t)(next.starts >> next_q) & kGroupMask, next_q, l.dim, c);
-        }
-        if (more && turn) {
-            ahead = look_ahead<true, DECAY>(l, total, p + kSaved + kBatch, next.edge);
-            if (DECAY) time = l.ts[l.row(min(p + kSaved + kBatch - 1, total - 1), total)];
+            next_enter.template read<true>(l.h0, b, (uint32_t)(b.starts >> (q + kSaved)) & kGroupMask, q + kSaved, l.dim, c);
         }
         const int n = (int)min(end - p, (int64_t)kSaved);
         const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
@@ -726,7 +712,6 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
 #pragma unroll
         for (int r = 0; r < kSaved; ++r) { u[r] = next_u[r]; x[r] = next_x[r]; }
         enter = next_enter;
-        b = next;
     }
 }
 
@@ -738,17 +723,16 @@ __global__ void __launch_bounds__(256) k_recur_states(const Lists<T> l, const Ca
 // two.  Bound by memory: 0.79 M rows of 256 bf16 channels, 2.06 GB in 414 us (5.0 TB/s); 0.80 M of 172 fp32, 2.78 GB in 602 us (4.6); lists
 // of ten, 1.14 M rows of 128 bf16, 1.28 GB in 276 us (4.6).
 template <typename T, int V, bool DECAY, bool STREAM>
-__global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Carries t, int blocks, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
+__global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Carries t, const Piece piece, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
                                                      T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
-    const int64_t quads = workgroups_of((t.tiles + kWaves - 1) / kWaves, blocks);
     const int wave = uniform((int)(threadIdx.x >> 6));
-    if (blockIdx.x >= quads) {
-        const int64_t first = ((blockIdx.x - quads) * kWaves + wave) * kWave;
+    if (blockIdx.x >= piece.workgroups) {
+        const int64_t first = ((int64_t)(blockIdx.x - piece.workgroups) * kWaves + wave) * kWave;
         if (dh0 && first < l.S) fill_empty(l, first, dlast, dh0);
         return;
     }
-    const Share share(blockIdx.x, blocks);
-    const int64_t tile = ((t.tiles + kWaves - 1) / kWaves - 1 - share.q) * kWaves + wave;
+    const Share share(blockIdx.x, piece.blocks);
+    const int64_t quad = piece.first + share.q, tile = ((t.tiles + kWaves - 1) / kWaves - 1 - quad) * kWaves + wave;
     const int c = channel_of<V>(l.dim, share.block);
     const int64_t total = l.total(), begin = tile * t.tile_rows, end = min(begin + t.tile_rows, total);
     float sum[V] = {};
@@ -759,7 +743,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
     if (tile >= 0 && begin < end) {         // (and so tile < t.tiles)
         const Entering<V> entering(t, tile, l.dim, c);
         const uint32_t known = end < total ? t.list[tile] : 0u;
-        const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved, last_batch = begin + (end - 1 - begin) / kBatch * kBatch;
+        const int64_t last_group = begin + (end - 1 - begin) / kSaved * kSaved;
         Pack<T, V> u[kSaved], x[kSaved], d[kSaved] = {};      // (d stays zero without dh)
         float enter[V];                                     // state before the group
         const Along rows_u(l, l.u, l.ld_u, total), rows_x(l, l.x, l.ld_x, total), rows_d(l, dh, ld_dh, total);
@@ -779,17 +763,14 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
         const int j = end < total ? uniform((int)(known & ~kCrosses)) : find_list(l, total, end - 1);
         const bool over = end == total || !uniform((int)(known & kCrosses));
         entering.take(!over, back);
-        auto time_before = [&](int64_t p) { return DECAY ? l.ts[l.row(max(p - 1, (int64_t)0), total)] : 0.0f; };
-        Batch b = locate<false, DECAY>(l, total, look_ahead<false, DECAY>(l, total, last_batch, j), over, (int)(end - 1 - last_batch), time_before(last_batch));
+        const Batch b = locate<false, DECAY>(l, total, begin, j, over, (int)(end - 1 - begin));
         Edges<V> start, leave;
         auto part = [](uint64_t bits, int q) { return (uint32_t)(bits >> q) & kGroupMask; };
-        int q = (int)(last_group - last_batch);
+        int q = (int)(last_group - begin);
         start.template read<true>(l.h0, b, part(b.starts, q), q, l.dim, c);
         leave.template read<false>(dlast, b, part(b.ends, q), q, l.dim, c);
-        Ahead ahead = look_ahead<false, DECAY>(l, total, last_batch - kBatch, b.edge);
-        float time = time_before(last_batch - kBatch);
         for (int64_t p = last_group; p >= begin; p -= kSaved) {
-            const bool more = p > begin, turn = q == 0;
+            const bool more = p > begin;
             const int n = (int)min(end - p, (int64_t)kSaved);
             const uint32_t starts = (uint32_t)(b.starts >> q), ends = (uint32_t)(b.ends >> q);
             arrive(u);
@@ -815,16 +796,9 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
             });
             arrive(d);
             arrive(leave.v);
-            Batch next = b;
-            if (more && turn) next = locate<false, DECAY>(l, total, ahead, (bool)(b.starts & 1), kBatch - 1, time);
-            const int next_q = turn ? kBatch - kSaved : q - kSaved;
             if (more) {
                 read_inputs(p - kSaved);
-                start.template read<true>(l.h0, next, part(next.starts, next_q), next_q, l.dim, c);
-            }
-            if (more && turn) {
-                ahead = look_ahead<false, DECAY>(l, total, p - 2 * kBatch, next.edge);
-                time = time_before(p - 2 * kBatch);
+                start.template read<true>(l.h0, b, part(b.starts, q - kSaved), q - kSaved, l.dim, c);
             }
             Global to_x = rows_dx.at(p + n - 1), to_u = rows_du.at(p + n - 1);
             each_row_back(n, [&](int r) {
@@ -848,10 +822,9 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
             });
             if (more) {
                 read_grads(p - kSaved);
-                leave.template read<false>(dlast, next, part(next.ends, next_q), next_q, l.dim, c);
+                leave.template read<false>(dlast, b, part(b.ends, q - kSaved), q - kSaved, l.dim, c);
             }
-            b = next;
-            q = next_q;
+            q -= kSaved;
         }
     }
     if (DECAY && sums) {                // the workgroup's share
@@ -863,7 +836,7 @@ __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Car
         for (int k = 1; k < kWaves; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[i] += s_sum[k][(threadIdx.x & 63) * V + i];
-        if (share.q * kWaves < t.tiles) store_floats<V>(sums + share.q * l.dim + c, sum);
+        if (quad * kWaves < t.tiles) store_floats<V>(sums + quad * l.dim + c, sum);
     }
 }
 
@@ -963,12 +936,9 @@ int check_workspace(const void* p, size_t have, size_t need) {
 // has, the less their reads overlap and the more unevenly they fill the chip; and every tile has its carry to find.  Tiles of 16, 32 and 64
 // rows: 35 K rows of 100 fp32 channels, states 13.6, 12.2, 15.2 us, gradients 21.2, 19.3, 24.5.  Of 64, 128 and 256: 0.79 M rows of 256
 // bf16 channels, states 219, 238, 246, gradients 378, 399, 413.
-// (A launch has fewer than 2^32 threads: tiles grow where there would be more than 2^20 workgroups of a span.)
 int64_t tile_rows_of(int64_t rows, int dim) {
     const int64_t blocks = (dim + kWave - 1) / kWave;
-    int64_t n = rows / 64 * blocks < 2048 ? 32 : 64;
-    while ((rows / (n * kSpan) + 1) * blocks > 1 << 20) n *= 2;
-    return n;
+    return rows / kBatch * blocks < 2048 ? 32 : kBatch;
 }
 
 size_t aligned(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -1010,10 +980,18 @@ Lists<T> typed(const tns_recur& r) {
             r.d_ts, r.d_decay, r.d_h0, r.d_t0, r.dim, (r.flags & TNS_NEWEST_FIRST) != 0, (r.flags & TNS_ZERO_BEYOND) != 0};
 }
 
-// Workgroups: of the kernels with one for every four tiles and block of channels, and every 256 lists where `lists` is set.
-unsigned groups_of(const tns_recur& r, const Workspace& w, int blocks, bool lists) {
-    return (unsigned)(workgroups_of((w.t.tiles + kWaves - 1) / kWaves, blocks) + (lists ? (r.S + kWaves * kWave - 1) / (kWaves * kWave) : 0));
+// Calls go(piece, workgroups) for the launches of a walk of `groups` groups of tiles, 2^30 threads each at most; the last one has `more`
+// workgroups beyond the walk's.
+template <typename F>
+void in_pieces(int64_t groups, int blocks, int threads, int64_t more, const F& go) {
+    const int64_t most = ((int64_t)1 << 30) / threads / blocks / kXcds * kXcds;      // (2^16 channels are 1024 blocks: 2048 groups at least)
+    for (int64_t first = 0; first < groups || (first == 0 && more); first += most) {
+        const int64_t n = std::min(groups - first, most), own = workgroups_of(n, blocks);
+        go(Piece{first, (unsigned)own, blocks}, dim3((unsigned)(own + (first + n == groups ? more : 0))));
+    }
 }
+int64_t quads_of(const Workspace& w) { return (w.t.tiles + kWaves - 1) / kWaves; }
+int64_t fills_of(const tns_recur& r, bool lists) { return lists ? (r.S + kWaves * kWave - 1) / (kWaves * kWave) : 0; }      // 256 lists a workgroup
 template <int V> int blocks_of(const tns_recur& r) { return (r.dim + kWave * V - 1) / (kWave * V); }
 
 // Whether rows are written past the caches: where one call's rows of u and x alone are more than the last-level cache holds (256 MiB), so that
@@ -1038,16 +1016,18 @@ void launch_run(const tns_recur& r, void* h, int64_t ld_h, float* last, void* sa
     const int blocks = blocks_of<V>(r);
     const Lists<T> l = typed<T>(r);
     if (w.t.tiles > 1) {
-        hipLaunchKernelGGL((k_recur_tails<T, V, DECAY>), dim3((unsigned)workgroups_of(w.spans, blocks)), dim3(kSpan * kWave), 0, stream, l, w.t, blocks);
+        in_pieces(w.spans, blocks, kSpan * kWave, 0, [&](Piece piece, dim3 grid) {
+            hipLaunchKernelGGL((k_recur_tails<T, V, DECAY>), grid, dim3(kSpan * kWave), 0, stream, l, w.t, piece);
+        });
         launch_join<false>(r, w, stream);
     }
-    if (const unsigned groups = groups_of(r, w, blocks, last != nullptr)) {
+    in_pieces(quads_of(w), blocks, 256, fills_of(r, last != nullptr), [&](Piece piece, dim3 grid) {
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<T*>(h), ld_h, last, static_cast<float*>(saved));
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, l, w.t, piece, static_cast<T*>(h), ld_h, last, static_cast<float*>(saved));
         };
         if (streams_out<T>(r, h, ld_h)) go(k_recur_states<T, V, DECAY, true>);
         else go(k_recur_states<T, V, DECAY, false>);
-    }
+    });
 }
 
 template <typename T, int V, bool DECAY>
@@ -1058,17 +1038,19 @@ void launch_grad(const tns_recur& r, const void* saved, const void* dh, int64_t 
     const Lists<T> l = typed<T>(r);
     const T* const d = static_cast<const T*>(dh);
     if (w.t.tiles > 1) {
-        hipLaunchKernelGGL((k_recur_heads<T, V, DECAY>), dim3((unsigned)workgroups_of(w.spans, blocks)), dim3(kSpan * kWave), 0, stream, l, w.t, blocks, d, ld_dh, dlast);
+        in_pieces(w.spans, blocks, kSpan * kWave, 0, [&](Piece piece, dim3 grid) {
+            hipLaunchKernelGGL((k_recur_heads<T, V, DECAY>), grid, dim3(kSpan * kWave), 0, stream, l, w.t, piece, d, ld_dh, dlast);
+        });
         launch_join<true>(r, w, stream);
     }
-    if (const unsigned groups = groups_of(r, w, blocks, dh0 != nullptr)) {
+    in_pieces(quads_of(w), blocks, 256, fills_of(r, dh0 != nullptr), [&](Piece piece, dim3 grid) {
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, stream, l, w.t, blocks, static_cast<const float*>(saved), d, ld_dh, dlast,
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, l, w.t, piece, static_cast<const float*>(saved), d, ld_dh, dlast,
                                static_cast<T*>(du), ld_du, static_cast<T*>(dx), ld_dx, dh0, ddecay ? w.sums : nullptr);
         };
         if (streams_out<T>(r, du, ld_du) && streams_out<T>(r, dx, ld_dx)) go(k_recur_grads<T, V, DECAY, true>);
         else go(k_recur_grads<T, V, DECAY, false>);
-    }
+    });
     if (ddecay)
         hipLaunchKernelGGL(k_recur_sums, dim3((r.dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, w.sums, (w.t.tiles + kWaves - 1) / kWaves, r.dim, ddecay);
 }

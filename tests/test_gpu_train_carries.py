@@ -50,3 +50,35 @@ def test_recurrence_carries(T, dtype, dim, rows, kind, newest_first):      # noq
     for k in ("h", "last", "du", "dx", "dh0"):
         close(k, got[k][:, some], want[k], want[k + "_off"], dtype if k in ("h", "du", "dx") else F32)
     close("ddecay", got["ddecay"][some], want["ddecay"], want["ddecay_off"])
+
+
+def test_recurrence_in_several_launches(T):      # noqa: F811
+    """More than 2^30 rows of one channel: both passes take two launches.  Values around the rows where one ends, zeros between them (gates of a half: nothing
+    gets through); both parts equal the oracle's."""
+    import torch
+    rows = (1 << 30) + 5000
+    g = torch.Generator("cuda").manual_seed(22)
+    rowptr = torch.tensor([0, 3000, (1 << 30) + 1000, rows], device="cuda")
+    u, x, dh = (torch.zeros((rows, 1), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    near, far = slice(0, 12_000), slice((1 << 30) - 7000, rows)
+    for part in (near, far):
+        n = part.stop - part.start
+        u[part] = (torch.randn((n, 1), generator=g, device="cuda") - 8).bfloat16()
+        x[part], dh[part] = (torch.randn((n, 1), generator=g, device="cuda").bfloat16() for _ in range(2))
+    h0, dlast = torch.randn((3, 1), generator=g, device="cuda"), torch.randn((3, 1), generator=g, device="cuda")
+    for newest_first in (False, True):
+        r = T.recur_run(rowptr, u, x, h0=h0, newest_first=newest_first, save=True)
+        got = dict(r, **T.recur_grad(rowptr, u, x, r["saved"], h0=h0, newest_first=newest_first, dh=dh, dlast=dlast))
+        for part, lens, there in ((near, [3000, 9000], [0, 1]), (far, [8000, 4000], [1, 2])):
+            starts, ends = h0[there].cpu().numpy(), dlast[there].cpu().numpy()
+            cut = there.index(1)                                     # the long list: its other end lies beyond the zeros
+            (starts if (part is far) != newest_first else ends)[cut] = 0
+            of = lambda v: v[part].float().cpu().numpy()             # noqa: E731
+            want = O.recurrence_scanned(np.concatenate([[0], np.cumsum(lens)]), of(u), of(x), h0=starts, newest_first=newest_first, dh=of(dh), dlast=ends)
+            for k in ("h", "du", "dx"):
+                close(k, got[k][part], want[k], want[k + "_off"], BF16)
+            whole = 1 - cut
+            for k in ("last", "dh0"):
+                close(k, got[k][there[whole]], want[k][whole], want[k + "_off"][whole])
+        between = slice(near.stop + 1000, far.start - 1000)
+        assert not got["dx"][between].any() and not got["h"][between].any()

@@ -244,3 +244,22 @@ for kind in (T.tns_recur, T.tns_pairs, T.tns_adamw_tensor):
             raise SystemExit(f"{kind.__name__}.{name} takes {other!r}")
 T.tns_adamw_destroy(opt)
 """)
+
+
+@pytest.mark.parametrize("rows, dim, S, walk", [((1 << 30) - 64, 1, 2, 1), ((1 << 30) + 64, 1, 2, 2), (1 << 33, 1, 2, 8), (1 << 33, 64, 2, 8), (1 << 30, 130, 2, 4),
+                                                (1 << 20, 1 << 16, 2, 1), ((1 << 20) + 1, 1 << 16, 2, 2), (1 << 33, 1, (1 << 31) - 1, 8)])
+def test_a_long_walk_takes_several_launches(run, rows, dim, S, walk):
+    # 2^30 threads of a walk a launch at most, 64 rows a wave; with the lists of the last states the last one has a thread for every list
+    run(f"""
+from paper_2311_17410_amd import train_binding as T
+r = T.tns_recur({S}, {rows}, {dim}, 0, 0, 0, 256, 256, 256, {dim}, {dim}, 256, 256, None, None)
+run, grad, _ = T.tns_recur_workspace(r)
+n = fake.fake_launches()
+T.tns_recur_run(r, 256, {dim}, 256, 256, 256, run)
+assert fake.fake_launches() - n == 2 * {walk} + 1, fake.fake_launches() - n      # first and second pass, the join between them
+last = -(-{rows} // 256) - ({walk} - 1) * ((1 << 22) // (-(-{dim} // 64)) // 8 * 8)      # groups of four tiles left for the last launch
+assert fake.fake_grid() == -(-last // 8) * 8 * -(-{dim} // 64) + -(-{S} // 256) and fake.fake_grid() < 1 << 24
+n = fake.fake_launches()
+T.tns_recur_grad(r, 256, 256, {dim}, 256, 256, {dim}, 256, {dim}, 256, 256, 256, grad)
+assert fake.fake_launches() - n == 2 * {walk} + 2, fake.fake_launches() - n      # and the sum of the decay's shares
+""")

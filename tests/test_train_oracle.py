@@ -309,3 +309,10 @@ def test_a_lost_or_repeated_carry_is_far_outside_the_bounds(span, rows, newest_f
         bad = O.recurrence_scanned(**a, **kw, change=mistake)
         for k in ("h", "dx", "du"):
             assert (np.abs(bad[k] - want[k]) > 4 * want[k + "_off"]).any(), (mistake.__name__, k)
+
+
+@pytest.mark.parametrize("dim", [1, 64, 300])
+def test_tiles_stay_as_they_are_however_many_rows_there_are(dim):
+    """A tile's rows fit the lanes of a wave: what is kept for every tile grows with the rows."""
+    one, two = (T.tns_recur_workspace(recur(S=2, rows=1 << k, dim=dim, ld_u=dim, ld_x=dim))[0] for k in (38, 39))
+    assert one >= (1 << 38) // 64 * (8 * dim + 5) and two > 1.999 * one
