@@ -68,7 +68,9 @@ __device__ __forceinline__ float of_quad(float v, int r) {
 }
 
 // Loss of a margin and its slope, both times scale and weight.  softplus(-m) = log(1 + e) + max(-m, 0) with e = exp(-|m|); the logarithm is
-// twice the inverse hyperbolic tangent of e / (2 + e), which is a third at most: nine terms of its series leave 1e-10 of it.  A side
+// twice the inverse hyperbolic tangent of e / (2 + e), which is a third at most: nine terms of its series leave 1e-10 of it.  The exponent
+// is rounded to 32 bits before it is raised: e, which is what loss and slope of a far margin are, has a relative error of (1.5 |m| + 2) 2^-24 at
+// most; to put it back costs 4000 events of 50 links half a microsecond of 35, for pairs that hardly count.  A side
 // whose factor is 0 is left out: its margin may be infinite.
 __device__ __forceinline__ void loss_of(float m, float w, float scale, float smoothing, float& loss, float& slope) {
     const float e = __builtin_amdgcn_exp2f(-fabsf(m) * tns::kLog2e), t = e * __builtin_amdgcn_rcpf(2.0f + e), q = t * t;

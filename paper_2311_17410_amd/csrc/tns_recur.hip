@@ -340,7 +340,8 @@ __device__ __forceinline__ void each_row_back(int n, const F& go) {
         if (r < n) go(r);
 }
 
-// Rate of the decay in powers of two.
+// Rate of the decay in powers of two.  Rounded, as its product with the gap is: exp(-decay gap) has a relative error of (2.5 decay gap + 3) 2^-24
+// at most, of which the product alone, in whatever base, would leave 1 (gate_of says what more bits would cost).
 template <int V, bool DECAY, typename T>
 __device__ __forceinline__ void rates(const Lists<T>& l, int c, float (&rate)[V]) {
 #pragma unroll

@@ -18,8 +18,12 @@ template <> __device__ __forceinline__ bf16 as_value<bf16>(float v) { return __b
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// z = sigmoid(u) and 1 - z, each with an error of some units in its last place: with E = exp(-u), z = 1 / (1 + E) and
-// 1 - z = E z, which is 1 from E = 2^24 on (and would be infinity times 0 in the end).
+// z = sigmoid(u) and 1 - z: with E = exp(-u), z = 1 / (1 + E) and 1 - z = E z, which is 1 from E = 2^64 on (and would be infinity times 0
+// in the end).  The exponent is rounded to 32 bits before it is raised, so E and whichever of the two is small have a relative error of
+// (1.5 |u| + 6) 2^-24 at most: 14 half units in the last place at |u| = 5, where z is 0.007, 126 at 80, where it is 2e-35.  This is a choice.
+// What the rounding leaves out can be put back (two more products, a sum and a select, three half units everywhere; the decay's likewise), but
+// these kernels issue vector instructions nearly as fast as memory feeds them: 0.79 M rows of 256 bf16 channels, states 219 -> 227 us and
+// gradients 394 -> 425 (with the decay's 251 and 471), 0.80 M of 172 fp32, gradients 607 -> 613 (621).  An absolute error of z is 2^-22 at most.
 __device__ __forceinline__ void gate_of(float u, float& z, float& rest) {
     const float a = u * -kLog2e, e = __builtin_amdgcn_exp2f(a);
     z = __builtin_amdgcn_rcpf(1.0f + e);

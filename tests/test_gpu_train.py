@@ -739,3 +739,40 @@ def test_within_autograd(T):
         with pytest.raises(RuntimeError, match="inplace"):
             kept.backward()
         opt.close()
+
+
+def test_gates_are_as_exact_as_stated(T):
+    """z, 1 - z and the decay alone, from lists of one event (x = 1 without a state; x = 0 with a state of 1): the relative errors of the header,
+    where the values are normal numbers."""
+    import torch
+    u = np.concatenate([np.linspace(-87, 87, 40_001), np.random.default_rng(23).normal(size=40_000)]).astype(np.float32)
+    rowptr = torch.arange(len(u) + 1, device="cuda")
+    g_u, one, none = torch_of(u)[:, None], torch.ones((len(u), 1), device="cuda"), torch.zeros((len(u), 1), device="cuda")
+    bound = (1.5 * np.abs(u.astype(np.float64)) + 6) * O.U
+    z, rest = O.sigmoid(u.astype(np.float64)), O.sigmoid(-u.astype(np.float64))
+    for x, h0, want in ((one, None, z), (none, one, rest)):
+        got = T.recur_run(rowptr, g_u, x, h0=h0)["h"][:, 0].cpu().numpy().astype(np.float64)
+        normal = want >= 2.0 ** -126
+        assert (np.abs(got - want) <= bound * want)[normal].all()
+    # gates shut (1 - z = 1): the decay of a state of 1 over times that begin at 0
+    for decay in (0.1, 1.0, 7.3):
+        gap = np.linspace(0, 87 / decay, 40_001).astype(np.float32)
+        shut, lam = torch.full((len(gap), 1), -200.0, device="cuda"), np.float32([decay])
+        zero = torch.zeros((len(gap), 1), device="cuda")
+        got = T.recur_run(torch.arange(len(gap) + 1, device="cuda"), shut, zero, ts=torch_of(gap), decay=torch_of(lam), h0=zero + 1, t0=zero[:, 0].contiguous())["h"][:, 0]
+        v = lam.astype(np.float64) * gap
+        want = np.exp(-v)
+        # (and the product with 1 - z = 1)
+        assert (np.abs(got.cpu().numpy() - want) <= (2.5 * v + 4) * O.U * want)[want >= 2.0 ** -126].all(), decay
+
+
+@pytest.mark.parametrize("at", [0, 700])
+def test_a_state_that_is_not_finite_stays_so(T, at):
+    """An infinite value in a list of many tiles: from there on the list's states are infinite or NaN, before it and in other lists finite."""
+    import torch
+    rng = np.random.default_rng(24)
+    a = the_lists(rng, [300, 3000, 50], 20, F32, True, True)
+    a["x"][300 + at, 7] = np.inf
+    h = T.recur_run(**on_gpu(a, F32))["h"].cpu().numpy()
+    bad = ~np.isfinite(h)
+    assert bad[300 + at: 3300, 7].all() and bad.sum() == 3000 - at
