@@ -127,19 +127,23 @@ TNS_API int tns_pair_loss(const tns_pairs *p, float *d_loss, float *d_margin, vo
 
 /* ---- AdamW ------------------------------------------------------------------------------------------
  *
- * One step over all tensors (every operation rounded to fp32 on its own):
+ * One step over all tensors.  m, v, codes and scales are rounded to fp32 operation by operation and so have the same bits wherever
+ * they are computed; a weight's change is a product with an approximate reciprocal, right to 8 parts in 2^24:
  *     g = grad * *d_grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) (g g)
  *     param = param (1 - lr weight_decay) - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  *
  * State of 8 bits: m and r = sqrt(v) as OCP e4m3 codes with an fp32 scale for every 256 weights of a tensor,
- * the largest magnitude over 448; m = code * scale, v = (code * scale)^2.  A new value is rounded to one
+ * the largest magnitude over 448; m = code * scale, v = (code * scale)^2.  A new m or r is rounded to one
  * of the two codes around it at random so that it is right on average (an average that moves by a tenth of
- * a percent a step would otherwise stay on its code for ever).  Only normal codes are written: an m below
- * 2^-6 of a scale becomes 0, an r below that is raised to it, so that no step is divided by a zero the
- * state cannot express; where all 256 are below 2^-100 the codes and the scale are 0.  The sixteen random
- * bits of weight i are those numbered 16 (i mod 4) of mix(key + G (i / 4 + 1)), key = mix(seed + G t), with
- * the mixing function mix and the increment G of splitmix64; i counts from a tensor's first weight on and
- * tensors follow each other, each rounded up to 256.
+ * a percent a step would otherwise stay on its code for ever).  v is not: a square is larger by the rounding's
+ * variance, which adds up over the steps that v averages.  With beta2 = 0.999 and normal gradients v is some 5 % high
+ * on average after thousands of steps (r 1 %), 0.7 to 1.6 times its value for a single weight over thousands
+ * of steps, 0.25 to 3 times at a single step.  Only normal codes are written: an m below 2^-6 of a scale becomes 0, an r
+ * below that is raised to it, so that no step is divided by a zero the state cannot express; where all 256
+ * are below 2^-100 the codes and the scale are 0.  The sixteen random bits of weight i, the same for m and r, are
+ * those numbered 16 (i mod 4) of mix(key + G (i / 4 + 1)), key = mix(seed + G t), with the mixing function mix and
+ * the increment G of splitmix64; i counts from a tensor's first weight on and tensors follow each other, each
+ * rounded up to 256.
  * States that are not finite poison their 256 weights, as they would poison single ones in 32 bits.
  */
 typedef struct {

@@ -316,3 +316,20 @@ def test_tiles_stay_as_they_are_however_many_rows_there_are(dim):
     """A tile's rows fit the lanes of a wave: what is kept for every tile grows with the rows."""
     one, two = (T.tns_recur_workspace(recur(S=2, rows=1 << k, dim=dim, ld_u=dim, ld_x=dim))[0] for k in (38, 39))
     assert one >= (1 << 38) // 64 * (8 * dim + 5) and two > 1.999 * one
+
+
+def test_an_8_bit_second_moment_is_high_by_its_roundings_variance():
+    """4000 steps of normal gradients: the root is right to a percent or two on average, its square high by some percent (as the header says)."""
+    rng, n, v = np.random.default_rng(25), 256, np.zeros(256)
+    state = dict(m=np.zeros(n, np.uint8), v=np.zeros(n, np.uint8), m_scale=np.zeros(1, np.float32), v_scale=np.zeros(1, np.float32))
+    param, squares, roots = np.zeros(n, np.float32), [], []
+    for t in range(1, 4001):
+        g = (0.02 * rng.normal(size=n)).astype(np.float32)
+        v = 0.999 * v + 0.001 * g.astype(np.float64) ** 2
+        _, _, state = O.adamw(param, g, state, t, weight_decay=0.0, seed=5)
+        if t > 2000 and t % 20 == 0:
+            r = O.e4m3_value(state["v"]).astype(np.float64) * state["v_scale"][0]
+            squares.append((r * r / v).mean())
+            roots.append((r / np.sqrt(v)).mean())
+    # single weights are off by 0.2, so their mean over 256 by 0.0125; four times that
+    assert 1.0 < np.mean(squares) < 1.1 and abs(np.mean(roots) - 1.01) < 0.05, (np.mean(squares), np.mean(roots))
