@@ -1099,7 +1099,7 @@ int tns_recur_run(const tns_recur* r, void* d_h, int64_t ld_h, float* d_h_last, 
     if (int e = check_workspace(d_workspace, workspace_bytes, carve(*r, nullptr).bytes)) return e;
     if (r->S == 0 && !(r->flags & TNS_ZERO_BEYOND)) return TNS_OK;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    choose(*r, ld_h % 2 == 0 && !misaligned(d_h, 4), [&](auto value, auto v, auto decay) {
+    choose(*r, !d_h || (ld_h % 2 == 0 && !misaligned(d_h, 4)), [&](auto value, auto v, auto decay) {
         launch_run<decltype(value), v(), decay()>(*r, d_h, ld_h, d_h_last, d_saved, d_workspace, stream);
     });
     return launched("tns_recur_run");

@@ -263,3 +263,15 @@ n = fake.fake_launches()
 T.tns_recur_grad(r, 256, 256, {dim}, 256, 256, {dim}, 256, {dim}, 256, 256, 256, grad)
 assert fake.fake_launches() - n == 2 * {walk} + 2, fake.fake_launches() - n      # and the sum of the decay's shares
 """)
+
+
+def test_the_stride_of_states_that_are_not_wanted_does_not_matter(run):
+    # 256 channels in 16 bits: two workgroups of pairs for every group of tiles, whatever ld_h is; only rows that are written can ask for single values
+    run("""
+from paper_2311_17410_amd import train_binding as T
+r = T.tns_recur(2, 100_000, 256, 1, 0, 0, 256, 256, 256, 256, 256, None, None, None, None)
+def grid(*h):
+    T.tns_recur_run(r, *h, 0, 0, 256, T.tns_recur_workspace(r)[0])
+    return fake.fake_grid()
+assert grid(0, 256) == grid(0, 257) == grid(256, 256) and grid(256, 257) == 2 * grid(256, 256)
+""")
