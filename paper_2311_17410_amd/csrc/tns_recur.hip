@@ -453,7 +453,7 @@ struct Entering {
 
 // First pass of the states: reads the rows of every list that crosses the end of a tile, from the list's begin or the tile's on.  For short
 // lists that is half a list a tile (1.14 M rows of 128 bf16 channels in lists of ten: 29 us), for long ones all rows, and then bound by memory
-// (0.79 M rows of 256 bf16 channels: 0.80 GB in 168 us, 4.8 TB/s).  Sixteen tiles a workgroup took a sixth more: two workgroups fill a compute unit,
+// (0.79 M rows of 256 bf16 channels: 0.82 GB in 165 us, 5.0 TB/s).  Sixteen tiles a workgroup took a sixth more: two workgroups fill a compute unit,
 // and their waves wait for each other.
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l, const Carries t, const Piece piece) {
@@ -503,7 +503,7 @@ __global__ void __launch_bounds__(kSpan * kWave) k_recur_tails(const Lists<T> l,
 }
 
 // First pass of the gradients: what the rows behind a tile's begin send back over it, from u and dh.  As k_recur_tails (0.79 M rows of 256
-// bf16 channels: 171 us).
+// bf16 channels: 167 us).
 template <typename T, int V, bool DECAY>
 __global__ void __launch_bounds__(kSpan * kWave) k_recur_heads(const Lists<T> l, const Carries t, const Piece piece, const T* dh, int64_t ld_dh, const float* dlast) {
     const Share share(blockIdx.x, piece.blocks);
@@ -648,8 +648,8 @@ __device__ void zero_rows(const Lists<T>& l, T* out, int64_t ld, int64_t begin, 
 
 // h = f h + z x along the rows of a tile, V channels a lane, 16 rows in registers and the next 16 on their way.  The list a row belongs to, and
 // the gap before it, lie in the lanes (64 rows at a time); what is the same for the wave (addresses, first and last rows) is the scalar
-// unit's.  Bound by memory: 0.79 M rows of 256 bf16 channels, all states written and saved, 1.23 GB in 223 us (5.5 TB/s); 0.80 M rows of
-// 172 fp32 channels, 1.70 GB in 331 us (5.1); 0.91 M of 128 fp32, 1.39 GB in 236 us (5.9); lists of ten, last states only, 1.14 M rows of 128
+// unit's.  Bound by memory: 0.79 M rows of 256 bf16 channels, all states written and saved, 1.26 GB in 219 us (5.8 TB/s); 0.80 M rows of
+// 172 fp32 channels, 1.70 GB in 334 us (5.1); 0.91 M of 128 fp32, 1.39 GB in 233 us (6.0); lists of ten, last states only, 1.14 M rows of 128
 // bf16: 0.69 GB in 141 us (4.9).  Four waves a SIMD: with the fifth that the registers have room for, the walk met less of what the first pass left
 // in the caches (0.80 M rows of 172 fp32: 348 us instead of 333; the others the same or 1 % more).
 template <typename T, int V, bool DECAY, bool STREAM>
@@ -721,8 +721,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 4))
 // The gradients of a tile's rows, group by group from the last one back.  A group's states are computed again from the one saved before it
 // (a sixteenth of what reading them all would cost, and they stay in fp32), then the group is walked back.  The next rows of u and x are on
 // their way during the walk back, those of dh during the walk forward: a second set of registers for them left one wave a SIMD instead of
-// two.  Bound by memory: 0.79 M rows of 256 bf16 channels, 2.06 GB in 414 us (5.0 TB/s); 0.80 M of 172 fp32, 2.78 GB in 602 us (4.6); lists
-// of ten, 1.14 M rows of 128 bf16, 1.28 GB in 276 us (4.6).
+// two.  Bound by memory: 0.79 M rows of 256 bf16 channels, 2.05 GB in 394 us (5.2 TB/s); 0.80 M of 172 fp32, 2.78 GB in 607 us (4.6); lists
+// of ten, 1.14 M rows of 128 bf16, 1.28 GB in 272 us (4.7).
 template <typename T, int V, bool DECAY, bool STREAM>
 __global__ void __launch_bounds__(256) k_recur_grads(const Lists<T> l, const Carries t, const Piece piece, const float* saved, const T* dh, int64_t ld_dh, const float* dlast,
                                                      T* du, int64_t ld_du, T* dx, int64_t ld_dx, float* dh0, float* sums) {
@@ -935,8 +935,9 @@ int check_workspace(const void* p, size_t have, size_t need) {
 
 // Rows of a tile.  A wave takes a tile's rows one after the other, so a small call is as long as its tiles; the fewer waves a large one
 // has, the less their reads overlap and the more unevenly they fill the chip; and every tile has its carry to find.  Tiles of 16, 32 and 64
-// rows: 35 K rows of 100 fp32 channels, states 13.6, 12.2, 15.2 us, gradients 21.2, 19.3, 24.5.  Of 64, 128 and 256: 0.79 M rows of 256
-// bf16 channels, states 219, 238, 246, gradients 378, 399, 413.
+// rows: 35 K rows of 100 fp32 channels, states 13.6, 12.2, 15.2 us, gradients 21.2, 19.3, 24.5.  Of 64, 128 and 256 (more
+// than a wave's lanes hold lists and gaps of; measured with code, since gone, that went from 64 places to the next): 0.79 M rows of 256 bf16
+// channels, states 219, 238, 246, gradients 378, 399, 413.
 int64_t tile_rows_of(int64_t rows, int dim) {
     const int64_t blocks = (dim + kWave - 1) / kWave;
     return rows / kBatch * blocks < 2048 ? 32 : kBatch;
