@@ -35,23 +35,29 @@ struct Distill {                        // tns_distill_desc with its types; a la
     float rate, scale;                  // rate: 1 / temperature
 };
 
-// Over a workgroup, in a fixed order; the same value for all threads.
-template <int THREADS, typename Op>
-__device__ __forceinline__ float over_workgroup(float v, float* s_part, const Op& op) {
-    v = over_lanes(v, kWave, op);
-    if constexpr (THREADS > kWave) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = s_part[0];
+// K values at once over a workgroup, in a fixed order; the same values for all threads.  `s_part` is used for this alone (so that one barrier is enough).
+template <int THREADS, int K, typename Op>
+__device__ __forceinline__ void over_workgroup(float (&v)[K], float (&s_part)[K][16], const Op& op) {
 #pragma unroll
-        for (int w = 1; w < THREADS / kWave; ++w) v = op(v, s_part[w]);
+    for (int k = 0; k < K; ++k) v[k] = over_lanes(v[k], kWave, op);
+    if constexpr (THREADS > kWave) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) s_part[k][threadIdx.x >> 6] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = s_part[k][0];
+#pragma unroll
+            for (int w = 1; w < THREADS / kWave; ++w) v[k] = op(v[k], s_part[k][w]);
+        }
+    } else {
+        __syncthreads();
     }
-    return v;
 }
 
-// Values of a row from `begin` on, `count` of them, as THREADS threads hold them: sixteen bytes at a time from the row's aligned addresses on,
-// so the first vector begins `skew` values before the piece.  What lies outside the piece is not touched.
+// `count` values of a row from `piece` on, as THREADS threads hold them: sixteen bytes at a time from aligned addresses on, so the first vector
+// begins `skew` values before the piece.  What lies outside the piece is not touched; its places hold -infinity.
 template <typename T, int THREADS, int NV>
 struct Held {
     static constexpr int VEC = 16 / sizeof(T), N = VEC * NV;
@@ -64,22 +70,42 @@ struct Held {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int at = first(j, skew);
-            raw[j] = Vec{};
-            if (at >= 0 && at + VEC <= count) raw[j] = *reinterpret_cast<const Vec*>(piece + at);
-            else if (at > -VEC && at < count)
+            if (at >= 0 && at + VEC <= count) {
+                raw[j] = *reinterpret_cast<const Vec*>(piece + at);
+            } else {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    if (at + i >= 0 && at + i < count) raw[j].v[i] = piece[at + i];
+                for (int i = 0; i < VEC; ++i) raw[j].v[i] = at + i >= 0 && at + i < count ? piece[at + i] : as_value<T>(-kInf);
+            }
         }
     }
-    // With the same skew as the vectors were read with, or value by value.
+    __device__ __forceinline__ float get(int j, int i) const { return as_float(raw[j].v[i]); }
+    __device__ __forceinline__ float top() const {
+        float v = -kInf;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v = fmaxf(v, get(j, i));
+        return v;
+    }
+    __device__ __forceinline__ float sum(float base, float by) const {
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v += __builtin_amdgcn_exp2f((get(j, i) - base) * by);
+        return v;
+    }
+    // With the same skew as the vectors were read with, or value by value.  STREAM: with the non-temporal hint.
+    template <bool STREAM>
     __device__ __forceinline__ static void write(T* piece, int count, int skew, bool same, int j, const float (&v)[VEC]) {
         const int at = first(j, skew);
         if (same && at >= 0 && at + VEC <= count) {
             Vec out;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) out.v[i] = as_value<T>(v[i]);
-            *reinterpret_cast<Vec*>(piece + at) = out;
+            using Words = uint32_t __attribute__((ext_vector_type(4)));
+            if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(Words, out), reinterpret_cast<Words*>(piece + at));
+            else *reinterpret_cast<Vec*>(piece + at) = out;
         } else if (at > -VEC && at < count) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
@@ -88,145 +114,101 @@ struct Held {
     }
 };
 
-// A piece's bits of the candidates that some id names.
-template <int PIECE>
-struct Names {
-    uint32_t word[PIECE / 32];
-    __device__ bool has(int at) const { return word[at >> 5] >> (at & 31) & 1; }
-};
-// What all pieces of a row know of the teacher: ids and p in LDS, p's sum, what its entropy adds to the loss, and whether an id of the
-// piece is named twice.
-struct Teacher {
-    float mass, rest, entropy;          // sum of p; of the others; sum of p log p
-    bool twice;
-};
+__device__ __forceinline__ float base_of(float top) { return top == -kInf ? 0.0f : top; }
 
-template <typename T, int THREADS, int PIECE>
-__device__ __forceinline__ Teacher teach(const Distill<T>& d, int64_t row, int64_t begin, int count, int32_t* s_id, float* s_p, Names<PIECE>& names, int* s_twice, float* s_part) {
-    for (int i = threadIdx.x; i < PIECE / 32; i += THREADS) names.word[i] = 0;
-    if (threadIdx.x == 0) *s_twice = 0;
+// What is known of a row's ids, in LDS.
+struct Ids {
+    int32_t* id;                        // -1 outside the candidates
+    float *p, *x;                       // teacher's probability (before it: score / temperature); student's score
+    __device__ Ids(float* mem, int K) : id(reinterpret_cast<int32_t*>(mem)), p(mem + K), x(mem + 2 * K) {}
+};
+constexpr size_t ids_bytes(int K) { return (size_t)K * 12; }
+
+// Reads them; the largest of the teacher's scores that the thread has seen.
+template <typename T, int THREADS>
+__device__ __forceinline__ float read_ids(const Distill<T>& d, int64_t row, const Ids& ids) {
     float top = -kInf;
     for (int k = threadIdx.x; k < d.K; k += THREADS) {
         const int32_t id = d.ids[row * d.K + k];
         const bool is = id >= 0 && id < d.V;
         const float t = is ? d.teacher[row * d.K + k] * d.rate : -kInf;
-        s_id[k] = is ? id : -1;
-        s_p[k] = t;
+        ids.id[k] = is ? id : -1;
+        ids.p[k] = t;
+        ids.x[k] = is ? as_float(d.logits[row * d.ld + id]) : 0.0f;
         top = fmaxf(top, t);
     }
-    float lse;
-    if (d.lse) {
-        lse = d.lse[row];
-        __syncthreads();
-    } else {
-        top = over_workgroup<THREADS>(top, s_part, Max{});
-        const float base = top == -kInf ? 0.0f : top;
-        float sum = 0.0f;
-        for (int k = threadIdx.x; k < d.K; k += THREADS) sum += expf(s_p[k] - base);
-        sum = over_workgroup<THREADS>(sum, s_part, Add{});
-        lse = sum > 0.0f || sum != sum ? base + logf(sum) : 0.0f;      // (no entry: every p is exp(-infinity))
-        __syncthreads();
-    }
-    float mass = 0.0f, entropy = 0.0f;
+    return top;
+}
+
+// Sums over a row: of p, of p log p, of p (student's score - largest) / temperature.
+struct Terms {
+    float mass, entropy, score;
+};
+template <typename T, int THREADS>
+__device__ __forceinline__ Terms terms_of(const Distill<T>& d, const Ids& ids, float lse, float base) {
+    Terms t = {0.0f, 0.0f, 0.0f};
     for (int k = threadIdx.x; k < d.K; k += THREADS) {
-        const float l = s_p[k] - lse, p = expf(l);
-        s_p[k] = p;
-        mass += p;
-        entropy += p == 0.0f ? 0.0f : p * l;
-        const int64_t at = s_id[k] - begin;
-        if (s_id[k] >= 0 && at >= 0 && at < count)
-            if (atomicOr(&names.word[at >> 5], 1u << (at & 31)) >> (at & 31) & 1) *s_twice = 1;
+        const float l = ids.p[k] - lse, p = expf(l);
+        ids.p[k] = p;
+        t.mass += p;
+        if (p != 0.0f) {
+            t.entropy += p * l;
+            t.score += p * ((ids.x[k] - base) * d.rate);
+        }
     }
-    Teacher t;
-    t.mass = over_workgroup<THREADS>(mass, s_part, Add{});
-    t.entropy = over_workgroup<THREADS>(entropy, s_part, Add{});
-    t.rest = d.lse ? fmaxf(1.0f - t.mass, 0.0f) : 0.0f;
-    if (t.mass != t.mass) t.rest = t.mass;
-    __syncthreads();
-    t.twice = *s_twice != 0;
     return t;
 }
+template <typename T>
+__device__ __forceinline__ float teacher_sum(const Distill<T>& d, const Ids& ids, float base, int threads) {
+    float sum = 0.0f;
+    for (int k = threadIdx.x; k < d.K; k += threads) sum += expf(ids.p[k] - base);
+    return sum;
+}
+// (no entry: every p is exp(-infinity))
+__device__ __forceinline__ float teacher_lse(float base, float sum) { return sum > 0.0f || sum != sum ? base + logf(sum) : 0.0f; }
+// The others' mass, and 0 without d_lse.
+template <typename T>
+__device__ __forceinline__ float rest_of(const Distill<T>& d, float mass) { return !d.lse ? 0.0f : mass == mass ? fmaxf(1.0f - mass, 0.0f) : mass; }
 
 // Of a row's scores, or a piece of them: the largest, and the sums of exp(rate (score - largest)) over all and over those that no id names.
 struct Stats {
     float top, all, others;
 };
-template <typename T, int THREADS, int NV, int PIECE>
-__device__ __forceinline__ Stats stats_of(const Distill<T>& d, const Held<T, THREADS, NV>& held, int count, int skew, bool split, const Names<PIECE>& names, float* s_part) {
-    using H = Held<T, THREADS, NV>;
-    Stats s = {-kInf, 0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < H::VEC; ++i) {
-            const int at = H::first(j, skew) + i;
-            const float v = as_float(held.raw[j].v[i]);
-            if (at >= 0 && at < count) s.top = fmaxf(s.top, v);
-        }
-    s.top = over_workgroup<THREADS>(s.top, s_part, Max{});
-    const float base = s.top == -kInf ? 0.0f : s.top, by = d.rate * kLog2e;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < H::VEC; ++i) {
-            const int at = H::first(j, skew) + i;
-            if (at < 0 || at >= count) continue;
-            const float e = __builtin_amdgcn_exp2f((as_float(held.raw[j].v[i]) - base) * by);
-            s.all += e;
-            if (split && !names.has(at)) s.others += e;
-        }
-    s.all = over_workgroup<THREADS>(s.all, s_part, Add{});
-    if (split) s.others = over_workgroup<THREADS>(s.others, s_part, Add{});
-    return s;
+__device__ __forceinline__ float loss_of(const Terms& t, float rest, const Stats& s) {
+    const float log_all = logf(s.all);
+    float l = t.entropy - t.score + (t.mass != 0.0f ? t.mass * log_all : 0.0f);
+    if (rest != 0.0f) l += rest * (logf(rest) - (logf(s.others) - log_all));
+    return l;
 }
 
-// Gradient of a row's piece and (`loss`) the row's loss, from the whole row's statistics.
-template <typename T, int THREADS, int NV, int PIECE>
-__device__ __forceinline__ void finish(const Distill<T>& d, const Held<T, THREADS, NV>& held, int64_t row, int64_t begin, int count, int skew, const Teacher& t, const Stats& s,
-                                       float weight, const int32_t* s_id, const float* s_p, const Names<PIECE>& names, float* s_part, bool loss, float* rows, T* dlogits) {
+// Gradient of a row's piece from the whole row's statistics.  By a named candidate it is q (mass + rest) - p, by another one q (mass + rest) -
+// rest exp(.) / others, both times c.  All are written as others first, then the named ones once more, by the threads that have them: a
+// workgroup's stores of one address stay in order over the barrier.
+template <bool STREAM, typename T, int THREADS, int NV>
+__device__ __forceinline__ void write_grad(const Distill<T>& d, const Held<T, THREADS, NV>& held, int64_t row, int64_t begin, int count, int skew, const Stats& s, float mass, float rest,
+                                           float weight, const Ids& ids, bool twice, T* dlogits) {
     using H = Held<T, THREADS, NV>;
-    const float base = s.top == -kInf ? 0.0f : s.top, by = d.rate * kLog2e, inverse = 1.0f / s.all, c = d.scale * d.rate * weight;
-    const T* const logits = d.logits + row * d.ld;
-    if (loss) {
-        const float log_all = logf(s.all);
-        float sum = 0.0f;
-        for (int k = threadIdx.x; k < d.K; k += THREADS)
-            if (s_p[k] != 0.0f) sum -= s_p[k] * ((as_float(logits[s_id[k]]) - base) * d.rate - log_all);
-        sum = over_workgroup<THREADS>(sum, s_part, Add{});
-        if (threadIdx.x == 0) {
-            float l = t.entropy + sum;
-            if (t.rest != 0.0f) l += t.rest * (logf(t.rest) - (logf(s.others) - log_all));
-            rows[row] = weight * l;
-        }
-    }
-    if (!dlogits) return;
-    // by a named candidate q (mass + rest) - p, by another one q (mass + rest) - rest exp(.) / others, both times c
-    const float named = c * (t.mass + t.rest) * inverse, other = t.rest != 0.0f ? named - c * t.rest / s.others : named;
+    const float base = base_of(s.top), by = d.rate * kLog2e, c = d.scale * d.rate * weight;
+    const float named = c * (mass + rest) * (1.0f / s.all), other = rest != 0.0f ? named - c * rest / s.others : named;
     T* const to = dlogits + row * d.V + begin;
-    const bool same = H::skew_of(to) == skew, split = other != named;
+    const bool same = H::skew_of(to) == skew;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         float g[H::VEC];
 #pragma unroll
-        for (int i = 0; i < H::VEC; ++i) {
-            const int at = H::first(j, skew) + i;
-            const float e = __builtin_amdgcn_exp2f((as_float(held.raw[j].v[i]) - base) * by);
-            g[i] = e * (split && at >= 0 && at < count && names.has(at) ? named : other);
-        }
-        H::write(to, count, skew, same, j, g);
+        for (int i = 0; i < H::VEC; ++i) g[i] = __builtin_amdgcn_exp2f((held.get(j, i) - base) * by) * other;
+        H::template write<STREAM>(to, count, skew, same, j, g);
     }
-    // then the named ones once more, whole: the workgroup's stores of one address stay in order over the barrier
     __syncthreads();
     for (int k = threadIdx.x; k < d.K; k += THREADS) {
-        const int64_t at = s_id[k] - begin;
-        if (s_id[k] < 0 || at < 0 || at >= count) continue;
-        float p = s_p[k];
-        if (t.twice) {                  // (threads of the same id add up the same terms in the same order)
+        const int64_t at = ids.id[k] - begin;
+        if (ids.id[k] < 0 || at < 0 || at >= count) continue;
+        float p = ids.p[k];
+        if (twice) {                    // (threads of the same id add up the same terms in the same order)
             p = 0.0f;
-            for (int i = 0; i < d.K; ++i) p += s_id[i] == s_id[k] ? s_p[i] : 0.0f;
+            for (int i = 0; i < d.K; ++i) p += ids.id[i] == ids.id[k] ? ids.p[i] : 0.0f;
         }
-        const float e = __builtin_amdgcn_exp2f((as_float(logits[s_id[k]]) - base) * by);
-        to[at] = as_value<T>(e * named - c * p);
+        to[at] = as_value<T>(__builtin_amdgcn_exp2f((ids.x[k] - base) * by) * named - c * p);
     }
 }
 
@@ -238,89 +220,182 @@ __device__ __forceinline__ void nothing(const Distill<T>& d, int64_t row, int64_
         for (int64_t i = threadIdx.x; i < count; i += THREADS) dlogits[row * d.V + begin + i] = T{};
 }
 
-// A whole row in a workgroup's registers: read once, written once.
-template <typename T, int THREADS, int NV>
+// Which candidates of a piece some id names, a bit each.
+template <int PLACES>
+struct Names {
+    uint32_t word[(PLACES + 31) / 32];
+    template <int THREADS>
+    __device__ __forceinline__ void clear() {
+        for (int i = threadIdx.x; i < (PLACES + 31) / 32; i += THREADS) word[i] = 0;
+    }
+    __device__ __forceinline__ bool add(int at) { return !(atomicOr(&word[at >> 5], 1u << (at & 31)) >> (at & 31) & 1); }      // whether it was not there
+};
+
+// A whole row in a workgroup's registers: read once, written once.  Bound by memory where there are many rows: 4000 of 10000 bf16 scores with
+// fifty ids, 160 MB in 34 us (4.7 TB/s); with 1024 threads to a row, a bit looked up for every score and bounds checked at every use it was 126 us,
+// bound by instructions.  600 rows of 1000 fp32 scores: 4.9 us, four waits one after the other.  REST: the scores that no id names are added up by themselves (what is left
+// of the sum over all without the named ones would lose them where they are few): the row lies in LDS too, the named ones are crossed
+// out there, and the threads take their values from it again.
+template <typename T, int THREADS, int NV, bool REST>
 __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, float* rows, T* dlogits) {
-    constexpr int PIECE = THREADS * NV * (16 / (int)sizeof(T));
-    __shared__ Names<PIECE> names;
-    __shared__ int32_t s_id[kMostIds];
-    __shared__ float s_p[kMostIds], s_part[16];
-    __shared__ int s_twice;
+    using H = Held<T, THREADS, NV>;
+    constexpr int PLACES = THREADS * H::N;
+    extern __shared__ float s_mem[];
+    __shared__ typename H::Vec s_row[REST ? THREADS * NV : 1];
+    __shared__ Names<PLACES> names;
+    __shared__ float s_top[2][16], s_lse[1][16], s_sum[6][16];
+    const Ids ids(s_mem, d.K);
     const int64_t row = d.first + blockIdx.x;
     const float weight = d.weight ? d.weight[row] : 1.0f;
     if (weight == 0.0f) return nothing<T, THREADS>(d, row, 0, d.V, rows, dlogits);
     const T* const piece = d.logits + row * d.ld;
-    const int count = (int)d.V, skew = Held<T, THREADS, NV>::skew_of(piece);
-    Held<T, THREADS, NV> held;
+    const int count = (int)d.V, skew = H::skew_of(piece);
+    H held;
     held.read(piece, count, skew);
-    const Teacher t = teach<T, THREADS>(d, row, 0, count, s_id, s_p, names, &s_twice, s_part);
-    if (t.mass == 0.0f && !d.lse) return nothing<T, THREADS>(d, row, 0, d.V, rows, dlogits);
-    const Stats s = stats_of(d, held, count, skew, t.rest != 0.0f, names, s_part);
-    finish(d, held, row, 0, count, skew, t, s, weight, s_id, s_p, names, s_part, true, rows, dlogits);
+    names.template clear<THREADS>();
+    float top[2];
+    top[1] = read_ids<T, THREADS>(d, row, ids);
+    if (REST)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) s_row[j * THREADS + threadIdx.x] = held.raw[j];
+    top[0] = held.top();
+    over_workgroup<THREADS>(top, s_top, Max{});
+    const float base = base_of(top[0]), by = d.rate * kLog2e;
+    float sum[6] = {};                  // over the row (REST: without the named), over the named, mass, entropy, score, whether some id came twice
+    for (int k = threadIdx.x; k < d.K; k += THREADS) {
+        const int at = ids.id[k];
+        if (at < 0) continue;
+        if (names.add(at)) sum[1] += __builtin_amdgcn_exp2f((ids.x[k] - base) * by);
+        else sum[5] = 1.0f;
+        if (REST) reinterpret_cast<T*>(s_row)[at + skew] = as_value<T>(-kInf);
+    }
+    float lse;
+    if (REST) {
+        lse = d.lse[row];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NV; ++j) held.raw[j] = s_row[j * THREADS + threadIdx.x];
+    } else {
+        float t[1] = {teacher_sum(d, ids, base_of(top[1]), THREADS)};
+        over_workgroup<THREADS>(t, s_lse, Add{});
+        lse = teacher_lse(base_of(top[1]), t[0]);
+    }
+    const Terms mine = terms_of<T, THREADS>(d, ids, lse, base);
+    sum[0] = held.sum(base, by);
+    sum[2] = mine.mass;
+    sum[3] = mine.entropy;
+    sum[4] = mine.score;
+    over_workgroup<THREADS>(sum, s_sum, Add{});
+    const Terms t = {sum[2], sum[3], sum[4]};
+    if (!REST && t.mass == 0.0f) return nothing<T, THREADS>(d, row, 0, d.V, rows, dlogits);
+    const Stats s = {top[0], REST ? sum[0] + sum[1] : sum[0], sum[0]};
+    const float rest = rest_of(d, t.mass);
+    if (threadIdx.x == 0) rows[row] = weight * loss_of(t, rest, s);
+    if (dlogits) write_grad<false>(d, held, row, 0, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
 }
 
-// Rows of several pieces: the pieces' statistics, then their gradients.
-constexpr int kThreads = 1024, kPieceBytes = 1 << 16;
-template <typename T> constexpr int kVectors = kPieceBytes / 16 / kThreads;
-template <typename T> constexpr int kPiece = kPieceBytes / (int)sizeof(T) - 16 / (int)sizeof(T);      // (a vector less: where the row is not aligned)
-template <typename T>
+// Rows of several pieces: the pieces' statistics, then their gradients.  200 rows of 500009 fp32 scores: 95 and 142 us before the second pass
+// was made to find the rows in the caches (below).
+constexpr int kThreads = 256, kVectors = 8, kPieceBytes = kThreads * kVectors * 16;
+template <typename T> constexpr int kPiece = (kPieceBytes - 16) / (int)sizeof(T);      // (a vector less: where the row is not aligned)
+template <typename T, bool REST>
 __global__ void __launch_bounds__(kThreads) k_distill_stats(const Distill<T> d, unsigned pieces, Stats* stats) {
-    constexpr int NV = kVectors<T>;
-    __shared__ Names<kPieceBytes / (int)sizeof(T)> names;
-    __shared__ int32_t s_id[kMostIds];
-    __shared__ float s_p[kMostIds], s_part[16];
-    __shared__ int s_twice;
+    using H = Held<T, kThreads, kVectors>;
+    __shared__ typename H::Vec s_row[REST ? kThreads * kVectors : 1];
+    __shared__ Names<kThreads * H::N> names;
+    __shared__ float s_top[1][16], s_sum[2][16];
     const int64_t row = d.first + blockIdx.x / pieces, begin = (int64_t)(blockIdx.x % pieces) * kPiece<T>;
     const int count = (int)min(d.V - begin, (int64_t)kPiece<T>);
     if (d.weight && d.weight[row] == 0.0f) return;
     const T* const piece = d.logits + row * d.ld + begin;
-    const int skew = Held<T, kThreads, NV>::skew_of(piece);
-    Held<T, kThreads, NV> held;
+    const int skew = H::skew_of(piece);
+    H held;
     held.read(piece, count, skew);
-    if (d.lse) teach<T, kThreads>(d, row, begin, count, s_id, s_p, names, &s_twice, s_part);
-    const Stats s = stats_of(d, held, count, skew, d.lse != nullptr, names, s_part);
-    if (threadIdx.x == 0) stats[row * pieces + blockIdx.x % pieces] = s;
+    float top[1], sum[2] = {};
+    if (REST) {
+        names.template clear<kThreads>();
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j) s_row[j * kThreads + threadIdx.x] = held.raw[j];
+    }
+    top[0] = held.top();
+    over_workgroup<kThreads>(top, s_top, Max{});
+    const float base = base_of(top[0]), by = d.rate * kLog2e;
+    if (REST) {
+        for (int k = threadIdx.x; k < d.K; k += kThreads) {
+            const int64_t at = d.ids[row * d.K + k] - begin;
+            if (at < 0 || at >= count) continue;
+            if (names.add((int)at)) sum[1] += __builtin_amdgcn_exp2f((as_float(piece[at]) - base) * by);
+            reinterpret_cast<T*>(s_row)[at + skew] = as_value<T>(-kInf);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j) held.raw[j] = s_row[j * kThreads + threadIdx.x];
+    }
+    sum[0] = held.sum(base, by);
+    over_workgroup<kThreads>(sum, s_sum, Add{});
+    if (threadIdx.x == 0) stats[row * pieces + blockIdx.x % pieces] = Stats{top[0], sum[0] + sum[1], sum[0]};
 }
-template <typename T>
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, unsigned pieces, unsigned written, const Stats* stats, float* rows, T* dlogits) {
-    constexpr int NV = kVectors<T>;
-    __shared__ Names<kPieceBytes / (int)sizeof(T)> names;
-    __shared__ int32_t s_id[kMostIds];
-    __shared__ float s_p[kMostIds], s_part[16];
-    __shared__ int s_twice;
+    using H = Held<T, kThreads, kVectors>;
+    extern __shared__ float s_mem[];
+    __shared__ Names<kThreads * H::N> names;
+    __shared__ float s_top[2][16], s_lse[1][16], s_sum[6][16];
+    const Ids ids(s_mem, d.K);
     const int64_t row = d.first + blockIdx.x / written, begin = (int64_t)(blockIdx.x % written) * kPiece<T>;
     const int count = (int)min(d.V - begin, (int64_t)kPiece<T>);
     const float weight = d.weight ? d.weight[row] : 1.0f;
     if (weight == 0.0f) return nothing<T, kThreads>(d, row, begin, count, rows, dlogits);
     const T* const piece = d.logits + row * d.ld + begin;
-    const int skew = Held<T, kThreads, NV>::skew_of(piece);
-    Held<T, kThreads, NV> held;
+    const int skew = H::skew_of(piece);
+    H held;
     if (dlogits) held.read(piece, count, skew);
-    const Teacher t = teach<T, kThreads>(d, row, begin, count, s_id, s_p, names, &s_twice, s_part);
-    if (t.mass == 0.0f && !d.lse) return nothing<T, kThreads>(d, row, begin, count, rows, dlogits);
-    Stats s = {-kInf, 0.0f, 0.0f};
-    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) s.top = fmaxf(s.top, stats[row * pieces + i].top);
-    s.top = over_workgroup<kThreads>(s.top, s_part, Max{});
-    const float base = s.top == -kInf ? 0.0f : s.top;
+    names.template clear<kThreads>();
+    float top[2] = {-kInf, -kInf};
+    top[1] = read_ids<T, kThreads>(d, row, ids);
+    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) top[0] = fmaxf(top[0], stats[row * pieces + i].top);
+    over_workgroup<kThreads>(top, s_top, Max{});
+    const float base = base_of(top[0]);
+    float sum[6] = {};                  // all, others, mass, entropy, score, whether some id of the piece came twice
     for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
         const Stats o = stats[row * pieces + i];
-        const float f = __builtin_amdgcn_exp2f((o.top == -kInf ? 0.0f - base : o.top - base) * d.rate * kLog2e);
-        s.all += f * o.all;
-        s.others += f * o.others;
+        const float f = __builtin_amdgcn_exp2f((base_of(o.top) - base) * d.rate * kLog2e);
+        sum[0] += o.all == 0.0f ? 0.0f : f * o.all;
+        sum[1] += o.others == 0.0f ? 0.0f : f * o.others;
     }
-    s.all = over_workgroup<kThreads>(s.all, s_part, Add{});
-    s.others = over_workgroup<kThreads>(s.others, s_part, Add{});
-    finish(d, held, row, begin, count, skew, t, s, weight, s_id, s_p, names, s_part, begin == 0, rows, dlogits);
+    for (int k = threadIdx.x; k < d.K; k += kThreads) {
+        const int64_t at = ids.id[k] - begin;
+        if (ids.id[k] >= 0 && at >= 0 && at < count && !names.add((int)at)) sum[5] = 1.0f;
+    }
+    float lse;
+    if (d.lse) {
+        lse = d.lse[row];
+    } else {
+        float t[1] = {teacher_sum(d, ids, base_of(top[1]), kThreads)};
+        over_workgroup<kThreads>(t, s_lse, Add{});
+        lse = teacher_lse(base_of(top[1]), t[0]);
+    }
+    const Terms mine = terms_of<T, kThreads>(d, ids, lse, base);
+    sum[2] = mine.mass;
+    sum[3] = mine.entropy;
+    sum[4] = mine.score;
+    over_workgroup<kThreads>(sum, s_sum, Add{});
+    const Terms t = {sum[2], sum[3], sum[4]};
+    if (t.mass == 0.0f && !d.lse) return nothing<T, kThreads>(d, row, begin, count, rows, dlogits);
+    const Stats s = {top[0], sum[0], sum[1]};
+    const float rest = rest_of(d, t.mass);
+    if (threadIdx.x == 0 && begin == 0) rows[row] = weight * loss_of(t, rest, s);
+    if (dlogits) write_grad<STREAM>(d, held, row, begin, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
 }
 
 // Sum of the rows' losses, in a fixed order.
 __global__ void __launch_bounds__(1024) k_distill_sum(const float* rows, int64_t n, float scale, float* loss) {
-    __shared__ float s_part[16];
-    float sum = 0.0f;
+    __shared__ float s_part[1][16];
+    float sum[1] = {};
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < n; i += 1024) sum += rows[i];
-    sum = over_workgroup<1024>(sum, s_part, Add{});
-    if (threadIdx.x == 0) *loss = scale * sum;
+    for (int64_t i = threadIdx.x; i < n; i += 1024) sum[0] += rows[i];
+    over_workgroup<1024>(sum, s_part, Add{});
+    if (threadIdx.x == 0) *loss = scale * sum[0];
 }
 
 // ---- host -------------------------------------------------------------------------------------------------
@@ -350,25 +425,40 @@ int launch(const tns_distill_desc& a, float* loss, float* rows, T* dlogits, void
     constexpr int VEC = 16 / (int)sizeof(T);
     Stats* const stats = reinterpret_cast<Stats*>(static_cast<char*>(workspace) + aligned(a.B * 4));
     if (!rows) rows = static_cast<float*>(workspace);
-    // Launches of at most 2^31 threads, `per` workgroups a row.
-    auto in_pieces = [&](int threads, int64_t per, const auto& go) {
-        const int64_t most = std::max<int64_t>(((int64_t)1 << 31) / threads / per, 1);
-        for (d.first = 0; d.first < a.B; d.first += most) go(dim3((unsigned)(std::min(a.B - d.first, most) * per)));
-    };
-    // As few threads as hold the row in two vectors each (a vector less: where it is not aligned).
+    const size_t lds = ids_bytes(a.K);
     auto row = [&](auto threads, auto vectors) {
-        in_pieces(threads(), 1, [&](dim3 grid) { hipLaunchKernelGGL((k_distill_row<T, threads(), vectors()>), grid, dim3(threads()), 0, stream, d, rows, dlogits); });
+        auto with = [&](auto kernel) {  // launches of at most 2^31 threads
+            const int64_t most = ((int64_t)1 << 31) / threads();
+            for (d.first = 0; d.first < a.B; d.first += most)
+                hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(a.B - d.first, most)), dim3(threads()), lds, stream, d, rows, dlogits);
+        };
+        if (a.d_lse) with(k_distill_row<T, threads(), vectors(), true>);
+        else with(k_distill_row<T, threads(), vectors(), false>);
     };
-    using Two = std::integral_constant<int, 2>;
-    using Four = std::integral_constant<int, 4>;
-    if (a.V <= 64 * 2 * VEC - VEC) row(std::integral_constant<int, 64>{}, Two{});
-    else if (a.V <= 256 * 2 * VEC - VEC) row(std::integral_constant<int, 256>{}, Two{});
-    else if (a.V <= 1024 * 2 * VEC - VEC) row(std::integral_constant<int, 1024>{}, Two{});
-    else if (a.V <= kPiece<T>) row(std::integral_constant<int, 1024>{}, Four{});
+    using std::integral_constant;
+    // (a vector less: where the row is not aligned)
+    if (a.V <= (64 * 1 - 1) * VEC) row(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (a.V <= (64 * 4 - 1) * VEC) row(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (a.V <= (256 * 2 - 1) * VEC) row(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else if (a.V <= (256 * 4 - 1) * VEC) row(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (a.V <= (256 * 6 - 1) * VEC) row(integral_constant<int, 256>{}, integral_constant<int, 6>{});
+    else if (a.V <= (512 * 4 - 1) * VEC) row(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+    else if (a.V <= (512 * 6 - 1) * VEC) row(integral_constant<int, 512>{}, integral_constant<int, 6>{});
     else {
         const unsigned pieces = (unsigned)pieces_of<T>(a.V), written = dlogits ? pieces : 1;
-        in_pieces(kThreads, pieces, [&](dim3 grid) { hipLaunchKernelGGL((k_distill_stats<T>), grid, dim3(kThreads), 0, stream, d, pieces, stats); });
-        in_pieces(kThreads, written, [&](dim3 grid) { hipLaunchKernelGGL((k_distill_grad<T>), grid, dim3(kThreads), 0, stream, d, pieces, written, stats, rows, dlogits); });
+        // Scores beyond the last-level cache (256 MiB) go through in parts that it holds: the second kernel finds there what the first has
+        // read, and writes past it.  200 rows of 500009 fp32 scores, 400 MB: 241 us at once, 225 with the hint on the stores, 213 in parts of
+        // 192 MiB, 228 of 96, 266 of 48 (without the hint 251, 246, 278).
+        const size_t bytes = (size_t)a.B * a.V * sizeof(T);
+        const int64_t parts = bytes > size_t(256) << 20 ? (int64_t)(bytes / (size_t(192) << 20)) + 1 : 1;
+        const int64_t most = std::max<int64_t>(std::min((a.B + parts - 1) / parts, ((int64_t)1 << 31) / kThreads / pieces), 1);
+        for (d.first = 0; d.first < a.B; d.first += most) {
+            const unsigned n = (unsigned)std::min(a.B - d.first, most);
+            if (a.d_lse) hipLaunchKernelGGL((k_distill_stats<T, true>), dim3(n * pieces), dim3(kThreads), 0, stream, d, pieces, stats);
+            else hipLaunchKernelGGL((k_distill_stats<T, false>), dim3(n * pieces), dim3(kThreads), 0, stream, d, pieces, stats);
+            if (parts > 1) hipLaunchKernelGGL((k_distill_grad<T, true>), dim3(n * written), dim3(kThreads), lds, stream, d, pieces, written, stats, rows, dlogits);
+            else hipLaunchKernelGGL((k_distill_grad<T, false>), dim3(n * written), dim3(kThreads), lds, stream, d, pieces, written, stats, rows, dlogits);
+        }
     }
     hipLaunchKernelGGL(k_distill_sum, dim3(1), dim3(1024), 0, stream, rows, a.B, d.scale, loss);
     return launched("tns_distill");
