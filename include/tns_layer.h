@@ -40,7 +40,7 @@ extern "C" {
  *   flags             TNS_NEWEST_FIRST: a list's first row is its newest event (of account without d_ts only).  TNS_ZERO_BEYOND: the
  *                     rows from d_rowptr[S] on of d_dk and d_dv are written as zeros; otherwise they are not written
  *   d_q               T [S, heads, head_dim], ld_q elements from one target to the next (>= heads * head_dim); aligned to T
- *   d_k, d_v          T [rows or num, kv_heads, head_dim], ld_k / ld_v from one row to the next
+ *   d_k, d_v          T [rows or num, kv_heads, head_dim], ld_k / ld_v from one row to the next, < 2^22
  *   d_index[rows]     row of k and v that holds the event's; may be NULL (row i holds event i's)
  *   d_mask[rows]      bytes, 0: the event is left out; may be NULL
  *   d_t[S], d_ts[rows]   times of the targets and of the events; both or neither

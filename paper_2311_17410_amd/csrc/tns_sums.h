@@ -46,13 +46,37 @@ __device__ __forceinline__ float over_lanes(float v, int n, const Op& op) {
     if (n > 32) v = with_neighbour<32>(v, op);
     return v;
 }
-// Over the lanes that have the same number modulo n: mirrored halves would pair other ones, so these go by shuffles up to 16 apart.
+// The value of the lane BY below in a row of sixteen, going round.
+template <int BY>
+__device__ __forceinline__ float row_turned(float v) { return moved_lane<0x120 + BY>(v); }
+// Over the lanes of a row of sixteen that have the same number modulo n: from half a row down, so that what is turned has the turn's period.
+template <typename Op>
+__device__ __forceinline__ float over_row_strided(float v, int n, const Op& op) {
+    if (n <= 8) v = op(v, row_turned<8>(v));
+    if (n <= 4) v = op(v, row_turned<4>(v));
+    if (n <= 2) v = op(v, row_turned<2>(v));
+    if (n <= 1) v = op(v, row_turned<1>(v));
+    return v;
+}
+// Over the lanes that have the same number modulo n.
 template <typename Op>
 __device__ __forceinline__ float over_strided(float v, int n, const Op& op) {
-    for (int by = n; by < 16; by *= 2) v = op(v, __shfl_xor(v, by));
+    v = over_row_strided(v, n, op);
     if (n <= 16) v = with_neighbour<16>(v, op);
     if (n <= 32) v = with_neighbour<32>(v, op);
     return v;
+}
+// Two sums for the price of one: over the lanes 16 (32) apart, `a` for those in even rows (the lower half), `b` for the others.
+template <int BY>
+__device__ __forceinline__ float add_either(float a, float b) {
+    static_assert(BY == 16 || BY == 32);
+    if constexpr (BY == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
 }
 
 }  // namespace

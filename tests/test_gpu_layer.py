@@ -747,3 +747,53 @@ def test_within_autograd(L):
         assert float((m.grad.double() - w.grad).abs().max()) < 1e3 * 2 ** -24 * float(w.grad.abs().max())
     with pytest.raises(ValueError, match="autograd"):
         L.block_run(mine[4], mine[4])
+
+
+# ---- many lists ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype, heads, kv_heads, dim, lists", [(F32, 1, 1, 256, 2500), (F32, 2, 2, 50, 4200), (BF16, 2, 2, 64, 8300), (BF16, 3, 3, 40, 4200), (F32, 4, 2, 7, 8300), (BF16, 8, 1, 60, 16500),
+                                                                (F32, 1, 1, 15, 33000), (BF16, 40, 20, 32, 1100)])
+@pytest.mark.parametrize("times, newest_first", [(True, True), (False, False)])
+def test_attend_many_lists(L, dtype, heads, kv_heads, dim, lists, times, newest_first):
+    """So many lists that brief ones are taken several a wave: some empty, some of 63 to 66 events, some far longer, the last wave's not full."""
+    rng = np.random.default_rng(lists + heads)
+    lens = np.minimum(rng.geometric(0.15, lists) - 1, 12)
+    lens[rng.integers(0, lists, 12)] = [63, 64, 65, 66, 100, 300, 700, 31, 32, 33, 17, 16]
+    lens[-1] = 40
+    a = the_events(rng, lens, heads, kv_heads, dim, dtype, buckets=5, times=times, masked=0.2, newest_first=newest_first)
+    check_attend(L, a, dtype)
+
+
+@pytest.mark.parametrize("dtype, dim, lists", [(F32, 64, 4200), (BF16, 50, 8300)])
+def test_attend_many_lists_gathered(L, dtype, dim, lists):
+    rng = np.random.default_rng(lists)
+    lens = np.minimum(rng.geometric(0.15, lists) - 1, 12)
+    lens[rng.integers(0, lists, 4)] = [64, 65, 500, 33]
+    a = the_events(rng, lens, 2, 2, dim, dtype, masked=0.1)
+    n, nodes = int(a["rowptr"][-1]), 300
+    a["index"] = rng.integers(-20, nodes + 20, n).astype(np.int32)
+    a["k"], a["v"] = values(rng, (nodes, 2, dim), dtype), values(rng, (nodes, 2, dim), dtype)
+    want = O.attend(**a)
+    close("out", L.attend_run(**on_gpu(a, dtype))["out"], want["out"], want["out_off"], dtype)
+
+
+def test_attend_many_lists_ruled_out_buckets_and_rows_beyond(L):
+    """Brief lists several a wave: buckets that are ruled out for some heads of a group, rows that no list holds, the same bits again."""
+    import torch
+    rng = np.random.default_rng(31)
+    lens = np.minimum(rng.geometric(0.2, 9000) - 1, 12)
+    a = the_events(rng, lens, 4, 2, 16, F32, buckets=4, times=False)
+    a["edges"] = np.float32([1, 2, 5])
+    a["table"][0, 1] = a["table"][2, 2] = a["table"][3] = -np.inf
+    dout = values(rng, a["q"].shape, F32)
+    r, d = check_attend(L, a, F32, dout)
+    g = on_gpu(a, F32)
+    n = int(a["rowptr"][-1])
+    for name in ("k", "v"):
+        g[name] = torch.cat((g[name], torch.full((777, 2, 16), float("nan"), device="cuda")))
+    again = L.attend_run(**g, save=True)
+    assert torch.equal(again["out"], r["out"])
+    back = L.attend_grad(**g, saved=again["saved"], dout=torch_of(dout))
+    for name in ("dk", "dv"):
+        assert torch.equal(back[name][:n], d[name]) and not back[name][n:].any()
+    assert torch.equal(back["dq"], d["dq"])
