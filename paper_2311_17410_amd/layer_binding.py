@@ -35,13 +35,13 @@ class tns_distill_desc(C.Structure):
                 ("d_weight", _vp), ("temperature", _f64), ("scale", _f64)]
 
 
-_ready = False
+_ready = None
 
 
 def lib():
     global _ready
-    L = _lib()
-    if not _ready:
+    if _ready is None:
+        L = _lib()
         size_p = C.POINTER(C.c_size_t)
         L.tns_attend_workspace.argtypes = [C.POINTER(tns_attend), size_p, size_p, size_p]
         L.tns_attend_run.argtypes = [C.POINTER(tns_attend), _at, _at, _at, C.c_size_t, _at]
@@ -53,8 +53,8 @@ def lib():
         L.tns_distill.argtypes = [C.POINTER(tns_distill_desc), _at, _at, _at, _at, C.c_size_t, _at]
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
-        _ready = True
-    return L
+        _ready = L
+    return _ready
 
 
 # ---- the C functions -----------------------------------------------------------------------------
@@ -112,13 +112,16 @@ _block_bytes = functools.lru_cache(maxsize=1024)(tns_block_workspace)
 _distill_bytes = functools.lru_cache(maxsize=1024)(tns_distill_workspace)
 
 
-def _heads(name, t, rows, heads, dim, like):
+def _heads(name, t, shape, like):
     """The address and the row stride of a tensor [rows, heads, dim] whose rows may lie apart."""
-    if t.dtype is not like.dtype or t.shape != (rows, heads, dim) or t.device != like.device:
-        raise ValueError(f"{name}: {like.dtype} of shape {(rows, heads, dim)} on {like.device} is wanted, not {t.dtype} of {tuple(t.shape)} on {t.device}")
-    if not ((t.stride(2) == 1 or dim <= 1) and (t.stride(1) == dim or heads <= 1)) and t.numel():
+    if t.dtype is not like.dtype or t.shape != shape or t.device != like.device:
+        raise ValueError(f"{name}: {like.dtype} of shape {shape} on {like.device} is wanted, not {t.dtype} of {tuple(t.shape)} on {t.device}")
+    rows, heads, dim = shape
+    if t.is_contiguous() or rows <= 1 and t[0].is_contiguous():
+        return t.data_ptr(), heads * dim
+    if not ((t.stride(2) == 1 or dim <= 1) and (t.stride(1) == dim or heads <= 1)):
         raise ValueError(f"{name}: the heads of a row and their channels have to lie side by side")
-    return t.data_ptr(), heads * dim if rows <= 1 else t.stride(0)
+    return t.data_ptr(), t.stride(0)
 
 
 def _described(rowptr, q, k, v, t, ts, edges, table, index, mask, scale, newest_first):
@@ -126,7 +129,7 @@ def _described(rowptr, q, k, v, t, ts, edges, table, index, mask, scale, newest_
     if rowptr.dim() != 1 or rowptr.shape[0] < 1 or q.dim() != 3 or k.dim() != 3:
         raise ValueError("rowptr has the shape [lists + 1], q [lists, heads, head_dim], k and v [rows, kv_heads, head_dim]")
     dev, f32 = q.device, torch.float32
-    S, have, (heads, dim), kv_heads = rowptr.shape[0] - 1, k.shape[0], q.shape[1:], k.shape[1]
+    S, (_, heads, dim), (have, kv_heads, _) = rowptr.shape[0] - 1, q.shape, k.shape
     rows = index.shape[0] if index is not None else have
     buckets = 0 if table is None else table.shape[0]
     if mask is not None and mask.dtype is torch.bool:
@@ -135,9 +138,9 @@ def _described(rowptr, q, k, v, t, ts, edges, table, index, mask, scale, newest_
         raise ValueError("edges without a table")
     if (edges is None) != (buckets <= 1) and not (buckets == 1 and edges.numel() == 0):
         raise ValueError("edges: one fewer than the rows of the table")
-    p_q, ld_q = _heads("q", q, S, heads, dim, q)
-    p_k, ld_k = _heads("k", k, have, kv_heads, dim, q)
-    p_v, ld_v = _heads("v", v, have, kv_heads, dim, q)
+    p_q, ld_q = _heads("q", q, (S, heads, dim), q)
+    p_k, ld_k = _heads("k", k, (have, kv_heads, dim), q)
+    p_v, ld_v = _heads("v", v, (have, kv_heads, dim), q)
     return tns_attend(S, rows, have if index is not None else 0, heads, kv_heads, dim, _dtype_of(q), buckets, TNS_ZERO_BEYOND | (TNS_NEWEST_FIRST if newest_first else 0),
                       _want("rowptr", rowptr, (S + 1,), torch.int64, dev), p_q, p_k, p_v, ld_q, ld_k, ld_v, _want("index", index, (rows,), torch.int32, dev),
                       _want("mask", mask, (rows,), torch.uint8, dev), _want("t", t, (S,), f32, dev), _want("ts", ts, (rows,), f32, dev),
@@ -161,7 +164,9 @@ def attend_run(rowptr, q, k, v, t=None, ts=None, edges=None, table=None, index=N
     out = dict(out=q.new_empty((a.S, a.heads, a.head_dim)), saved=q.new_empty(saved, dtype=torch.uint8) if save else None)
     ws = q.new_empty(run, dtype=torch.uint8)
     with on:
-        tns_attend_run(a, out["out"].data_ptr(), out["saved"].data_ptr() if save else 0, ws.data_ptr(), run, stream)
+        rc = lib().tns_attend_run(C.byref(a), out["out"].data_ptr(), out["saved"].data_ptr() if save else 0, ws.data_ptr(), run, stream)
+    if rc:
+        _check(rc, "tns_attend_run")
     return out
 
 
@@ -203,7 +208,9 @@ def block_run(x, branch, gate=None, scale=None, post=None, pre=None, eps=1e-6, c
     b = _between(x, branch, gate, scale, post, pre, eps, center)
     out = dict(out=x.new_empty(x.shape), next=None if pre is None else x.new_empty(x.shape))
     with on:
-        tns_block_run(b, out["out"].data_ptr(), 0 if pre is None else out["next"].data_ptr(), stream)
+        rc = lib().tns_block_run(C.byref(b), out["out"].data_ptr(), 0 if pre is None else out["next"].data_ptr(), stream)
+    if rc:
+        _check(rc, "tns_block_run")
     return out
 
 
@@ -242,5 +249,7 @@ def distill(logits, ids, teacher, lse=None, weight=None, temperature=1.0, scale=
     out = dict(loss=logits.new_empty((), dtype=f32), rows=logits.new_empty(B, dtype=f32), dlogits=logits.new_empty((B, V)) if grad else None)
     ws = logits.new_empty(need, dtype=torch.uint8)
     with on:
-        tns_distill(d, out["loss"].data_ptr(), out["rows"].data_ptr(), out["dlogits"].data_ptr() if grad else 0, ws.data_ptr(), need, stream)
+        rc = lib().tns_distill(C.byref(d), out["loss"].data_ptr(), out["rows"].data_ptr(), out["dlogits"].data_ptr() if grad else 0, ws.data_ptr(), need, stream)
+    if rc:
+        _check(rc, "tns_distill")
     return out
