@@ -79,20 +79,40 @@ struct Part {
     bool whole;                         // the list has no other part
 };
 
-// The list that holds row p < total: the last one that begins at or before it.  Called by the whole wave, which looks at 64 lists a step.
-// (What a ballot votes on is computed without branches.)
+// The lists that hold the K rows p[] < total: the last ones that begin at or before them.  Called by the whole wave, which looks at 64 lists a step, for
+// all K at once.  (What a ballot votes on is computed without branches.)
+template <int K, typename T>
+__device__ void find_lists(const Attend<T>& a, const int64_t (&p)[K], int64_t (&list)[K]) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo[K], hi[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        lo[k] = 0;
+        hi[k] = a.S;
+    }
+    for (int64_t wide = a.S; wide > 1;) {
+        const int64_t by = (wide + kWave - 1) / kWave;
+        int64_t at[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) at[k] = a.rowptr[min(lo[k] + (lane + 1) * by, hi[k])];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int64_t j = lo[k] + (lane + 1) * by;
+            const int c = __popcll(__ballot((j < hi[k]) & (min(max(at[k], (int64_t)0), a.rows) <= p[k])));
+            lo[k] += c * by;
+            hi[k] = min(lo[k] + by, hi[k]);
+        }
+        wide = by;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) list[k] = uniform(lo[k]);
+}
 template <typename T>
 __device__ int64_t find_list(const Attend<T>& a, int64_t p) {
-    const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = a.S;
-    while (hi - lo > 1) {
-        const int64_t by = (hi - lo + kWave - 1) / kWave, j = lo + (lane + 1) * by;
-        const int64_t at = min(max(a.rowptr[min(j, hi)], (int64_t)0), a.rows);
-        const int c = __popcll(__ballot((j < hi) & (at <= p)));
-        lo += c * by;
-        hi = min(lo + by, hi);
-    }
-    return uniform(lo);
+    const int64_t row[1] = {p};
+    int64_t list[1];
+    find_lists(a, row, list);
+    return list[0];
 }
 
 // A list's edges as they lie in memory, the lane's or the wave's.
@@ -114,7 +134,8 @@ struct Walk {
     int64_t next, block, from = 0, stride;     // next: list of lane 0 when 64 more are looked at; from: that of those that were
     uint64_t left = 0;                  // of the 64, a bit each
     Edges edges;                        // lane i's: of list from + i stride
-    __device__ Walk(int64_t begin, int64_t stride) : next(begin), block(begin), stride(stride) {}
+    // (Waves that have no list, or one fewer, are the last ones: they begin with the blocks.)
+    __device__ Walk(int64_t begin, int64_t stride) : next(begin), block(stride - 1 - begin), stride(stride) {}
 
     // The next part, false if there is none.  For every block it also says (`first`) which list that is cut has its first part there, or -1, and calls
     // beyond(block).
@@ -147,14 +168,17 @@ struct Walk {
             int32_t starts = -1;
             bool any = false;
             const int64_t total = a.total();
-            if (w.begin + size < total) {      // the list that goes on behind the block, and whether it begins in it
-                const int64_t list = find_list(a, w.begin + size), from = a.edge(list), to = a.edge(list + 1);
-                if (from >= w.begin && from < w.begin + size && to - from > size) starts = (int32_t)list;
-            }
             if (w.begin < total) {
-                w.list = find_list(a, w.begin);
-                w.list_begin = a.edge(w.list);
-                w.list_end = a.edge(w.list + 1);
+                const int64_t row[2] = {w.begin, min(w.begin + size, total - 1)};
+                int64_t list[2];
+                find_lists(a, row, list);
+                Edges here(a, list[0]), on(a, list[1]);      // of the list that the block begins in, and of the one that goes on behind it
+                here.tidy(a);
+                on.tidy(a);
+                if (w.begin + size < total && uniform(on.begin) >= w.begin && uniform(on.begin) < w.begin + size && uniform(on.end - on.begin) > size) starts = (int32_t)list[1];
+                w.list = list[0];
+                w.list_begin = uniform(here.begin);
+                w.list_end = uniform(here.end);
                 w.end = min(w.list_end, w.begin + size);
                 w.whole = false;
                 any = w.list_begin < w.begin && w.begin < w.list_end && w.list_end - w.list_begin > size;

@@ -217,36 +217,45 @@ __global__ void __launch_bounds__(1024) k_attend_join(const Attend<T> a, const C
             if (end - block > kMany) continue;
             for (int c0 = 0; c0 < all; c0 += kOwn * kWave) {
                 __syncthreads();
+                int c[kOwn], h[kOwn];
+                float top[kOwn], l[kOwn] = {}, acc[kOwn] = {};
 #pragma unroll
                 for (int j = 0; j < kOwn; ++j) {
-                    const int c = min(c0 + j * kWave + lane, all - 1), h = c / a.dim;
-                    float top = -kInf, l = 0.0f, acc = 0.0f;
-#pragma unroll 4
-                    for (int64_t b = block + wave; b < end; b += 16) {
-                        const int64_t at = slot_of(b, block, cut);
-                        const float m = work.stats[2 * (at * a.heads + h)], n = work.stats[2 * (at * a.heads + h) + 1], v = work.acc[at * all + c];
-                        const float both = fmaxf(top, m), base = both == -kInf ? 0.0f : both, keep = __builtin_amdgcn_exp2f(top - base), f = __builtin_amdgcn_exp2f(m - base);
-                        l = keep * l + f * n;
-                        acc = keep * acc + f * v;
-                        top = both;
+                    c[j] = min(c0 + j * kWave + lane, all - 1);
+                    h[j] = c[j] / a.dim;
+                    top[j] = -kInf;
+                }
+#pragma unroll 2
+                for (int64_t b = block + wave; b < end; b += 16) {
+                    const int64_t at = slot_of(b, block, cut);
+#pragma unroll
+                    for (int j = 0; j < kOwn; ++j) {
+                        const float m = work.stats[2 * (at * a.heads + h[j])], n = work.stats[2 * (at * a.heads + h[j]) + 1], v = work.acc[at * all + c[j]];
+                        const float both = fmaxf(top[j], m), base = both == -kInf ? 0.0f : both, keep = __builtin_amdgcn_exp2f(top[j] - base), f = __builtin_amdgcn_exp2f(m - base);
+                        l[j] = keep * l[j] + f * n;
+                        acc[j] = keep * acc[j] + f * v;
+                        top[j] = both;
                     }
-                    s_top[wave][j * kWave + lane] = top;
-                    s_l[wave][j * kWave + lane] = l;
-                    s_acc[wave][j * kWave + lane] = acc;
+                }
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) {
+                    s_top[wave][j * kWave + lane] = top[j];
+                    s_l[wave][j * kWave + lane] = l[j];
+                    s_acc[wave][j * kWave + lane] = acc[j];
                 }
                 __syncthreads();
-                const int c = c0 + (int)threadIdx.x;
-                if ((int)threadIdx.x >= kOwn * kWave || c >= all) continue;
-                float top = -kInf, l = 0.0f, acc = 0.0f;
+                const int mine = c0 + (int)threadIdx.x;
+                if ((int)threadIdx.x >= kOwn * kWave || mine >= all) continue;
+                float most = -kInf, sum = 0.0f, value = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s_top[i][threadIdx.x]);
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, s_top[i][threadIdx.x]);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float m = s_top[i][threadIdx.x], f = m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-                    l += f * s_l[i][threadIdx.x];
-                    acc += f * s_acc[i][threadIdx.x];
+                    const float m = s_top[i][threadIdx.x], f = m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m - most);
+                    sum += f * s_l[i][threadIdx.x];
+                    value += f * s_acc[i][threadIdx.x];
                 }
-                write(list, c / a.dim, c % a.dim, top, l, acc);
+                write(list, mine / a.dim, mine % a.dim, most, sum, value);
             }
         }
         return;

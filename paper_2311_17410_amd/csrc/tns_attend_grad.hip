@@ -260,21 +260,22 @@ __global__ void __launch_bounds__(1024) k_attend_grad_join(const Attend<T> a, co
             if (end - block > kMany) continue;
             for (int c0 = 0; c0 < all; c0 += kOwn * kWave) {
                 __syncthreads();
-#pragma unroll
-                for (int j = 0; j < kOwn; ++j) {
-                    const int c = min(c0 + j * kWave + lane, all - 1);
-                    float acc = 0.0f;
+                float acc[kOwn] = {};
 #pragma unroll 4
-                    for (int64_t b = block + wave; b < end; b += 16) acc += work.acc[slot_of(b, block, cut) * all + c];
-                    s_acc[wave][j * kWave + lane] = acc;
-                }
-                __syncthreads();
-                const int c = c0 + (int)threadIdx.x;
-                if ((int)threadIdx.x >= kOwn * kWave || c >= all) continue;
-                float acc = 0.0f;
+                for (int64_t b = block + wave; b < end; b += 16) {
+                    const float* const row = work.acc + slot_of(b, block, cut) * all;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc += s_acc[i][threadIdx.x];
-                dq[list * all + c] = as_value<T>(acc);
+                    for (int j = 0; j < kOwn; ++j) acc[j] += row[min(c0 + j * kWave + lane, all - 1)];
+                }
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) s_acc[wave][j * kWave + lane] = acc[j];
+                __syncthreads();
+                const int mine = c0 + (int)threadIdx.x;
+                if ((int)threadIdx.x >= kOwn * kWave || mine >= all) continue;
+                float value = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) value += s_acc[i][threadIdx.x];
+                dq[list * all + mine] = as_value<T>(value);
             }
         }
         return;

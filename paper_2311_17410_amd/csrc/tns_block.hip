@@ -46,27 +46,26 @@ template <typename T, int VEC, int G, int NV>
 struct Team {
     static constexpr int THREADS = G > 256 ? G : 256, ROWS = THREADS / G, N = VEC * NV;
     int at[NV];
-    bool there[NV];
+    bool there[NV], whole;              // whole: every lane has all its channels
 
-    __device__ Team(int dim) {
+    __device__ Team(int dim) : whole(dim == G * N) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             at[j] = (j * G + (int)(threadIdx.x % G)) * VEC;
             there[j] = at[j] < dim;
         }
     }
-    __device__ __forceinline__ void read(const T* row, bool is, Vec<T, VEC> (&to)[NV]) const {
+    // (Without branches, so that all arrays' rows are on their way at once: lanes beyond the row read its first channels.)
+    __device__ __forceinline__ void read(const T* row, Vec<T, VEC> (&to)[NV]) const {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            to[j] = Vec<T, VEC>{};
-            if (is && there[j]) to[j] = *reinterpret_cast<const Vec<T, VEC>*>(row + at[j]);
-        }
+        for (int j = 0; j < NV; ++j) to[j] = *reinterpret_cast<const Vec<T, VEC>*>(row + (there[j] ? at[j] : 0));
     }
-    __device__ __forceinline__ static void widen(const Vec<T, VEC> (&v)[NV], float (&to)[N]) {
+    // Values of a row that `is`, zero beyond it.
+    __device__ __forceinline__ void widen(const Vec<T, VEC> (&v)[NV], bool is, float (&to)[N]) const {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) to[j * VEC + i] = as_float(v[j].v[i]);
+            for (int i = 0; i < VEC; ++i) to[j * VEC + i] = is && there[j] ? as_float(v[j].v[i]) : 0.0f;
     }
     __device__ __forceinline__ void write(T* row, bool is, const float (&v)[N]) const {
 #pragma unroll
@@ -137,7 +136,9 @@ struct Team {
     }
 };
 
-template <typename T, int VEC, int G, int NV>
+// Bound by memory: a million rows of 128 fp32 channels without a gate, 2.05 GB in 395 us (5.2 TB/s); 66600 of 172 bf16, 115 MB in 29 us (3.9): there
+// the instructions of sums and gates are as many as memory leaves time for.
+template <typename T, int VEC, int G, int NV, bool GATE>
 __global__ void __launch_bounds__(G > 256 ? G : 256) k_block(const Block<T> b, T* out, T* next) {
     using Rows = Team<T, VEC, G, NV>;
     constexpr int N = Rows::N;
@@ -148,26 +149,37 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) k_block(const Block<T> b, T
     team.weights(b.pre, pre);
 #pragma unroll
     for (int i = 0; i < N; ++i) factor[i] *= other[i];
+    struct Raw {
+        Vec<T, VEC> branch[NV], x[NV], gate[GATE ? NV : 1];
+    };
+    auto read = [&](int64_t row, Raw& raw) {
+        row = min(row, b.rows - 1);
+        team.read(b.branch + row * b.ld_branch, raw.branch);
+        team.read(b.x + row * b.ld_x, raw.x);
+        if constexpr (GATE) team.read(b.gate + row * b.ld_gate, raw.gate);
+    };
+    const int64_t stride = (int64_t)gridDim.x * Rows::ROWS;
+    int64_t row = (int64_t)blockIdx.x * Rows::ROWS + threadIdx.x / G;
+    Raw raw;
     // (every lane makes every turn: the sums take all of a wave or workgroup)
-    for (int64_t row0 = (int64_t)blockIdx.x * Rows::ROWS; row0 < b.rows; row0 += (int64_t)gridDim.x * Rows::ROWS) {
-        const int64_t row = row0 + threadIdx.x / G;
+    for (int64_t row0 = (int64_t)blockIdx.x * Rows::ROWS; row0 < b.rows; row0 += stride, row += stride) {
+        read(row, raw);
         const bool is = row < b.rows;
-        Vec<T, VEC> raw_x[NV], raw_b[NV], raw_g[NV];
-        team.read(b.branch + row * b.ld_branch, is, raw_b);
-        team.read(b.x + row * b.ld_x, is, raw_x);
-        if (b.gate) team.read(b.gate + row * b.ld_gate, is, raw_g);
         float v[N], x[N];
-        Rows::widen(raw_b, v);
-        Rows::widen(raw_x, x);
+        team.widen(raw.branch, is, v);
+        team.widen(raw.x, is, x);
         if (b.post) team.norm(b, v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float z = 1.0f, rest;
-            if (b.gate) gate_of(as_float(raw_g[i / VEC].v[i % VEC]), z, rest);
+            if constexpr (GATE) gate_of(as_float(raw.gate[i / VEC].v[i % VEC]), z, rest);
             x[i] += factor[i] * z * v[i];
         }
         team.write(out + row * b.dim, is, x);
         if (b.pre) {
+            if (!team.whole)
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = team.there[i / VEC] ? x[i] : 0.0f;      // (a gate of the first channels' may be no number)
             team.norm(b, x);
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] *= pre[i];
@@ -178,7 +190,9 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) k_block(const Block<T> b, T
 
 // All gradients of a row while it is in registers; norms and gate are computed again.  Every lane adds up its channels' part of the
 // weights' gradients over the rows it sees: of scale and post the same sum, of (gradient by out) sigmoid(gate) norm(branch).
-template <typename T, int VEC, int G, int NV>
+// A gradient that is not there is read from x and not used.  A million rows of 128 fp32 channels, 3.07 GB in 622 us (4.9 TB/s); 66600 of 172 bf16,
+// 183 MB in 42 us (4.4).  The next row read ahead made it slower (645 us: fewer waves), as did more workgroups.
+template <typename T, int VEC, int G, int NV, bool GATE>
 __global__ void __launch_bounds__(G > 256 ? G : 256) k_block_grad(const Block<T> b, const T* dout, int64_t ld_dout, const T* dnext, int64_t ld_dnext, T* dx, T* dbranch, T* dgate, float* shares) {
     using Rows = Team<T, VEC, G, NV>;
     constexpr int N = Rows::N;
@@ -192,35 +206,48 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) k_block_grad(const Block<T>
         factor[i] *= other[i];
         both[i] = of_pre[i] = 0.0f;
     }
-    for (int64_t row0 = (int64_t)blockIdx.x * Rows::ROWS; row0 < b.rows; row0 += (int64_t)gridDim.x * Rows::ROWS) {
-        const int64_t row = row0 + threadIdx.x / G;
+    struct Raw {
+        Vec<T, VEC> branch[NV], gate[GATE ? NV : 1], x[NV], dout[NV], dnext[NV];
+    };
+    const T *const from_out = dout ? dout : b.x, *const from_next = dnext ? dnext : b.x;
+    const int64_t ld_out = dout ? ld_dout : b.ld_x, ld_next = dnext ? ld_dnext : b.ld_x;
+    auto read = [&](int64_t row, Raw& raw) {
+        row = min(row, b.rows - 1);
+        team.read(b.branch + row * b.ld_branch, raw.branch);
+        if constexpr (GATE) team.read(b.gate + row * b.ld_gate, raw.gate);
+        team.read(b.x + row * b.ld_x, raw.x);
+        team.read(from_out + row * ld_out, raw.dout);
+        team.read(from_next + row * ld_next, raw.dnext);
+    };
+    const int64_t stride = (int64_t)gridDim.x * Rows::ROWS;
+    int64_t row = (int64_t)blockIdx.x * Rows::ROWS + threadIdx.x / G;
+    Raw raw;
+    for (int64_t row0 = (int64_t)blockIdx.x * Rows::ROWS; row0 < b.rows; row0 += stride, row += stride) {
+        read(row, raw);
         const bool is = row < b.rows;
-        Vec<T, VEC> raw_x[NV], raw_b[NV], raw_g[NV] = {}, raw_o[NV], raw_n[NV];
-        team.read(b.branch + row * b.ld_branch, is, raw_b);
-        if (b.gate) team.read(b.gate + row * b.ld_gate, is, raw_g);
-        team.read(b.x + row * b.ld_x, is && dnext, raw_x);
-        team.read(dout + row * ld_dout, is && dout, raw_o);
-        team.read(dnext + row * ld_dnext, is && dnext, raw_n);
         float y[N], z[N], rest[N], g[N], r = 1.0f;
-        Rows::widen(raw_b, y);
+        team.widen(raw.branch, is, y);
         if (b.post) r = team.norm(b, y);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             z[i] = 1.0f;
             rest[i] = 0.0f;
-            if (b.gate) gate_of(as_float(raw_g[i / VEC].v[i % VEC]), z[i], rest[i]);
+            if constexpr (GATE) {
+                gate_of(as_float(raw.gate[i / VEC].v[i % VEC]), z[i], rest[i]);
+                z[i] = is && team.there[i / VEC] ? z[i] : 0.0f;
+            }
         }
-        Rows::widen(raw_o, g);
+        team.widen(raw.dout, is && dout, g);
         if (dnext) {
             float m[N], d[N];
-            Rows::widen(raw_x, m);
-            Rows::widen(raw_n, d);
+            team.widen(raw.x, is, m);
+            team.widen(raw.dnext, is, d);
 #pragma unroll
             for (int i = 0; i < N; ++i) m[i] += factor[i] * z[i] * y[i];
             const float rm = team.norm(b, m);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                of_pre[i] += d[i] * m[i];
+                of_pre[i] += is ? d[i] * m[i] : 0.0f;      // (a row that is not has a norm of 1 / sqrt(eps))
                 d[i] *= pre[i];
             }
             team.through_norm(b, d, m, rm);
@@ -232,11 +259,11 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) k_block_grad(const Block<T>
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             g[i] *= z[i];
-            both[i] += g[i] * y[i];
+            both[i] += is ? g[i] * y[i] : 0.0f;
             g[i] *= factor[i];
             to_gate[i] = g[i] * y[i] * rest[i];
         }
-        if (b.gate) team.write(dgate + row * b.dim, is, to_gate);
+        if constexpr (GATE) team.write(dgate + row * b.dim, is, to_gate);
         if (b.post) team.through_norm(b, g, y, r);
         team.write(dbranch + row * b.dim, is, g);
     }
@@ -326,30 +353,45 @@ Block<T> typed(const tns_block& b) {
             b.d_scale, b.d_post, b.d_pre, (float)b.eps, 1.0f / (float)b.dim, b.dim, (b.flags & TNS_CENTER) != 0};
 }
 
-// Calls `go` with the type, the channels of a vector, the lanes of a row and the vectors of a lane: as few lanes as hold the row in one vector
-// each, then a wave with eight channels a lane, then workgroups.
+// Calls `go` with the type, the channels of a vector, the lanes of a row and the vectors of a lane.  A sum over a row takes as many steps as its lanes
+// double, whatever they hold, so rows have few lanes of up to kHeld channels before they have more: 66600 rows of 172 bf16 channels in 16 lanes of
+// 12 channels, in 32 of 8, in 64 of 4: outputs 29, 28, 33 us, gradients 42, 50, 59.
+constexpr int kHeld = 12;
 template <typename A, typename F>
 void choose(const tns_block& b, const A& fits, const F& go) {
+    using std::integral_constant;
     auto teams = [&](auto value, auto vec) {
-        constexpr int V = vec(), More = 8 / V;
-        auto with = [&](auto lanes, auto vectors) { go(value, vec, lanes, vectors); };
-        using One = std::integral_constant<int, 1>;
-        using Many = std::integral_constant<int, More>;
-        if (b.dim <= 8 * V) with(std::integral_constant<int, 8>{}, One{});
-        else if (b.dim <= 16 * V) with(std::integral_constant<int, 16>{}, One{});
-        else if (b.dim <= 32 * V) with(std::integral_constant<int, 32>{}, One{});
-        else if (b.dim <= 64 * V) with(std::integral_constant<int, 64>{}, One{});
-        else if (b.dim <= 64 * 8) with(std::integral_constant<int, 64>{}, Many{});
-        else if (b.dim <= 256 * 8) with(std::integral_constant<int, 256>{}, Many{});
-        else with(std::integral_constant<int, 1024>{}, Many{});
+        constexpr int V = vec();
+        const int vectors = (b.dim + V - 1) / V;
+        bool done = false;
+        auto with = [&](auto lanes, auto many) {
+            if constexpr (V * many() <= (lanes() > 64 ? 8 : kHeld)) {
+                if (done || vectors > lanes() * many()) return;
+                done = true;
+                go(value, vec, lanes, many);
+            }
+        };
+        with(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+        auto all = [&](auto lanes) {
+            with(lanes, integral_constant<int, 1>{});
+            with(lanes, integral_constant<int, 2>{});
+            with(lanes, integral_constant<int, 3>{});
+            with(lanes, integral_constant<int, 4>{});
+            if constexpr (V == 1) with(lanes, integral_constant<int, 8>{});
+        };
+        all(integral_constant<int, 16>{});
+        all(integral_constant<int, 32>{});
+        all(integral_constant<int, 64>{});
+        with(integral_constant<int, 256>{}, integral_constant<int, 8 / V>{});
+        with(integral_constant<int, 1024>{}, integral_constant<int, 8 / V>{});
     };
     if (b.dtype == TNS_F32) {
-        if (fits(4)) teams(float{}, std::integral_constant<int, 4>{});
-        else teams(float{}, std::integral_constant<int, 1>{});
+        if (fits(4)) teams(float{}, integral_constant<int, 4>{});
+        else teams(float{}, integral_constant<int, 1>{});
     } else {
-        if (fits(8)) teams(bf16{}, std::integral_constant<int, 8>{});
-        else if (fits(4)) teams(bf16{}, std::integral_constant<int, 4>{});
-        else teams(bf16{}, std::integral_constant<int, 1>{});
+        if (fits(8)) teams(bf16{}, integral_constant<int, 8>{});
+        else if (fits(4)) teams(bf16{}, integral_constant<int, 4>{});
+        else teams(bf16{}, integral_constant<int, 1>{});
     }
 }
 bool fits(const tns_block& b, int n, std::initializer_list<const void*> arrays, int64_t ld_a, int64_t ld_b) {
@@ -383,8 +425,11 @@ int tns_block_run(const tns_block* b, void* d_out, void* d_next, void* hip_strea
     choose(*b, [&](int n) { return fits(*b, n, {b->d_x, b->d_branch, b->d_gate, d_out, d_next}, 0, 0); }, [&](auto value, auto vec, auto lanes, auto vectors) {
         using T = decltype(value);
         using Rows = Team<T, vec(), lanes(), vectors()>;
-        hipLaunchKernelGGL((k_block<T, vec(), lanes(), vectors()>), dim3(groups_of(b->rows, Rows::ROWS, kGroups)), dim3(Rows::THREADS), 0, stream, typed<T>(*b),
-                           static_cast<T*>(d_out), static_cast<T*>(d_next));
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(groups_of(b->rows, Rows::ROWS, kGroups)), dim3(Rows::THREADS), 0, stream, typed<T>(*b), static_cast<T*>(d_out), static_cast<T*>(d_next));
+        };
+        if (b->d_gate) launch(k_block<T, vec(), lanes(), vectors(), true>);
+        else launch(k_block<T, vec(), lanes(), vectors(), false>);
     });
     return launched("tns_block_run");
 }
@@ -425,8 +470,12 @@ int tns_block_grad(const tns_block* b, const void* d_dout, int64_t ld_dout, cons
             using T = decltype(value);
             using Rows = Team<T, vec(), lanes(), vectors()>;
             groups = groups_of(b->rows, Rows::ROWS, kGradGroups);
-            hipLaunchKernelGGL((k_block_grad<T, vec(), lanes(), vectors()>), dim3(groups), dim3(Rows::THREADS), 0, stream, typed<T>(*b), static_cast<const T*>(d_dout), ld_dout,
-                               static_cast<const T*>(d_dnext), ld_dnext, static_cast<T*>(d_dx), static_cast<T*>(d_dbranch), static_cast<T*>(d_dgate), sums ? shares : nullptr);
+            auto launch = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3(groups), dim3(Rows::THREADS), 0, stream, typed<T>(*b), static_cast<const T*>(d_dout), ld_dout, static_cast<const T*>(d_dnext),
+                                   ld_dnext, static_cast<T*>(d_dx), static_cast<T*>(d_dbranch), static_cast<T*>(d_dgate), sums ? shares : nullptr);
+            };
+            if (b->d_gate) launch(k_block_grad<T, vec(), lanes(), vectors(), true>);
+            else launch(k_block_grad<T, vec(), lanes(), vectors(), false>);
         });
     if (sums)
         hipLaunchKernelGGL(k_block_sums, dim3((b->dim + kChannels - 1) / kChannels), dim3(1024), 0, stream, shares, groups, b->dim, b->d_scale, b->d_post, d_dscale, d_dpost, d_dpre);
