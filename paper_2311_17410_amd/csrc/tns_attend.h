@@ -71,6 +71,7 @@ struct Cut {
     int lanes, wide, slots, turns;      // powers of two but for turns, the waves that the heads of k and v take (the grid's second dimension)
     int log_lanes, log_width;           // of lanes, and of lanes * wide
     bool exact;                         // every lane of every wave has a head and all its channels
+    int log_copies;                     // of the table's gradient that a wave has, for its slots in turn
     int brief;                          // lists of so many events at most are taken a slot each; -1: none
 };
 struct Part {
@@ -211,11 +212,12 @@ struct Own {
     }
 };
 
-// The lane's sixteen bytes of a row of a head: pieces of VEC channels, the p-th at ((p lanes) + lane) VEC.
+// A lane's sixteen bytes of a row of a head, at any address that is aligned to T: N channels side by side (VEC = N), where a head has no whole number of
+// them the last lane's begin further to the front, so that they end with the row; or one by one (VEC = 1) where a head has fewer.
 template <typename T, int VEC>
 struct Row {
     static constexpr int N = 16 / sizeof(T), PIECES = N / VEC;
-    struct alignas(VEC * sizeof(T)) Piece { T v[VEC]; };
+    struct Piece { T v[VEC]; };
     union {
         Piece piece[PIECES];
         uint32_t word[4];
@@ -239,15 +241,17 @@ struct Row {
     }
     // The lane's part of the product with another row.  Two products of 16 bits and their sum are one instruction, off by 2.4 * 2^-24 of the
     // terms' magnitudes where two rounded sums would be off by 2: measured over values 2^12 apart.
-    __device__ __forceinline__ float dot(const Row& o) const {
+    // MASK: of the channels that are in `mask`, each once for all lanes.
+    template <bool MASK>
+    __device__ __forceinline__ float dot(const Row& o, const uint32_t (&mask)[4]) const {
         float v = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (sizeof(T) == 4) {
-                v += __uint_as_float(word[i]) * __uint_as_float(o.word[i]);
+                v += __uint_as_float(MASK ? word[i] & mask[i] : word[i]) * __uint_as_float(o.word[i]);
             } else {
                 using Pair = __bf16 __attribute__((ext_vector_type(2)));
-                v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, word[i]), __builtin_bit_cast(Pair, o.word[i]), v, false);
+                v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, MASK ? word[i] & mask[i] : word[i]), __builtin_bit_cast(Pair, o.word[i]), v, false);
             }
         }
         return v;
@@ -255,13 +259,6 @@ struct Row {
     __device__ __forceinline__ void clear_unless(bool keep) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) word[i] = keep ? word[i] : 0u;
-    }
-    // Zeros in the pieces that are not there (they hold those of channel 0, which may be infinite).
-    __device__ __forceinline__ void clear_beyond(const bool (&there)[PIECES]) {
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) piece[p].v[i] = there[p] ? piece[p].v[i] : T{};
     }
     __device__ __forceinline__ void set(const float (&v)[N]) {
         if constexpr (sizeof(T) == 4) {
@@ -301,6 +298,8 @@ struct Place {
     uint32_t at[PIECES];                // bytes of the pieces from the begin of a row of k or v on, those of channel 0 where there are no more (`there`)
     uint32_t in_q[PIECES];              // values from the begin of a row of q on, of the group's first head
     bool there[PIECES];
+    int channel;                        // of the lane's first value (VEC = N)
+    uint32_t mask[4];                   // of the values that no other lane has
 
     __device__ Place(const Attend<T>& a, const Cut& cut, int turn) {
         lane = threadIdx.x & 63;
@@ -312,12 +311,23 @@ struct Place {
         kv = min(kv, a.kv_heads - 1);
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int c = (p * cut.lanes + mine) * VEC;
-            there[p] = EXACT || c < a.dim;
-            at[p] = (uint32_t)(kv * a.dim + (there[p] ? c : 0)) * sizeof(T);
-            in_q[p] = (uint32_t)(kv * a.group * a.dim + (there[p] ? c : 0));
+            const int own = VEC == N ? mine * N : p;
+            there[p] = EXACT || own < a.dim;
+            const int c = VEC == N ? min(own, a.dim - N) : there[p] ? p : 0;
+            at[p] = (uint32_t)(kv * a.dim + c) * sizeof(T);
+            in_q[p] = (uint32_t)(kv * a.group * a.dim + c);
+            if (VEC == N) channel = c;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            constexpr int PER = 4 / sizeof(T);
+            mask[i] = 0;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) mask[i] |= counts(i * PER + k) ? (PER == 1 ? ~0u : 0xffffu << 16 * k) : 0u;
         }
     }
+    // Whether no other lane has the lane's i-th value.
+    __device__ __forceinline__ bool counts(int i) const { return EXACT || (VEC == N ? there[0] && channel + i >= mine * N : there[VEC == N ? 0 : i]); }
     // Rows of the lane's group of heads of an array's list, zero where there is no such head or channel.
     template <int G>
     __device__ __forceinline__ void heads(const Attend<T>& a, const T* list, Row<T, VEC> (&to)[G]) const {
@@ -336,7 +346,7 @@ struct Place {
         for (int g = 0; g < G; ++g)
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                struct alignas(VEC < 4 ? VEC * 4 : 16) Floats { float v[VEC]; } piece = *lane_at<const Floats>(list, (in_q[p] + (uint32_t)(min(g, a.group - 1) * a.dim)) * 4u);
+                struct Floats { float v[VEC]; } piece = *lane_at<const Floats>(list, (in_q[p] + (uint32_t)(min(g, a.group - 1) * a.dim)) * 4u);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) to[g][p * VEC + i] = head && there[p] && g < a.group ? piece.v[i] : 0.0f;
             }
@@ -346,7 +356,7 @@ struct Place {
     __device__ __forceinline__ void write(U* list, int more, const float (&v)[N]) const {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            struct alignas(VEC * sizeof(U) < 16 ? VEC * sizeof(U) : 16) Some { U v[VEC]; } some;
+            struct Some { U v[VEC]; } some;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) some.v[i] = as_value<U>(v[p * VEC + i]);
             if (there[p]) *lane_at<Some>(list, (in_q[p] + (uint32_t)more) * (uint32_t)sizeof(U)) = some;
@@ -361,10 +371,11 @@ struct Place {
             constexpr int R = count();
             if (!head || (lane & 15) >> min(cut.log_width, 4)) return;
             constexpr int STEP = sizeof(T) == 2 && VEC >= 2 && R >= 2 ? 2 : 1;
+            if (VEC == N && !there[0]) return;
 #pragma unroll
             for (int i = 0; i < R; i += STEP) {
-                const int at = first + i, c = ((at / VEC) * cut.lanes + mine) * VEC + at % VEC;
-                if (EXACT || c < a.dim) go((uint32_t)((kv * a.group + g) * a.dim + c), v[i], v[i + STEP - 1], std::integral_constant<int, STEP>{});
+                const int c = VEC == N ? channel + first + i : first + i;
+                if (VEC == N || c < a.dim) go((uint32_t)((kv * a.group + g) * a.dim + c), v[i], v[i + STEP - 1], std::integral_constant<int, STEP>{});
             }
         };
         if (cut.slots == 1) return write(std::integral_constant<int, N>{});
@@ -384,7 +395,7 @@ struct Place {
 // Writes one or two values.
 template <typename U, typename Two>
 __device__ __forceinline__ void put(U* base, uint32_t at, float a, float b, Two) {
-    struct alignas(Two() * sizeof(U) < 4 ? sizeof(U) : 4) Some { U v[Two()]; } some;
+    struct Some { U v[Two()]; } some;
     some.v[0] = as_value<U>(a);
     if constexpr (Two() == 2) some.v[1] = as_value<U>(b);
     *lane_at<Some>(base, at * (uint32_t)sizeof(U)) = some;
@@ -612,10 +623,15 @@ Cut cut_of(const tns_attend& a) {
     c.turns = (a.kv_heads + c.wide - 1) / c.wide;
     c.log_lanes = __builtin_ctz(c.lanes);
     c.exact = c.lanes * n == a.head_dim && a.kv_heads % c.wide == 0;
-    c.brief = c.log_width >= 2 && a.S / c.slots * c.turns >= 2048 ? 64 : -1;
     c.log_width = __builtin_ctz(c.lanes * c.wide);
+    // Blocks: of 64 rows; of fewer where that leaves few of them for the chip, and a call is as long as its blocks; of more where there would be more
+    // than 16384.
     c.part = 6;
+    while (c.part > 4 && ((a.rows * c.turns) >> (c.part - 1)) <= 2048) --c.part;
     while (c.part < 9 && ((a.rows * c.turns) >> c.part) > 16384) ++c.part;
+    c.brief = c.log_width >= 2 && a.S / c.slots * c.turns >= 2048 ? std::min(64, 1 << c.part) : -1;
+    c.log_copies = std::min(__builtin_ctz(c.slots), 3);
+    while (c.log_copies && ((size_t)a.buckets * a.heads * kWaves << c.log_copies) > 4096) --c.log_copies;
     c.blocks = (a.rows + ((int64_t)1 << c.part) - 1) >> c.part;
     return c;
 }
@@ -660,7 +676,7 @@ Layout carve(const tns_attend& a, const Cut& c, bool grad, void* base) {
     return l;
 }
 size_t saved_out_bytes(const tns_attend& a) { return aligned((size_t)a.S * a.heads * a.head_dim * 4); }
-size_t saved_bytes(const tns_attend& a) { return saved_out_bytes(a) + aligned((size_t)a.S * a.heads * 4); }
+inline size_t saved_bytes(const tns_attend& a) { return saved_out_bytes(a) + aligned((size_t)a.S * a.heads * 4); }
 
 template <typename T>
 Attend<T> typed(const tns_attend& a) {
@@ -671,10 +687,10 @@ Attend<T> typed(const tns_attend& a) {
             (a.flags & TNS_NEWEST_FIRST) != 0, (a.flags & TNS_ZERO_BEYOND) != 0, (float)(a.scale * 1.4426950408889634)};
 }
 
-// Calls `go` with the type, the channels that a lane reads at once, the heads that share a key, and the lanes of a head: where rows are read sixteen
-// bytes at a time and no lane is idle the compiler knows them, 0 otherwise.  `fits(n)`: n values at once are aligned everywhere.
-template <typename F, typename A>
-void choose(const tns_attend& a, const Cut& c, const A& fits, const F& go) {
+// Calls `go` with the type, the channels that a lane reads at once, the heads that share a key, and the lanes of a head: where no lane is idle or has
+// another one's channels the compiler knows them, 0 otherwise.
+template <typename F>
+void choose(const tns_attend& a, const Cut& c, const F& go) {
     using std::integral_constant;
     const int group = power_of_two(a.heads / a.kv_heads);
     auto with = [&](auto value, auto vec, auto lanes) {
@@ -683,33 +699,20 @@ void choose(const tns_attend& a, const Cut& c, const A& fits, const F& go) {
         else if (group == 4) go(value, vec, integral_constant<int, 4>{}, lanes);
         else go(value, vec, integral_constant<int, 8>{}, integral_constant<int, 0>{});
     };
-    auto whole = [&](auto value, auto vec) {
-        if (c.exact && c.lanes == 4) with(value, vec, integral_constant<int, 4>{});
-        else if (c.exact && c.lanes == 8) with(value, vec, integral_constant<int, 8>{});
-        else if (c.exact && c.lanes == 16) with(value, vec, integral_constant<int, 16>{});
-        else with(value, vec, integral_constant<int, 0>{});
+    auto of = [&](auto value) {
+        constexpr int N = 16 / (int)sizeof(value);
+        using Whole = integral_constant<int, N>;
+        if (a.head_dim < N) with(value, integral_constant<int, 1>{}, integral_constant<int, 0>{});
+        else if (c.exact && c.lanes == 4) with(value, Whole{}, integral_constant<int, 4>{});
+        else if (c.exact && c.lanes == 8) with(value, Whole{}, integral_constant<int, 8>{});
+        else if (c.exact && c.lanes == 16) with(value, Whole{}, integral_constant<int, 16>{});
+        else with(value, Whole{}, integral_constant<int, 0>{});
     };
-    if (a.dtype == TNS_F32) {
-        if (fits(4)) whole(float{}, integral_constant<int, 4>{});
-        else if (fits(2)) with(float{}, integral_constant<int, 2>{}, integral_constant<int, 0>{});
-        else with(float{}, integral_constant<int, 1>{}, integral_constant<int, 0>{});
-    } else {
-        if (fits(8)) whole(bf16{}, integral_constant<int, 8>{});
-        else if (fits(4)) with(bf16{}, integral_constant<int, 4>{}, integral_constant<int, 0>{});
-        else if (fits(2)) with(bf16{}, integral_constant<int, 2>{}, integral_constant<int, 0>{});
-        else with(bf16{}, integral_constant<int, 1>{}, integral_constant<int, 0>{});
-    }
+    if (a.dtype == TNS_F32) of(float{});
+    else of(bf16{});
 }
 // LDS of a kernel: edges, table, and `more` tables.
 size_t lds_of(const tns_attend& a, int more) { return (size_t)(a.buckets + std::max(a.buckets, 1) * a.heads + more * a.buckets * a.heads) * 4; }
-bool fits(const tns_attend& a, int n, std::initializer_list<const void*> arrays) {
-    const size_t size = a.dtype == TNS_F32 ? 4 : 2;
-    if (a.head_dim % n || (a.S > 1 && a.ld_q % n) || (a.rows > 1 && (a.ld_k % n || a.ld_v % n))) return false;
-    for (const void* p : arrays)
-        if (misaligned(p, n * size)) return false;
-    return true;
-}
-
 int launched(const char* what) {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? (int)TNS_OK : fail_hip(e, what);

@@ -25,11 +25,10 @@ struct Running {
         bool mixed = false;             // an event that is left out by some of the lane's heads only
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!EXACT) b.k[u].clear_beyond(at.there);
             bool some = false, all = true;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const float dot = over_head<LANES>(b.k[u].dot(q[g]), cut.lanes);
+                const float dot = over_head<LANES>(b.k[u].template dot<!EXACT>(q[g], at.mask), cut.lanes);
                 const float bias = s_table[max(bucket[u], 0) * a.heads + at.kv * a.group + min(g, a.group - 1)];
                 const bool counts = bucket[u] >= 0 && bias != -kInf;
                 s[u][g] = counts ? dot * a.scale + bias : -kInf;
@@ -314,7 +313,7 @@ int tns_attend_run(const tns_attend* a, void* d_out, void* d_saved, void* d_work
     float* const saved = static_cast<float*>(d_saved);
     float* const lse = saved ? saved + saved_out_bytes(*a) / 4 : nullptr;
     const size_t lds = lds_of(*a, 0);
-    choose(*a, c, [&](int n) { return fits(*a, n, {a->d_q, a->d_k, a->d_v, d_out}); }, [&](auto value, auto vec, auto group, auto lanes) {
+    choose(*a, c, [&](auto value, auto vec, auto group, auto lanes) {
         using T = decltype(value);
         const Attend<T> t = typed<T>(*a);
         const Args<T> args = {t, c, l.w, static_cast<T*>(d_out), saved, lse, nullptr, nullptr, nullptr, nullptr, 0};

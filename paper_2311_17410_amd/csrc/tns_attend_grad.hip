@@ -34,7 +34,7 @@ struct Back {
             lse[g] = g < a.group ? now.saved_lse[list * a.heads + at.kv * a.group + g] : kInf;
             float dot = 0.0f;
 #pragma unroll
-            for (int i = 0; i < N; ++i) dot += d[g].get(i) * out[g][i];
+            for (int i = 0; i < N; ++i) dot += at.counts(i) ? d[g].get(i) * out[g][i] : 0.0f;
             delta[g] = over_head<LANES>(dot, now.cut.lanes);
         }
     }
@@ -42,10 +42,6 @@ struct Back {
     template <int LANES>
     __device__ __forceinline__ bool take(const Attend<T>& a, const Cut& cut, const Place<T, VEC, EXACT>& at, Row<T, VEC>& k, Row<T, VEC>& v, int bucket, const float* s_table, float scale,
                                          bool (&counts)[G], float (&ds)[G], float (&to_k)[N], float (&to_v)[N]) {
-        if (!EXACT) {
-            k.clear_beyond(at.there);
-            v.clear_beyond(at.there);
-        }
         bool some = false, all = true;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -59,7 +55,7 @@ struct Back {
         const bool careful = G > 1 && __ballot(some && !all) != 0;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const float score = over_head<LANES>(k.dot(q[g]), cut.lanes), dp = over_head<LANES>(v.dot(d[g]), cut.lanes);
+            const float score = over_head<LANES>(k.template dot<!EXACT>(q[g], at.mask), cut.lanes), dp = over_head<LANES>(v.template dot<!EXACT>(d[g], at.mask), cut.lanes);
             const float p = counts[g] ? __builtin_amdgcn_exp2f(score * a.scale + ds[g] - lse[g]) : 0.0f;
             ds[g] = counts[g] ? p * (dp - delta[g]) : 0.0f;
             const float by = ds[g] * scale;
@@ -83,12 +79,12 @@ struct Back {
     }
 };
 
-// Adds to the wave's part of the table's gradient, one slot after the other: the LDS unit takes a wave's requests in order, and those of one slot go
-// to different entries, so the order of the sums is the same every time.
+// Adds to the wave's part of the table's gradient.  Slots take turns, as many at once as the wave has copies of the table: requests of one turn go to
+// different entries, and the LDS unit takes a wave's requests in order, so the order of the sums is the same every time.
 template <typename T, int VEC, int G, bool EXACT>
 __device__ __forceinline__ void add_to_table(const Attend<T>& a, const Cut& cut, const Place<T, VEC, EXACT>& at, int bucket, const bool (&counts)[G], const float (&ds)[G], float* s_mine) {
-    for (int e = 0; e < cut.slots; ++e) {
-        if (at.slot == e && at.head && at.mine == 0)
+    for (int e = 0; e < cut.slots >> cut.log_copies; ++e) {
+        if (at.slot >> cut.log_copies == e && at.head && at.mine == 0)
 #pragma unroll
             for (int g = 0; g < G; ++g)
                 if (counts[g]) __hip_atomic_fetch_add(&s_mine[bucket * a.heads + at.kv * a.group + g], ds[g], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
@@ -106,14 +102,16 @@ __global__ void __launch_bounds__(kWaves* kWave) k_attend_grad(const Args<T>) {
     constexpr int N = Row<T, VEC>::N, U = G == 2 ? 2 : 1, OWN = 1;
     const Args<T>& start = args_now<T>();
     const int entries = start.a.buckets * start.a.heads, wave = uniform((int)(threadIdx.x >> 6));
-    float *const s_edges = s_mem, *const s_table = s_mem + start.a.buckets, *const s_sums = s_table + max(entries, start.a.heads), *const s_mine = s_sums + wave * entries;
+    float *const s_edges = s_mem, *const s_table = s_mem + start.a.buckets, *const s_sums = s_table + max(entries, start.a.heads);
     const int64_t stride = (int64_t)gridDim.x * kWaves, begin = (int64_t)blockIdx.x * kWaves + wave;
     const Place<T, VEC, EXACT> at(start.a, start.cut, blockIdx.y);
+    const int copies = kWaves << start.cut.log_copies;
+    float* const s_mine = s_sums + ((wave << start.cut.log_copies) + (at.slot & ((1 << start.cut.log_copies) - 1))) * entries;      // the slot's
     const int log_slots = 6 - start.cut.log_width, lane0 = at.lane & ~((1 << start.cut.log_width) - 1);
     Edges edges;
     if (start.cut.brief >= 0) edges = Edges(start.a, (begin << log_slots) + at.slot);
     if (start.tables)
-        for (int i = threadIdx.x; i < kWaves * entries; i += kWaves * kWave) s_sums[i] = 0.0f;
+        for (int i = threadIdx.x; i < copies * entries; i += kWaves * kWave) s_sums[i] = 0.0f;
     stage(start.a, s_edges, s_table);
     if (start.cut.brief >= 0)
         for (int64_t group = begin; group << log_slots < args_now<T>().a.S; group += stride) {
@@ -227,8 +225,7 @@ __global__ void __launch_bounds__(kWaves* kWave) k_attend_grad(const Args<T>) {
     const int64_t share = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     for (int i = threadIdx.x; i < entries; i += kWaves * kWave) {
         float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) sum += s_sums[k * entries + i];
+        for (int k = 0; k < copies; ++k) sum += s_sums[k * entries + i];
         last.work.tables[share * entries + i] = sum;
     }
 }
@@ -314,9 +311,9 @@ int tns_attend_grad(const tns_attend* a, const void* d_saved, const void* d_dout
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const float* const saved = static_cast<const float*>(d_saved);
     const float* const lse = saved + saved_out_bytes(*a) / 4;
-    const size_t lds = lds_of(*a, kWaves);
+    const size_t lds = lds_of(*a, kWaves << c.log_copies);
     const unsigned few = few_of(c), sums = (a->buckets * a->heads + kEntries - 1) / kEntries, joins = sums + few + many_of(*a, c);
-    choose(*a, c, [&](int n) { return fits(*a, n, {a->d_q, a->d_k, a->d_v, d_dout, d_dq, d_dk, d_dv}); }, [&](auto value, auto vec, auto group, auto lanes) {
+    choose(*a, c, [&](auto value, auto vec, auto group, auto lanes) {
         using T = decltype(value);
         const Attend<T> t = typed<T>(*a);
         const Args<T> args = {t, c, l.w, nullptr, const_cast<float*>(saved), const_cast<float*>(lse), static_cast<const T*>(d_dout), static_cast<T*>(d_dq),
