@@ -535,7 +535,7 @@ __device__ __forceinline__ void each_batch(B& batch, int n, int by, const Read& 
 
 // ---- lists of several parts ---------------------------------------------------------------------------------
 // A workgroup joins the lists whose first part ends with one of sixteen blocks, one after the other: a wave has every sixteenth part, a lane
-// kOwn channels.  Lists of more than kMany parts are joined by a workgroup for every kSlice channels of a head (a list of that many parts holds a block whose number is a
+// kOwn channels, and every so many channels a workgroup of their own.  Lists of more than kMany parts are joined by a workgroup for every kSlice channels of a head (a list of that many parts holds a block whose number is a
 // multiple of kMany; the first such block stands for it).
 constexpr int kMany = 256, kOwn = 4, kSlice = 16;
 __device__ __forceinline__ int64_t parts_end(int64_t list_end, const Cut& cut) { return min((list_end + ((int64_t)1 << cut.part) - 1) >> cut.part, cut.blocks); }
@@ -652,7 +652,7 @@ int groups_of(const tns_attend& a, const Cut& c, int most) {
     return (int)std::min<int64_t>((a.S + c.blocks + kWaves - 1) / kWaves, std::max(most / c.turns, 1));
 }
 unsigned slices_of(const tns_attend& a) { return (a.head_dim + kSlice - 1) / kSlice; }
-unsigned few_of(const Cut& c) { return c.blocks > 1 ? (unsigned)((c.blocks + 15) / 16) : 0; }
+unsigned few_of(const tns_attend& a, const Cut& c) { return c.blocks > 1 ? (unsigned)((c.blocks + 15) / 16 * ((a.heads * a.head_dim + kOwn * kWave - 1) / (kOwn * kWave))) : 0; }
 unsigned many_of(const tns_attend& a, const Cut& c) { return c.blocks > kMany ? (unsigned)(((c.blocks + kMany - 1) / kMany) * a.heads * slices_of(a)) : 0; }
 
 struct Layout {

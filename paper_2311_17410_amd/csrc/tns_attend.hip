@@ -207,55 +207,54 @@ __global__ void __launch_bounds__(1024) k_attend_join(const Attend<T> a, const C
     if (blockIdx.x < few) {
         __shared__ float s_top[16][kOwn * kWave], s_l[16][kOwn * kWave], s_acc[16][kOwn * kWave];
         const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, all = a.heads * a.dim;
-        const int64_t block0 = (int64_t)blockIdx.x * 16;
+        const int chunks = (all + kOwn * kWave - 1) / (kOwn * kWave), c0 = (int)(blockIdx.x % chunks) * kOwn * kWave;
+        const int64_t block0 = (int64_t)(blockIdx.x / chunks) * 16;
         const int32_t begins = lane < 16 && block0 + lane < cut.blocks ? work.first[block0 + lane] : -1;
         for (uint64_t left = __ballot(begins >= 0); left; left &= left - 1) {
             const int k = __builtin_ctzll(left);
             const int64_t block = block0 + k, list = __builtin_amdgcn_readlane(begins, k);
             const int64_t end = parts_end(a.edge(list + 1), cut);
             if (end - block > kMany) continue;
-            for (int c0 = 0; c0 < all; c0 += kOwn * kWave) {
-                __syncthreads();
-                int c[kOwn], h[kOwn];
-                float top[kOwn], l[kOwn] = {}, acc[kOwn] = {};
+            __syncthreads();
+            int c[kOwn], h[kOwn];
+            float top[kOwn], l[kOwn] = {}, acc[kOwn] = {};
 #pragma unroll
-                for (int j = 0; j < kOwn; ++j) {
-                    c[j] = min(c0 + j * kWave + lane, all - 1);
-                    h[j] = c[j] / a.dim;
-                    top[j] = -kInf;
-                }
-#pragma unroll 2
-                for (int64_t b = block + wave; b < end; b += 16) {
-                    const int64_t at = slot_of(b, block, cut);
-#pragma unroll
-                    for (int j = 0; j < kOwn; ++j) {
-                        const float m = work.stats[2 * (at * a.heads + h[j])], n = work.stats[2 * (at * a.heads + h[j]) + 1], v = work.acc[at * all + c[j]];
-                        const float both = fmaxf(top[j], m), base = both == -kInf ? 0.0f : both, keep = __builtin_amdgcn_exp2f(top[j] - base), f = __builtin_amdgcn_exp2f(m - base);
-                        l[j] = keep * l[j] + f * n;
-                        acc[j] = keep * acc[j] + f * v;
-                        top[j] = both;
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < kOwn; ++j) {
-                    s_top[wave][j * kWave + lane] = top[j];
-                    s_l[wave][j * kWave + lane] = l[j];
-                    s_acc[wave][j * kWave + lane] = acc[j];
-                }
-                __syncthreads();
-                const int mine = c0 + (int)threadIdx.x;
-                if ((int)threadIdx.x >= kOwn * kWave || mine >= all) continue;
-                float most = -kInf, sum = 0.0f, value = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, s_top[i][threadIdx.x]);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float m = s_top[i][threadIdx.x], f = m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m - most);
-                    sum += f * s_l[i][threadIdx.x];
-                    value += f * s_acc[i][threadIdx.x];
-                }
-                write(list, mine / a.dim, mine % a.dim, most, sum, value);
+            for (int j = 0; j < kOwn; ++j) {
+                c[j] = min(c0 + j * kWave + lane, all - 1);
+                h[j] = c[j] / a.dim;
+                top[j] = -kInf;
             }
+#pragma unroll 2
+            for (int64_t b = block + wave; b < end; b += 16) {
+                const int64_t at = slot_of(b, block, cut);
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) {
+                    const float m = work.stats[2 * (at * a.heads + h[j])], n = work.stats[2 * (at * a.heads + h[j]) + 1], v = work.acc[at * all + c[j]];
+                    const float both = fmaxf(top[j], m), base = both == -kInf ? 0.0f : both, keep = __builtin_amdgcn_exp2f(top[j] - base), f = __builtin_amdgcn_exp2f(m - base);
+                    l[j] = keep * l[j] + f * n;
+                    acc[j] = keep * acc[j] + f * v;
+                    top[j] = both;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kOwn; ++j) {
+                s_top[wave][j * kWave + lane] = top[j];
+                s_l[wave][j * kWave + lane] = l[j];
+                s_acc[wave][j * kWave + lane] = acc[j];
+            }
+            __syncthreads();
+            const int mine = c0 + (int)threadIdx.x;
+            if ((int)threadIdx.x >= kOwn * kWave || mine >= all) continue;
+            float most = -kInf, sum = 0.0f, value = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, s_top[i][threadIdx.x]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float m = s_top[i][threadIdx.x], f = m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m - most);
+                sum += f * s_l[i][threadIdx.x];
+                value += f * s_acc[i][threadIdx.x];
+            }
+            write(list, mine / a.dim, mine % a.dim, most, sum, value);
         }
         return;
     }
@@ -324,7 +323,7 @@ int tns_attend_run(const tns_attend* a, void* d_out, void* d_saved, void* d_work
         if constexpr (lanes() == 0) launch(k_attend<T, vec(), group(), 0, 2>, per_cu[2]);
         else if (a->d_index) launch(k_attend<T, vec(), group(), lanes(), 1>, per_cu[1]);
         else launch(k_attend<T, vec(), group(), lanes(), 0>, per_cu[0]);
-        if (const unsigned few = few_of(c))
+        if (const unsigned few = few_of(*a, c))
             hipLaunchKernelGGL((k_attend_join<T>), dim3(few + many_of(*a, c)), dim3(1024), 0, stream, t, c, l.w, few, static_cast<T*>(d_out), saved, lse);
     });
     return launched("tns_attend_run");

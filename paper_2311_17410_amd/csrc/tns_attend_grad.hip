@@ -248,32 +248,31 @@ __global__ void __launch_bounds__(1024) k_attend_grad_join(const Attend<T> a, co
     if (group < few) {
         __shared__ float s_acc[16][kOwn * kWave];
         const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, all = a.heads * a.dim;
-        const int64_t block0 = (int64_t)group * 16;
+        const int chunks = (all + kOwn * kWave - 1) / (kOwn * kWave), c0 = (int)(group % chunks) * kOwn * kWave;
+        const int64_t block0 = (int64_t)(group / chunks) * 16;
         const int32_t begins = lane < 16 && block0 + lane < cut.blocks ? work.first[block0 + lane] : -1;
         for (uint64_t left = __ballot(begins >= 0); left; left &= left - 1) {
             const int k = __builtin_ctzll(left);
             const int64_t block = block0 + k, list = __builtin_amdgcn_readlane(begins, k);
             const int64_t end = parts_end(a.edge(list + 1), cut);
             if (end - block > kMany) continue;
-            for (int c0 = 0; c0 < all; c0 += kOwn * kWave) {
-                __syncthreads();
-                float acc[kOwn] = {};
+            __syncthreads();
+            float acc[kOwn] = {};
 #pragma unroll 4
-                for (int64_t b = block + wave; b < end; b += 16) {
-                    const float* const row = work.acc + slot_of(b, block, cut) * all;
+            for (int64_t b = block + wave; b < end; b += 16) {
+                const float* const row = work.acc + slot_of(b, block, cut) * all;
 #pragma unroll
-                    for (int j = 0; j < kOwn; ++j) acc[j] += row[min(c0 + j * kWave + lane, all - 1)];
-                }
-#pragma unroll
-                for (int j = 0; j < kOwn; ++j) s_acc[wave][j * kWave + lane] = acc[j];
-                __syncthreads();
-                const int mine = c0 + (int)threadIdx.x;
-                if ((int)threadIdx.x >= kOwn * kWave || mine >= all) continue;
-                float value = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) value += s_acc[i][threadIdx.x];
-                dq[list * all + mine] = as_value<T>(value);
+                for (int j = 0; j < kOwn; ++j) acc[j] += row[min(c0 + j * kWave + lane, all - 1)];
             }
+#pragma unroll
+            for (int j = 0; j < kOwn; ++j) s_acc[wave][j * kWave + lane] = acc[j];
+            __syncthreads();
+            const int mine = c0 + (int)threadIdx.x;
+            if ((int)threadIdx.x >= kOwn * kWave || mine >= all) continue;
+            float value = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) value += s_acc[i][threadIdx.x];
+            dq[list * all + mine] = as_value<T>(value);
         }
         return;
     }
@@ -312,7 +311,7 @@ int tns_attend_grad(const tns_attend* a, const void* d_saved, const void* d_dout
     const float* const saved = static_cast<const float*>(d_saved);
     const float* const lse = saved + saved_out_bytes(*a) / 4;
     const size_t lds = lds_of(*a, kWaves << c.log_copies);
-    const unsigned few = few_of(c), sums = (a->buckets * a->heads + kEntries - 1) / kEntries, joins = sums + few + many_of(*a, c);
+    const unsigned few = few_of(*a, c), sums = (a->buckets * a->heads + kEntries - 1) / kEntries, joins = sums + few + many_of(*a, c);
     choose(*a, c, [&](auto value, auto vec, auto group, auto lanes) {
         using T = decltype(value);
         const Attend<T> t = typed<T>(*a);

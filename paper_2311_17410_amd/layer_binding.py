@@ -112,6 +112,12 @@ _block_bytes = functools.lru_cache(maxsize=1024)(tns_block_workspace)
 _distill_bytes = functools.lru_cache(maxsize=1024)(tns_distill_workspace)
 
 
+def _like(t):
+    """A tensor of t's shape and type, dense."""
+    import torch
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)      # (the first takes half as long)
+
+
 def _heads(name, t, shape, like):
     """The address and the row stride of a tensor [rows, heads, dim] whose rows may lie apart."""
     if t.dtype is not like.dtype or t.shape != shape or t.device != like.device:
@@ -161,7 +167,7 @@ def attend_run(rowptr, q, k, v, t=None, ts=None, edges=None, table=None, index=N
     on, stream = _on(q)
     a = _described(rowptr, q, k, v, t, ts, edges, table, index, mask, scale, newest_first)
     run, _, saved = _sizes(a)
-    out = dict(out=q.new_empty((a.S, a.heads, a.head_dim)), saved=q.new_empty(saved, dtype=torch.uint8) if save else None)
+    out = dict(out=_like(q), saved=q.new_empty(saved, dtype=torch.uint8) if save else None)
     ws = q.new_empty(run, dtype=torch.uint8)
     with on:
         rc = lib().tns_attend_run(C.byref(a), out["out"].data_ptr(), out["saved"].data_ptr() if save else 0, ws.data_ptr(), run, stream)
@@ -182,7 +188,7 @@ def attend_grad(rowptr, q, k, v, saved, dout, t=None, ts=None, edges=None, table
         raise ValueError("saved: attend_run(save=True) returns it")
     p_saved = _want("saved", saved, (size,), torch.uint8, q.device)
     p_dout = _want("dout", dout, q.shape, q.dtype, q.device)
-    out = dict(dq=q.new_empty(q.shape), dk=q.new_empty(k.shape), dv=q.new_empty(k.shape), dtable=None if table is None else q.new_empty(table.shape, dtype=torch.float32))
+    out = dict(dq=_like(q), dk=_like(k), dv=_like(v), dtable=None if table is None else _like(table))
     ws = q.new_empty(grad, dtype=torch.uint8)
     with on:
         tns_attend_grad(a, p_saved, p_dout, out["dq"].data_ptr(), out["dk"].data_ptr(), out["dv"].data_ptr(), 0 if table is None else out["dtable"].data_ptr(), ws.data_ptr(),
@@ -206,7 +212,7 @@ def block_run(x, branch, gate=None, scale=None, post=None, pre=None, eps=1e-6, c
     _unrecorded(x, branch, gate, scale, post, pre)
     on, stream = _on(x)
     b = _between(x, branch, gate, scale, post, pre, eps, center)
-    out = dict(out=x.new_empty(x.shape), next=None if pre is None else x.new_empty(x.shape))
+    out = dict(out=_like(x), next=None if pre is None else _like(x))
     with on:
         rc = lib().tns_block_run(C.byref(b), out["out"].data_ptr(), 0 if pre is None else out["next"].data_ptr(), stream)
     if rc:
@@ -222,9 +228,8 @@ def block_grad(x, branch, dout=None, dnext=None, gate=None, scale=None, post=Non
     on, stream = _on(x)
     b = _between(x, branch, gate, scale, post, pre, eps, center)
     p_dout, p_dnext = (_want(name, v, x.shape, x.dtype, x.device, False) for name, v in (("dout", dout), ("dnext", dnext)))
-    new = lambda given, *a, **kw: None if given is None else x.new_empty(*a, **kw)      # noqa: E731
-    out = dict(dx=x.new_empty(x.shape), dbranch=x.new_empty(x.shape), dgate=new(gate, x.shape),
-               **{name: new(given, b.dim, dtype=torch.float32) for name, given in (("dscale", scale), ("dpost", post), ("dpre", pre))})
+    out = dict(dx=_like(x), dbranch=_like(branch), dgate=None if gate is None else _like(gate), dscale=None if scale is None else _like(scale),
+               dpost=None if post is None else _like(post), dpre=None if pre is None else _like(pre))
     need = _block_bytes(b.rows, b.dim)
     ws = x.new_empty(need, dtype=torch.uint8)
     p = lambda t: 0 if t is None else t.data_ptr()      # noqa: E731
@@ -246,7 +251,7 @@ def distill(logits, ids, teacher, lse=None, weight=None, temperature=1.0, scale=
     d = tns_distill_desc(B, V, K, _dtype_of(logits), _want("logits", logits, (B, V), logits.dtype, dev, False), _ld(logits, V), _want("ids", ids, (B, K), torch.int32, dev),
                          _want("teacher", teacher, (B, K), f32, dev), _want("lse", lse, (B,), f32, dev), _want("weight", weight, (B,), f32, dev), temperature, scale)
     need = _distill_bytes(B, V, K)
-    out = dict(loss=logits.new_empty((), dtype=f32), rows=logits.new_empty(B, dtype=f32), dlogits=logits.new_empty((B, V)) if grad else None)
+    out = dict(loss=logits.new_empty((), dtype=f32), rows=logits.new_empty(B, dtype=f32), dlogits=_like(logits) if grad else None)
     ws = logits.new_empty(need, dtype=torch.uint8)
     with on:
         rc = lib().tns_distill(C.byref(d), out["loss"].data_ptr(), out["rows"].data_ptr(), out["dlogits"].data_ptr() if grad else 0, ws.data_ptr(), need, stream)
