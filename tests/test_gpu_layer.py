@@ -797,3 +797,63 @@ def test_attend_many_lists_ruled_out_buckets_and_rows_beyond(L):
     for name in ("dk", "dv"):
         assert torch.equal(back[name][:n], d[name]) and not back[name][n:].any()
     assert torch.equal(back["dq"], d["dq"])
+
+
+def test_attend_rows_without_lists(L):
+    """No list at all, and rows all the same: their gradients are zeros, the table's too."""
+    import torch
+    k = torch.full((200, 2, 8), float("nan"), device="cuda")
+    q = torch.empty((0, 4, 8), device="cuda")
+    table, edges = torch.ones((3, 4), device="cuda"), torch.tensor([1.0, 2.0], device="cuda")
+    rp = torch.zeros(1, dtype=torch.int64, device="cuda")
+    r = L.attend_run(rp, q, k, k, table=table, edges=edges, save=True)
+    d = L.attend_grad(rp, q, k, k, r["saved"], q, table=table, edges=edges)
+    assert r["out"].shape == q.shape and not d["dk"].any() and not d["dv"].any() and not d["dtable"].any()
+    desc = L.tns_attend(0, 200, 0, 4, 2, 8, 0, 3, L.TNS_ZERO_BEYOND, None, None, k.data_ptr(), k.data_ptr(), 32, 16, 16, None, None, None, None, edges.data_ptr(), table.data_ptr(), 1.0)
+    need = L.tns_attend_workspace(desc)[1]
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    d["dk"].fill_(1)
+    L.tns_attend_grad(desc, 0, 0, 0, d["dk"].data_ptr(), d["dv"].data_ptr(), d["dtable"].data_ptr(), ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+    assert not d["dk"].any()
+
+
+def test_first_calls_within_a_capture(L):
+    """Kernels that have not run before in this process (sizes that no other test has) may be captured."""
+    import torch
+    rng = np.random.default_rng(40)
+    a = the_events(rng, [9, 0, 70], 8, 1, 68, BF16, buckets=3)
+    g, dout = on_gpu(a, BF16), torch_of(values(rng, a["q"].shape, BF16), BF16)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = L.attend_run(**g, save=True)
+        d = L.attend_grad(**g, saved=r["saved"], dout=dout)
+    want = O.attend(**a, dout=dout.float().cpu().numpy())
+    for _ in range(2):
+        r["out"].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        close("out", r["out"], want["out"], want["out_off"], BF16)
+        for name in ("dq", "dk", "dv"):
+            close(name, d[name], want[name], want[name + "_off"], BF16)
+        close("dtable", d["dtable"], want["dtable"], want["dtable_off"])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attend_infinite_keys(L, dtype):
+    """A key of minus infinity against a positive query: the event's score is minus infinity and its p zero, at whole and at odd head sizes."""
+    rng = np.random.default_rng(41)
+    for dim in (8, 13, 43, 64):
+        a = the_events(rng, [5, 40], 2, 2, dim, dtype, buckets=0, times=False)
+        a["q"][:, :, 0] = np.abs(a["q"][:, :, 0]) + 0.5
+        g = on_gpu(a, dtype)
+        a["q"] = g["q"].float().cpu().numpy()      # (as the type holds them)
+        g["k"][2, :, 0] = -float("inf")
+        g["k"][30, 1, 0] = -float("inf")
+        got = L.attend_run(**g)["out"]
+        assert bool(got.isfinite().all())
+        # the same with these events left out
+        a["k"][2, :, 0] = -1e4
+        a["k"][30, 1, 0] = -1e4
+        want = O.attend(**a)
+        # p of exp(-5000 and less) is 0 in the oracle too
+        close("out", got, want["out"], want["out_off"], dtype)
