@@ -42,6 +42,11 @@ struct Back {
     template <int LANES>
     __device__ __forceinline__ bool take(const Attend<T>& a, const Cut& cut, const Place<T, VEC, EXACT>& at, Row<T, VEC>& k, Row<T, VEC>& v, int bucket, const float* s_table, float scale,
                                          bool (&counts)[G], float (&ds)[G], float (&to_k)[N], float (&to_v)[N]) {
+        if constexpr (G > 1 && sizeof(T) == 2)      // (opaque here: the compiler would keep all heads' values widened, 32 registers a head, and fewer waves)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) asm("" : "+v"(q[g].word[i]), "+v"(d[g].word[i]));
         bool some = false, all = true;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -94,12 +99,14 @@ __device__ __forceinline__ void add_to_table(const Attend<T>& a, const Cut& cut,
 }
 
 // One pass over k and v: the scores again, p from the saved logarithm of their sum, and all gradients of an event while its rows are in
-// registers.
+// registers.  ds = p (dp - delta) with dp = dout . v; delta = dout . out from outputs saved in fp32 (of bf16 ones the difference would keep their rounding,
+// and the table's gradient, in which most of it cancels, would show it).  Bound by memory: 131072 lists of ten, two heads of 64 bf16 channels, 1.35 GB in
+// 259 us (5.2 TB/s); 3001 histories, eight heads of 32 fp32 channels on four, 1.65 GB in 342 us (4.8).
 template <typename T, int VEC, int G, int LANES>
 __global__ void __launch_bounds__(kWaves* kWave) k_attend_grad(const Args<T>) {
     extern __shared__ float s_mem[];
     constexpr bool EXACT = LANES != 0;
-    constexpr int N = Row<T, VEC>::N, U = G == 2 ? 2 : 1, OWN = 1;
+    constexpr int N = Row<T, VEC>::N, U = G == 2 && sizeof(T) == 4 ? 2 : 1, OWN = 1;
     const Args<T>& start = args_now<T>();
     const int entries = start.a.buckets * start.a.heads, wave = uniform((int)(threadIdx.x >> 6));
     float *const s_edges = s_mem, *const s_table = s_mem + start.a.buckets, *const s_sums = s_table + max(entries, start.a.heads);
