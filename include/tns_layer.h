@@ -32,7 +32,8 @@ extern "C" {
  * table entry is -infinity.  Where no event is left out is zero, and its gradients are.
  *
  *   S, d_rowptr[S+1]  lists, as in tns_recur.  S < 2^31
- *   rows              rows that the events' arrays have room for, at least d_rowptr[S]; rows from d_rowptr[S] on are not read.  < 2^40
+ *   rows              rows that the events' arrays have room for, at least d_rowptr[S]; rows from d_rowptr[S] on do not count,
+ *                     whatever they hold.  < 2^40 (calls of more than 2^34 rows times 256 channels of all heads are refused)
  *   num               rows of k and v with d_index, < 2^31 (without: k and v have `rows` rows, and num is 0)
  *   heads, kv_heads   heads of q; of k and v.  kv_heads divides heads, heads / kv_heads <= 8, heads <= 1024
  *   head_dim          1 .. 256

@@ -195,8 +195,8 @@ struct Walk {
 };
 
 // Where there are many lists, those of `brief` events at most are taken a slot each: what a list costs apart from its events (its query, its
-// edges, its result) is then paid once for all slots, and nothing is joined.  131072 lists of ten, two heads of 64 bf16 channels, outputs: 171 us,
-// a wave to a list 169; gathered, four heads of 32, 66600 lists: 63 and 74.
+// edges, its result) is then paid once for all slots, and nothing is joined.  131072 lists of ten, two heads of 64 bf16 channels, outputs: 169 us
+// either way; gathered, four heads of 32, 66600 lists: 63 us, a wave to a list 74.
 struct Own {
     int64_t list, begin;
     int n, events;                      // of the list; that are taken here, 0 of lists that are not (`here`)
@@ -442,9 +442,10 @@ __device__ __forceinline__ void stage(const Attend<T>& a, float* s_edges, float*
     for (int i = threadIdx.x; i < max(a.buckets, 1) * a.heads; i += kWaves * kWave) s_table[i] = a.buckets ? a.table[i] * kLog2e : 0.0f;
     __syncthreads();
 }
+
 struct Work {
-    int32_t* first;                     // [blocks]
-    float *stats, *acc;                 // [blocks, heads, 2], [blocks, heads, dim]: of the parts of lists that have several
+    int32_t* first;                     // [blocks]: the list that is cut and has its first part there, or -1
+    float *stats, *acc;                 // [2 blocks, heads, 2], [2 blocks, heads, dim]: of the parts of lists that have several
     float* tables;                      // [workgroups of the gradients, buckets * heads]
 };
 
@@ -534,9 +535,9 @@ __device__ __forceinline__ void each_batch(B& batch, int n, int by, const Read& 
 }
 
 // ---- lists of several parts ---------------------------------------------------------------------------------
-// A workgroup joins the lists whose first part ends with one of sixteen blocks, one after the other: a wave has every sixteenth part, a lane
-// kOwn channels, and every so many channels a workgroup of their own.  Lists of more than kMany parts are joined by a workgroup for every kSlice channels of a head (a list of that many parts holds a block whose number is a
-// multiple of kMany; the first such block stands for it).
+// A workgroup joins the lists whose first part lies in one of sixteen blocks, one after the other: a wave has every sixteenth part, a lane kOwn
+// channels, and every so many channels a workgroup of their own.  Lists of more than kMany parts are joined by a workgroup for every kSlice
+// channels of a head (a list of that many parts holds a block whose number is a multiple of kMany; the first such block stands for it).
 constexpr int kMany = 256, kOwn = 4, kSlice = 16;
 __device__ __forceinline__ int64_t parts_end(int64_t list_end, const Cut& cut) { return min((list_end + ((int64_t)1 << cut.part) - 1) >> cut.part, cut.blocks); }
 
@@ -651,9 +652,13 @@ int resident(K kernel, size_t lds, int& per_cu) {      // per_cu: what was found
 int groups_of(const tns_attend& a, const Cut& c, int most) {
     return (int)std::min<int64_t>((a.S + c.blocks + kWaves - 1) / kWaves, std::max(most / c.turns, 1));
 }
-unsigned slices_of(const tns_attend& a) { return (a.head_dim + kSlice - 1) / kSlice; }
-unsigned few_of(const tns_attend& a, const Cut& c) { return c.blocks > 1 ? (unsigned)((c.blocks + 15) / 16 * ((a.heads * a.head_dim + kOwn * kWave - 1) / (kOwn * kWave))) : 0; }
-unsigned many_of(const tns_attend& a, const Cut& c) { return c.blocks > kMany ? (unsigned)(((c.blocks + kMany - 1) / kMany) * a.heads * slices_of(a)) : 0; }
+int64_t slices_of(const tns_attend& a) { return (a.head_dim + kSlice - 1) / kSlice; }
+int64_t few_of(const tns_attend& a, const Cut& c) { return c.blocks > 1 ? (c.blocks + 15) / 16 * ((a.heads * a.head_dim + kOwn * kWave - 1) / (kOwn * kWave)) : 0; }
+int64_t many_of(const tns_attend& a, const Cut& c) { return c.blocks > kMany ? (c.blocks + kMany - 1) / kMany * a.heads * slices_of(a) : 0; }
+// (A launch has fewer than 2^32 threads: 2^34 rows of up to 256 channels.)
+int check_joins(const tns_attend& a, const Cut& c) {
+    return few_of(a, c) + many_of(a, c) > (int64_t)1 << 21 ? fail(TNS_ESIZE, "more rows times channels than one call can join") : (int)TNS_OK;
+}
 
 struct Layout {
     Work w;

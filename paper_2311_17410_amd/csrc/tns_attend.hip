@@ -313,6 +313,7 @@ int tns_attend_run(const tns_attend* a, void* d_out, void* d_saved, void* d_work
     const Cut c = cut_of(*a);
     const Layout l = carve(*a, c, false, d_workspace);
     if (int e = check_workspace(d_workspace, workspace_bytes, l.bytes)) return e;
+    if (int e = check_joins(*a, c)) return e;
     if (a->S == 0) return TNS_OK;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     float* const saved = static_cast<float*>(d_saved);
@@ -329,8 +330,8 @@ int tns_attend_run(const tns_attend* a, void* d_out, void* d_saved, void* d_work
         if constexpr (lanes() == 0) launch(k_attend<T, vec(), group(), 0, 2>, per_cu[2]);
         else if (a->d_index) launch(k_attend<T, vec(), group(), lanes(), 1>, per_cu[1]);
         else launch(k_attend<T, vec(), group(), lanes(), 0>, per_cu[0]);
-        if (const unsigned few = few_of(*a, c))
-            hipLaunchKernelGGL((k_attend_join<T>), dim3(few + many_of(*a, c)), dim3(1024), 0, stream, t, c, l.w, few, static_cast<T*>(d_out), saved, lse);
+        if (const unsigned few = (unsigned)few_of(*a, c))
+            hipLaunchKernelGGL((k_attend_join<T>), dim3(few + (unsigned)many_of(*a, c)), dim3(1024), 0, stream, t, c, l.w, few, static_cast<T*>(d_out), saved, lse);
     });
     return launched("tns_attend_run");
 }

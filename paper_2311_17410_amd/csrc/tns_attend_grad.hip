@@ -318,7 +318,8 @@ int tns_attend_grad(const tns_attend* a, const void* d_saved, const void* d_dout
     const float* const saved = static_cast<const float*>(d_saved);
     const float* const lse = saved + saved_out_bytes(*a) / 4;
     const size_t lds = lds_of(*a, kWaves << c.log_copies);
-    const unsigned few = few_of(*a, c), sums = (a->buckets * a->heads + kEntries - 1) / kEntries, joins = sums + few + many_of(*a, c);
+    if (int e = check_joins(*a, c)) return e;
+    const unsigned few = (unsigned)few_of(*a, c), sums = (a->buckets * a->heads + kEntries - 1) / kEntries, joins = sums + few + (unsigned)many_of(*a, c);
     choose(*a, c, [&](auto value, auto vec, auto group, auto lanes) {
         using T = decltype(value);
         const Attend<T> t = typed<T>(*a);

@@ -170,6 +170,11 @@ def test_attend_refuses_outputs():
     for at, value, status in [(0, 0, B.TNS_EINVAL), (0, 264, B.TNS_EINVAL), (1, 0, B.TNS_EINVAL), (1, 258, B.TNS_EINVAL), (2, 0, B.TNS_EINVAL), (3, 0, B.TNS_EINVAL),
                               (4, 0, B.TNS_EINVAL), (4, 257, B.TNS_EINVAL), (5, 0, B.TNS_EINVAL), (6, 0, B.TNS_EINVAL), (7, 0, B.TNS_ESIZE)]:
         refused(status, L.tns_attend_grad, a, *[value if i == at else v for i, v in enumerate(ok)])
+    many = attend(rows=1 << 38)                                               # more blocks than a launch has workgroups for
+    refused(B.TNS_ESIZE, L.tns_attend_run, many, 256, 256, 256, 1 << 62)
+    refused(B.TNS_ESIZE, L.tns_attend_grad, many, *ok[:7], 1 << 62)
+    refused(B.TNS_ESIZE, L.tns_attend_run, attend(ld_k=1 << 22), 256, 256, 256, BIG)
+    refused(B.TNS_ESIZE, L.tns_attend_run, attend(ld_v=1 << 22), 256, 256, 256, BIG)
     refused(B.TNS_EINVAL, L.tns_attend_grad, attend(d_index=256, num=4), *ok)      # no gradients by gathered rows
     refused(B.TNS_EINVAL, L.tns_attend_grad, attend(buckets=0, d_table=None, d_edges=None), *ok)
 
