@@ -126,7 +126,8 @@ TNS_API int tns_block_grad(const tns_block *b, const void *d_dout, int64_t ld_do
  * and the mass of the others, rest = max(1 - sum p, 0), is compared as a whole:
  *     loss = weight * (sum_k p_k (log p_k - log q[id_k]) + rest (log rest - log(sum of q over the candidates that no id names)))
  * An id outside [0, V) and a teacher's score of -infinity have p = 0 (the latter's id is named all the same); terms of p = 0 and rest = 0
- * are 0.  A candidate named twice has two terms.  A row without any p > 0 has loss 0 and gradient 0 without d_lse.
+ * are 0; a loss is infinite where p (rest) is above 0 and the student's q (of all others) is 0.  A candidate named twice has two terms.
+ * Without d_lse a row without any p > 0 has loss 0 and gradient 0.
  * A row of weight 0 is not read, whatever lies there: its loss and gradient are 0.
  *
  *   B, V, K         rows, candidates, ids of a row: B, V < 2^31, V >= 1, 0 <= K <= 1024

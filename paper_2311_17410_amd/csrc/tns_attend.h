@@ -630,7 +630,9 @@ Cut cut_of(const tns_attend& a) {
     c.part = 6;
     while (c.part > 4 && ((a.rows * c.turns) >> (c.part - 1)) <= 2048) --c.part;
     while (c.part < 9 && ((a.rows * c.turns) >> c.part) > 16384) ++c.part;
-    c.brief = c.log_width >= 2 && a.S / c.slots * c.turns >= 2048 ? std::min(64, 1 << c.part) : -1;
+    // Brief lists a slot each: where there are enough of them, and short ones by what rows there are (8300 lists of 64, two heads of 64 bf16 channels,
+    // gradients: 99 us, 85 otherwise; of ten, outputs: 12 and 15).
+    c.brief = c.log_width >= 2 && a.S / c.slots * c.turns >= 2048 && a.rows <= 16 * a.S ? std::min(64, 1 << c.part) : -1;
     c.log_copies = std::min(__builtin_ctz(c.slots), 3);
     while (c.log_copies && ((size_t)a.buckets * a.heads * kWaves << c.log_copies) > 4096) --c.log_copies;
     c.blocks = (a.rows + ((int64_t)1 << c.part) - 1) >> c.part;
