@@ -3,12 +3,6 @@
 
 namespace {
 
-// Zeros in the values from..to of an array, by a wave.
-template <typename T>
-__device__ void zero_values(T* base, int64_t from, int64_t to) {
-    for (int64_t i = from + (threadIdx.x & 63); i < to; i += kWave) base[i] = T{};
-}
-
 // A lane's share of the gradients of a list, for a group of heads.
 template <typename T, int VEC, int G, bool EXACT>
 struct Back {
@@ -179,8 +173,8 @@ __global__ void __launch_bounds__(kWaves* kWave) k_attend_grad(const Args<T>) {
         const bool any = walk.get(a, cut, blockIdx.y == 0 ? now.work.first : nullptr, w, [&](int64_t block) {
             if (!a.zero_beyond || blockIdx.y) return;
             const int64_t from = max(block << cut.part, a.total()), to = min((block + 1) << cut.part, a.rows);
-            zero_values(now.dk, from * row_of, to * row_of);
-            zero_values(now.dv, from * row_of, to * row_of);
+            tns::zero_values(now.dk + from * row_of, max(to - from, (int64_t)0) * row_of, at.lane, kWave);
+            tns::zero_values(now.dv + from * row_of, max(to - from, (int64_t)0) * row_of, at.lane, kWave);
         });
         if (!any) break;
         const float t = a.t ? a.t[w.list] : 0.0f, scale = a.scale * kLn2;

@@ -216,8 +216,7 @@ __device__ __forceinline__ void write_grad(const Distill<T>& d, const Held<T, TH
 template <typename T, int THREADS>
 __device__ __forceinline__ void nothing(const Distill<T>& d, int64_t row, int64_t begin, int64_t count, float* rows, T* dlogits) {
     if (threadIdx.x == 0 && begin == 0) rows[row] = 0.0f;
-    if (dlogits)
-        for (int64_t i = threadIdx.x; i < count; i += THREADS) dlogits[row * d.V + begin + i] = T{};
+    if (dlogits) tns::zero_values(dlogits + row * d.V + begin, count, threadIdx.x, THREADS);
 }
 
 // Which candidates of a piece some id names, a bit each.

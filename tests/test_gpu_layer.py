@@ -857,3 +857,28 @@ def test_attend_infinite_keys(L, dtype):
         want = O.attend(**a)
         # p of exp(-5000 and less) is 0 in the oracle too
         close("out", got, want["out"], want["out_off"], dtype)
+
+
+@pytest.mark.parametrize("dtype, kv_heads, dim, skip", [(F32, 1, 3, 1), (F32, 2, 16, 0), (BF16, 1, 7, 1), (BF16, 3, 5, 6), (BF16, 2, 32, 3)])
+@pytest.mark.parametrize("rows, beyond", [(0, 1), (5, 700), (130, 63), (64, 64)])
+def test_attend_zeros_beyond_at_any_address(L, rows, beyond, dtype, kv_heads, dim, skip):
+    """Rows beyond the lists become zeros, and nothing beside them: at every address that the type allows."""
+    import torch
+    rng = np.random.default_rng(rows + dim)
+    a = the_events(rng, [rows], kv_heads, kv_heads, dim, dtype, buckets=0, times=False)
+    g = on_gpu(a, dtype)
+    for name in ("k", "v"):
+        g[name] = torch.cat((g[name], torch.full((beyond, kv_heads, dim), float("nan"), dtype=g[name].dtype, device="cuda")))
+    r = L.attend_run(**g, save=True)
+    dout = torch_of(values(rng, a["q"].shape, dtype), dtype)
+    want = O.attend(**a, dout=dout.float().cpu().numpy())
+    desc = L._described(g["rowptr"], g["q"], g["k"], g["v"], None, None, None, None, None, None, None, True)
+    need, size, n = L.tns_attend_workspace(desc)[1], kv_heads * dim, rows + beyond
+    out = [torch.full((n * size + skip + 9,), 7.0, dtype=dout.dtype, device="cuda") for _ in range(2)]
+    dq, ws = torch.empty_like(g["q"]), torch.empty(need, dtype=torch.uint8, device="cuda")
+    at = skip * dout.element_size()
+    L.tns_attend_grad(desc, r["saved"].data_ptr(), dout.data_ptr(), dq.data_ptr(), out[0].data_ptr() + at, out[1].data_ptr() + at, 0, ws.data_ptr(), need,
+                      torch.cuda.current_stream().cuda_stream)
+    for name, got in zip(("dk", "dv"), out):
+        assert bool((got[:skip] == 7).all()) and bool((got[skip + n * size:] == 7).all()) and not got[skip + rows * size: skip + n * size].any()
+        close(name, got[skip: skip + rows * size].view(rows, kv_heads, dim), want[name], want[name + "_off"], dtype)
