@@ -8,6 +8,7 @@
 
 #include "../../include/tns_layer.h"
 #include "tns_internal.h"
+#include "tns_parts.h"
 #include "tns_sums.h"
 #include "tns_values.h"
 
@@ -19,11 +20,13 @@ using tns::bf16;
 using tns::fail;
 using tns::fail_hip;
 using tns::gap_of;
+using tns::is_many;
 using tns::kLog2e;
 using tns::Max;
 using tns::over_lanes;
 using tns::over_row_strided;
 using tns::over_strided;
+using tns::parts_end;
 
 namespace {
 
@@ -537,19 +540,18 @@ __device__ __forceinline__ void each_batch(B& batch, int n, int by, const Read& 
 // ---- lists of several parts ---------------------------------------------------------------------------------
 // A workgroup joins the lists whose first part lies in one of sixteen blocks, one after the other: a wave has every sixteenth part, a lane kOwn
 // channels, and every so many channels a workgroup of their own.  Lists of more than kMany parts are joined by a workgroup for every kSlice
-// channels of a head (a list of that many parts holds a block whose number is a multiple of kMany; the first such block stands for it).
-constexpr int kMany = 256, kOwn = 4, kSlice = 16;
-__device__ __forceinline__ int64_t parts_end(int64_t list_end, const Cut& cut) { return min((list_end + ((int64_t)1 << cut.part) - 1) >> cut.part, cut.blocks); }
-
-// The list of many parts that workgroup `many` of the blocks' multiples of kMany joins, and its first block; -1 if there is none.
+// channels of a head, at the place that stands for them (tns_parts.h).
+constexpr int kOwn = 4, kSlice = 16;
 template <typename T>
-__device__ __forceinline__ int64_t many_of(const Attend<T>& a, const Cut& cut, int64_t many, int64_t& begin, int64_t& end) {
-    const int64_t row = many * kMany << cut.part;
-    if (row >= a.total()) return -1;
-    const int64_t list = find_list(a, row);
-    begin = a.edge(list) >> cut.part;
-    end = parts_end(a.edge(list + 1), cut);
-    return end - begin > kMany && (begin + kMany - 1) / kMany == many ? list : -1;
+struct ListsOf {
+    const Attend<T>& a;
+    __device__ int64_t total() const { return a.total(); }
+    __device__ int64_t edge(int64_t list) const { return a.edge(list); }
+    __device__ int64_t find(int64_t row) const { return find_list(a, row); }
+};
+template <typename T>
+__device__ __forceinline__ int64_t many_of(const Attend<T>& a, const Cut& cut, int64_t place, int64_t& first, int64_t& end) {
+    return tns::many_at(place, cut.part, cut.blocks, ListsOf<T>{a}, first, end);
 }
 
 // The number of a list's part that lies in block b, the list's first part in block `first`.
@@ -656,7 +658,7 @@ int groups_of(const tns_attend& a, const Cut& c, int most) {
 }
 int64_t slices_of(const tns_attend& a) { return (a.head_dim + kSlice - 1) / kSlice; }
 int64_t few_of(const tns_attend& a, const Cut& c) { return c.blocks > 1 ? (c.blocks + 15) / 16 * ((a.heads * a.head_dim + kOwn * kWave - 1) / (kOwn * kWave)) : 0; }
-int64_t many_of(const tns_attend& a, const Cut& c) { return c.blocks > kMany ? (c.blocks + kMany - 1) / kMany * a.heads * slices_of(a) : 0; }
+int64_t many_of(const tns_attend& a, const Cut& c) { return tns::many_places(c.blocks) * a.heads * slices_of(a); }
 // (A launch has fewer than 2^32 threads: 2^34 rows of up to 256 channels.)
 int check_joins(const tns_attend& a, const Cut& c) {
     return few_of(a, c) + many_of(a, c) > (int64_t)1 << 21 ? fail(TNS_ESIZE, "more rows times channels than one call can join") : (int)TNS_OK;

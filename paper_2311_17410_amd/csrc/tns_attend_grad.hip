@@ -255,8 +255,8 @@ __global__ void __launch_bounds__(1024) k_attend_grad_join(const Attend<T> a, co
         for (uint64_t left = __ballot(begins >= 0); left; left &= left - 1) {
             const int k = __builtin_ctzll(left);
             const int64_t block = block0 + k, list = __builtin_amdgcn_readlane(begins, k);
-            const int64_t end = parts_end(a.edge(list + 1), cut);
-            if (end - block > kMany) continue;
+            const int64_t end = parts_end(a.edge(list + 1), cut.part, cut.blocks);
+            if (is_many(block, end)) continue;
             __syncthreads();
             float acc[kOwn] = {};
 #pragma unroll 4
