@@ -255,11 +255,17 @@ def distill(logits, ids, teacher, lse=None, weight=None, temperature=1.0, scale=
         if lse is not None:
             rest = V(1.0) - mass
             if rest.v > 0:
-                others = where(~inside, e).sum(0, deep)
+                left = ~inside & ~np.isneginf(logits[b])
                 g = q * (mass + rest)
-                if others.v > 0:
-                    loss = loss + rest * (rest.log() - (others.log() - log_total))
-                    g = g - where(~inside, e * (rest * others.inverse()))
+                if left.any():
+                    # by the others' own largest score: by that of all, a named one far above them would leave their sum no bits
+                    raw = logits[b].astype(np.float64)
+                    own, down = (np.where(left, raw - raw[left].max(), -np.inf), raw[left].max() - raw.max())
+                    eo = (V(own, U * np.abs(np.where(left, own, 0.0))) * V(rate, 2 * U * rate)).exp()
+                    others = where(left, eo).sum(0, deep)
+                    log_others = others.log() + V(down, U * np.abs(down)) * V(rate, 2 * U * rate)
+                    loss = loss + rest * (rest.log() - (log_others - log_total))
+                    g = g - where(left, eo * (rest * others.inverse()))
                 else:                                             # the student gives the others nothing
                     loss = V(np.inf)
         minus = V(np.zeros(n))

@@ -170,33 +170,41 @@ __device__ __forceinline__ float teacher_lse(float base, float sum) { return sum
 template <typename T>
 __device__ __forceinline__ float rest_of(const Distill<T>& d, float mass) { return !d.lse ? 0.0f : mass == mass ? fmaxf(1.0f - mass, 0.0f) : mass; }
 
-// Of a row's scores, or a piece of them: the largest, and the sums of exp(rate (score - largest)) over all and over those that no id names.
+// Of a row's scores, or a piece of them: the largest, and the sum of exp(rate (score - largest)).  With d_lse the same of those that no id names: their
+// sum by their own largest, since by that of all it would be zero where a named one lies some ninety temperatures above them.
 struct Stats {
-    float top, all, others;
+    float top, others_top, all, others;
 };
-__device__ __forceinline__ float loss_of(const Terms& t, float rest, const Stats& s) {
+// exp(rate (others' largest - largest)): what the others' exponentials are by the largest of all.  0 where there are none.
+__device__ __forceinline__ float others_scale(const Stats& s, float by) { return s.others == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((base_of(s.others_top) - base_of(s.top)) * by); }
+__device__ __forceinline__ float loss_of(const Terms& t, float rest, const Stats& s, float rate) {
     const float log_all = logf(s.all);
     float l = t.entropy - t.score + (t.mass != 0.0f ? t.mass * log_all : 0.0f);
-    if (rest != 0.0f) l += rest * (logf(rest) - (logf(s.others) - log_all));
+    if (rest != 0.0f) l += rest * (logf(rest) - (logf(s.others) + (base_of(s.others_top) - base_of(s.top)) * rate - log_all));
     return l;
 }
 
 // Gradient of a row's piece from the whole row's statistics.  By a named candidate it is q (mass + rest) - p, by another one q (mass + rest) -
-// rest exp(.) / others, both times c.  All are written as others first, then the named ones once more, by the threads that have them: a
-// workgroup's stores of one address stay in order over the barrier.
-template <bool STREAM, typename T, int THREADS, int NV>
+// rest exp(.) / others, both times c; with d_lse (REST) the latter's exponential is by the others' largest, and q's factor is brought there.  All are written
+// as others first, then the named ones once more, by the threads that have them: a workgroup's stores of one address stay in order over the barrier.
+template <bool REST, bool STREAM, typename T, int THREADS, int NV>
 __device__ __forceinline__ void write_grad(const Distill<T>& d, const Held<T, THREADS, NV>& held, int64_t row, int64_t begin, int count, int skew, const Stats& s, float mass, float rest,
                                            float weight, const Ids& ids, bool twice, T* dlogits) {
     using H = Held<T, THREADS, NV>;
-    const float base = base_of(s.top), by = d.rate * kLog2e, c = d.scale * d.rate * weight;
-    const float named = c * (mass + rest) * (1.0f / s.all), other = rest != 0.0f ? named - c * rest / s.others : named;
+    const float base = base_of(s.top), by = d.rate * kLog2e, c = d.scale * d.rate * weight, named = c * (mass + rest) * (1.0f / s.all);
+    float other = named, other_base = base;
+    if (REST) {
+        other = named * others_scale(s, by);
+        if (rest != 0.0f && s.others != 0.0f) other -= c * rest / s.others;
+        other_base = base_of(s.others_top);
+    }
     T* const to = dlogits + row * d.V + begin;
     const bool same = H::skew_of(to) == skew;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         float g[H::VEC];
 #pragma unroll
-        for (int i = 0; i < H::VEC; ++i) g[i] = __builtin_amdgcn_exp2f((held.get(j, i) - base) * by) * other;
+        for (int i = 0; i < H::VEC; ++i) g[i] = __builtin_amdgcn_exp2f((held.get(j, i) - other_base) * by) * other;
         H::template write<STREAM>(to, count, skew, same, j, g);
     }
     __syncthreads();
@@ -252,45 +260,61 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
     H held;
     held.read(piece, count, skew);
     names.template clear<THREADS>();
-    float top[2];
+    float top[2];                       // of the row (REST: of the others); of the teacher's (REST: of the named)
     top[1] = read_ids<T, THREADS>(d, row, ids);
-    if (REST)
+    float sum[6] = {};                  // over the row (REST: without the named), over the named, mass, entropy, score, whether some id came twice
+    uint32_t adds = 0;                  // of the thread's ids, a bit each: whether it adds the candidate to the named
+    if (REST) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) s_row[j * THREADS + threadIdx.x] = held.raw[j];
-    top[0] = held.top();
-    over_workgroup<THREADS>(top, s_top, Max{});
-    const float base = base_of(top[0]), by = d.rate * kLog2e;
-    float sum[6] = {};                  // over the row (REST: without the named), over the named, mass, entropy, score, whether some id came twice
-    for (int k = threadIdx.x; k < d.K; k += THREADS) {
+        __syncthreads();
+        top[1] = -kInf;
+    } else {
+        top[0] = held.top();
+        over_workgroup<THREADS>(top, s_top, Max{});
+    }
+    for (int k = threadIdx.x, bit = 0; k < d.K; k += THREADS, ++bit) {
         const int at = ids.id[k];
         if (at < 0) continue;
-        if (names.add(at)) sum[1] += __builtin_amdgcn_exp2f((ids.x[k] - base) * by);
+        if (names.add(at)) adds |= 1u << bit;
         else sum[5] = 1.0f;
-        if (REST) reinterpret_cast<T*>(s_row)[at + skew] = as_value<T>(-kInf);
+        if (REST) {
+            reinterpret_cast<T*>(s_row)[at + skew] = as_value<T>(-kInf);
+            top[1] = fmaxf(top[1], ids.x[k]);
+        }
     }
-    float lse;
+    float lse, others_top = -kInf;
     if (REST) {
         lse = d.lse[row];
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < NV; ++j) held.raw[j] = s_row[j * THREADS + threadIdx.x];
+        top[0] = held.top();
+        over_workgroup<THREADS>(top, s_top, Max{});
+        others_top = top[0];
+        top[0] = fmaxf(top[0], top[1]);
     } else {
         float t[1] = {teacher_sum(d, ids, base_of(top[1]), THREADS)};
         over_workgroup<THREADS>(t, s_lse, Add{});
         lse = teacher_lse(base_of(top[1]), t[0]);
     }
+    const float base = base_of(top[0]), by = d.rate * kLog2e;
+    if (REST)
+        for (int k = threadIdx.x, bit = 0; k < d.K; k += THREADS, ++bit)
+            if (adds >> bit & 1) sum[1] += __builtin_amdgcn_exp2f((ids.x[k] - base) * by);
     const Terms mine = terms_of<T, THREADS>(d, ids, lse, base);
-    sum[0] = held.sum(base, by);
+    sum[0] = held.sum(REST ? base_of(others_top) : base, by);
     sum[2] = mine.mass;
     sum[3] = mine.entropy;
     sum[4] = mine.score;
     over_workgroup<THREADS>(sum, s_sum, Add{});
     const Terms t = {sum[2], sum[3], sum[4]};
     if (!REST && t.mass == 0.0f) return nothing<T, THREADS>(d, row, 0, d.V, rows, dlogits);
-    const Stats s = {top[0], REST ? sum[0] + sum[1] : sum[0], sum[0]};
+    Stats s = {top[0], REST ? others_top : top[0], sum[0], sum[0]};
+    if (REST) s.all = sum[1] + others_scale(s, by) * sum[0];
     const float rest = rest_of(d, t.mass);
-    if (threadIdx.x == 0) rows[row] = weight * loss_of(t, rest, s);
-    if (dlogits) write_grad<false>(d, held, row, 0, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
+    if (threadIdx.x == 0) rows[row] = weight * loss_of(t, rest, s, d.rate);
+    if (dlogits) write_grad<REST, false>(d, held, row, 0, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
 }
 
 // Rows of several pieces: the pieces' statistics, then their gradients.  200 rows of 500009 fp32 scores: 95 and 142 us before the second pass
@@ -302,7 +326,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_stats(const Distill<T> d, 
     using H = Held<T, kThreads, kVectors>;
     __shared__ typename H::Vec s_row[REST ? kThreads * kVectors : 1];
     __shared__ Names<kThreads * H::N> names;
-    __shared__ float s_top[1][16], s_sum[2][16];
+    __shared__ float s_top[2][16], s_sum[2][16];
     const int64_t row = d.first + blockIdx.x / pieces, begin = (int64_t)(blockIdx.x % pieces) * kPiece<T>;
     const int count = (int)min(d.V - begin, (int64_t)kPiece<T>);
     if (d.weight && d.weight[row] == 0.0f) return;
@@ -310,36 +334,54 @@ __global__ void __launch_bounds__(kThreads) k_distill_stats(const Distill<T> d, 
     const int skew = H::skew_of(piece);
     H held;
     held.read(piece, count, skew);
-    float top[1], sum[2] = {};
+    float top[2] = {-kInf, -kInf}, sum[2] = {};      // of all (REST: of the others), of the named
+    const float by = d.rate * kLog2e;
+    constexpr int NAMED = REST ? kMostIds / kThreads : 0;
+    int at[NAMED + 1];                  // the thread's named candidates of the piece, or -1
+    float x[NAMED + 1];
+    uint32_t adds = 0;                  // a bit each: whether it adds the candidate to the named
     if (REST) {
+#pragma unroll
+        for (int i = 0; i < NAMED; ++i) {
+            const int k = threadIdx.x + i * kThreads;
+            const int64_t place = k < d.K ? d.ids[row * d.K + k] - begin : -1;
+            at[i] = place >= 0 && place < count ? (int)place : -1;
+            x[i] = at[i] >= 0 ? as_float(piece[at[i]]) : -kInf;
+            top[1] = fmaxf(top[1], x[i]);
+        }
         names.template clear<kThreads>();
 #pragma unroll
         for (int j = 0; j < kVectors; ++j) s_row[j * kThreads + threadIdx.x] = held.raw[j];
-    }
-    top[0] = held.top();
-    over_workgroup<kThreads>(top, s_top, Max{});
-    const float base = base_of(top[0]), by = d.rate * kLog2e;
-    if (REST) {
-        for (int k = threadIdx.x; k < d.K; k += kThreads) {
-            const int64_t at = d.ids[row * d.K + k] - begin;
-            if (at < 0 || at >= count) continue;
-            if (names.add((int)at)) sum[1] += __builtin_amdgcn_exp2f((as_float(piece[at]) - base) * by);
-            reinterpret_cast<T*>(s_row)[at + skew] = as_value<T>(-kInf);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NAMED; ++i) {
+            if (at[i] < 0) continue;
+            if (names.add(at[i])) adds |= 1u << i;
+            reinterpret_cast<T*>(s_row)[at[i] + skew] = as_value<T>(-kInf);
         }
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kVectors; ++j) held.raw[j] = s_row[j * kThreads + threadIdx.x];
     }
-    sum[0] = held.sum(base, by);
+    top[0] = held.top();
+    over_workgroup<kThreads>(top, s_top, Max{});
+    const float others_top = top[0], base = base_of(fmaxf(top[0], top[1]));
+#pragma unroll
+    for (int i = 0; i < NAMED; ++i)
+        if (adds >> i & 1) sum[1] += __builtin_amdgcn_exp2f((x[i] - base) * by);
+    sum[0] = held.sum(base_of(others_top), by);
     over_workgroup<kThreads>(sum, s_sum, Add{});
-    if (threadIdx.x == 0) stats[row * pieces + blockIdx.x % pieces] = Stats{top[0], sum[0] + sum[1], sum[0]};
+    if (threadIdx.x) return;
+    Stats s = {fmaxf(top[0], top[1]), others_top, sum[0], sum[0]};
+    if (REST) s.all = sum[1] + others_scale(s, by) * sum[0];
+    stats[row * pieces + blockIdx.x % pieces] = s;
 }
-template <typename T, bool STREAM>
+template <typename T, bool REST, bool STREAM>
 __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, unsigned pieces, unsigned written, const Stats* stats, float* rows, T* dlogits) {
     using H = Held<T, kThreads, kVectors>;
     extern __shared__ float s_mem[];
     __shared__ Names<kThreads * H::N> names;
-    __shared__ float s_top[2][16], s_lse[1][16], s_sum[6][16];
+    __shared__ float s_top[3][16], s_lse[1][16], s_sum[6][16];
     const Ids ids(s_mem, d.K);
     const int64_t row = d.first + blockIdx.x / written, begin = (int64_t)(blockIdx.x % written) * kPiece<T>;
     const int count = (int)min(d.V - begin, (int64_t)kPiece<T>);
@@ -350,24 +392,26 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, u
     H held;
     if (dlogits) held.read(piece, count, skew);
     names.template clear<kThreads>();
-    float top[2] = {-kInf, -kInf};
+    float top[3] = {-kInf, -kInf, -kInf};      // of all, of the teacher's, of the others
     top[1] = read_ids<T, kThreads>(d, row, ids);
-    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) top[0] = fmaxf(top[0], stats[row * pieces + i].top);
+    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
+        top[0] = fmaxf(top[0], stats[row * pieces + i].top);
+        top[2] = fmaxf(top[2], stats[row * pieces + i].others_top);
+    }
     over_workgroup<kThreads>(top, s_top, Max{});
-    const float base = base_of(top[0]);
+    const float base = base_of(top[0]), others_base = base_of(top[2]), by = d.rate * kLog2e;
     float sum[6] = {};                  // all, others, mass, entropy, score, whether some id of the piece came twice
     for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
         const Stats o = stats[row * pieces + i];
-        const float f = __builtin_amdgcn_exp2f((base_of(o.top) - base) * d.rate * kLog2e);
-        sum[0] += o.all == 0.0f ? 0.0f : f * o.all;
-        sum[1] += o.others == 0.0f ? 0.0f : f * o.others;
+        sum[0] += o.all == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((base_of(o.top) - base) * by) * o.all;
+        sum[1] += o.others == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((base_of(o.others_top) - others_base) * by) * o.others;
     }
     for (int k = threadIdx.x; k < d.K; k += kThreads) {
         const int64_t at = ids.id[k] - begin;
         if (ids.id[k] >= 0 && at >= 0 && at < count && !names.add((int)at)) sum[5] = 1.0f;
     }
     float lse;
-    if (d.lse) {
+    if (REST) {
         lse = d.lse[row];
     } else {
         float t[1] = {teacher_sum(d, ids, base_of(top[1]), kThreads)};
@@ -380,11 +424,11 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, u
     sum[4] = mine.score;
     over_workgroup<kThreads>(sum, s_sum, Add{});
     const Terms t = {sum[2], sum[3], sum[4]};
-    if (t.mass == 0.0f && !d.lse) return nothing<T, kThreads>(d, row, begin, count, rows, dlogits);
-    const Stats s = {top[0], sum[0], sum[1]};
+    if (!REST && t.mass == 0.0f) return nothing<T, kThreads>(d, row, begin, count, rows, dlogits);
+    const Stats s = {top[0], top[2], sum[0], sum[1]};
     const float rest = rest_of(d, t.mass);
-    if (threadIdx.x == 0 && begin == 0) rows[row] = weight * loss_of(t, rest, s);
-    if (dlogits) write_grad<STREAM>(d, held, row, begin, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
+    if (threadIdx.x == 0 && begin == 0) rows[row] = weight * loss_of(t, rest, s, d.rate);
+    if (dlogits) write_grad<REST, STREAM>(d, held, row, begin, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
 }
 
 // Sum of the rows' losses, in a fixed order.
@@ -453,10 +497,13 @@ int launch(const tns_distill_desc& a, float* loss, float* rows, T* dlogits, void
         const int64_t most = std::max<int64_t>(std::min((a.B + parts - 1) / parts, ((int64_t)1 << 31) / kThreads / pieces), 1);
         for (d.first = 0; d.first < a.B; d.first += most) {
             const unsigned n = (unsigned)std::min(a.B - d.first, most);
-            if (a.d_lse) hipLaunchKernelGGL((k_distill_stats<T, true>), dim3(n * pieces), dim3(kThreads), 0, stream, d, pieces, stats);
-            else hipLaunchKernelGGL((k_distill_stats<T, false>), dim3(n * pieces), dim3(kThreads), 0, stream, d, pieces, stats);
-            if (parts > 1) hipLaunchKernelGGL((k_distill_grad<T, true>), dim3(n * written), dim3(kThreads), lds, stream, d, pieces, written, stats, rows, dlogits);
-            else hipLaunchKernelGGL((k_distill_grad<T, false>), dim3(n * written), dim3(kThreads), lds, stream, d, pieces, written, stats, rows, dlogits);
+            auto with = [&](auto rest) {
+                hipLaunchKernelGGL((k_distill_stats<T, rest()>), dim3(n * pieces), dim3(kThreads), 0, stream, d, pieces, stats);
+                if (parts > 1) hipLaunchKernelGGL((k_distill_grad<T, rest(), true>), dim3(n * written), dim3(kThreads), lds, stream, d, pieces, written, stats, rows, dlogits);
+                else hipLaunchKernelGGL((k_distill_grad<T, rest(), false>), dim3(n * written), dim3(kThreads), lds, stream, d, pieces, written, stats, rows, dlogits);
+            };
+            if (a.d_lse) with(std::true_type{});
+            else with(std::false_type{});
         }
     }
     hipLaunchKernelGGL(k_distill_sum, dim3(1), dim3(1024), 0, stream, rows, a.B, d.scale, loss);

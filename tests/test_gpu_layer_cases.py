@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import layer_oracle as O
-from test_gpu_layer import L, on_gpu, the_events      # noqa: F401
+from test_gpu_layer import L, check_distill, on_gpu, the_events, the_scores      # noqa: F401
 from test_gpu_train import BF16, F32, close, torch_of, values
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +63,52 @@ def test_attend_long_lists_in_blocks_of_512_rows(L):      # noqa: F811
     L.tns_attend_grad(desc, saved.data_ptr(), dout.data_ptr(), *[t.data_ptr() for t in out[1:]], 0, ws.data_ptr(), ws.numel(), stream)
     for t in out:
         assert not t.any()                                        # (a NaN is true)
+
+
+# ---- distillation: named candidates far above the others --------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [4, 50, 600, 3001, 9000, 40000])
+@pytest.mark.parametrize("lead", [60.0, 90.0, 100.0, 128.0, 300.0, 1000.0, 4096.0])
+def test_distill_named_far_above_the_others(L, lead, n, dtype):      # noqa: F811
+    """A student that is sure of named candidates: the others' mass is compared in the logarithm, and their gradients stay numbers.  Of the named, one
+    leads (rows 0, 1), all do (2), or the last of the row alone is unnamed and far below (3); an unnamed one leads in row 4."""
+    rng = np.random.default_rng(n + int(lead))
+    K = min(n - 1, 12)
+    a = the_scores(rng, 5, n, K, dtype, True)
+    for b in range(5):
+        a["ids"][b] = rng.permutation(n - 1)[:K]
+    for b in (0, 1):
+        a["logits"][b, a["ids"][b, 0]] += lead
+    a["logits"][2, a["ids"][2]] += lead
+    a["logits"][3, n - 1] -= lead
+    a["logits"][4, n - 1] += lead
+    if dtype == BF16:
+        a["logits"] = torch_of(a["logits"], BF16).float().cpu().numpy()
+    check_distill(L, a, dtype, temperature=1.0)
+    check_distill(L, a, dtype, temperature=0.5)
+    for temperature in (1.0, 0.5):
+        r = L.distill(**{k: torch_of(v, dtype if k == "logits" else None) for k, v in a.items()}, temperature=temperature)
+        assert bool(r["rows"].isfinite().all()) and bool(r["dlogits"].isfinite().all())
+
+
+def test_distill_a_sure_student_in_numbers(L):      # noqa: F811
+    import torch
+    logits = torch.tensor([[100.0, 0.0, 0.5, -1.0]], device="cuda")
+    r = L.distill(logits, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.tensor([[0.7]], device="cuda").log(), lse=torch.zeros(1, device="cuda"))
+    e = np.exp([0.0, 0.5, -1.0])
+    # 0.7 log 0.7 + 0.3 (log 0.3 - log(1 + exp 0.5 + exp -1) + 100); the scores' difference and the logarithm are some ten roundings of values up to 100
+    assert abs(float(r["loss"]) - (0.7 * np.log(0.7) + 0.3 * (np.log(0.3) - np.log(e.sum()) + 100))) < 10 * 2 ** -24 * 100
+    assert np.allclose(r["dlogits"].cpu().numpy()[0], np.concatenate([[0.3], -0.3 * e / e.sum()]), rtol=0, atol=20 * 2 ** -24)
+
+
+def test_distill_others_that_are_all_ruled_out(L):      # noqa: F811
+    """Mass of others whose scores are all -infinity: an infinite loss as the header says, and no gradient by them."""
+    import torch
+    inf = float("inf")
+    ids, teacher = torch.tensor([[0, 2]], dtype=torch.int32, device="cuda"), torch.tensor([[0.4, 0.4]], device="cuda").log()
+    for n in (4, 40000):
+        logits = torch.full((1, n), -inf, device="cuda")
+        logits[0, 0], logits[0, 2] = 1.0, -3.0
+        r = L.distill(logits, ids, teacher, lse=torch.zeros(1, device="cuda"))
+        assert float(r["rows"][0]) == inf and not r["dlogits"][0, 3:].any() and bool(r["dlogits"].isfinite().all())

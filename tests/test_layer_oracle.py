@@ -115,6 +115,17 @@ def test_distill_closed_forms_and_differences(rest):
     assert O.distill(np.zeros((1, 8)), np.int32([[-1]]), np.zeros((1, 1)))["loss"] == 0
 
 
+def test_distill_named_far_above_the_others():
+    """One named candidate of score 100 and more above three others: the others' share of the loss is a sum in the logarithm."""
+    for lead in (100.0, 1000.0):
+        s = np.float64([[lead, 0.0, 0.5, -1.0]])
+        r = O.distill(s, np.int32([[0]]), np.log([[0.7]]), lse=np.zeros(1))
+        others = np.exp(s[0, 1:]) / np.exp(s[0, 1:]).sum()
+        # log q of the named one is 0 but for exp(-99), that of the others together log of their sum minus the lead
+        assert np.isclose(r["loss"], 0.7 * np.log(0.7) + 0.3 * (np.log(0.3) - (np.log(np.exp(s[0, 1:]).sum()) - lead)), rtol=1e-12)
+        assert np.allclose(r["dlogits"][0], np.concatenate([[0.3], -0.3 * others]), rtol=1e-12) and np.isfinite(r["dlogits_off"]).all()
+
+
 # ---- interface -----------------------------------------------------------------------------------
 
 def test_every_declared_symbol_is_exported_and_bound():
