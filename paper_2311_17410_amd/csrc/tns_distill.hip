@@ -227,15 +227,25 @@ __device__ __forceinline__ void nothing(const Distill<T>& d, int64_t row, int64_
     if (dlogits) tns::zero_values(dlogits + row * d.V + begin, count, threadIdx.x, THREADS);
 }
 
-// Which candidates of a piece some id names, a bit each.
+// Whether no lower k has the same id: of a candidate that is named more than once the lowest k's thread adds it to the named, whichever comes first.
+__device__ __forceinline__ bool first_of(const int32_t* ids, int k) {
+    for (int i = 0; i < k; ++i)
+        if (ids[i] == ids[k]) return false;
+    return true;
+}
+
+// Which candidates of a piece some id names, a bit each, and whether some id came twice.
 template <int PLACES>
 struct Names {
-    uint32_t word[(PLACES + 31) / 32];
+    uint32_t twice, word[(PLACES + 31) / 32];
     template <int THREADS>
     __device__ __forceinline__ void clear() {
         for (int i = threadIdx.x; i < (PLACES + 31) / 32; i += THREADS) word[i] = 0;
+        if (threadIdx.x == 0) twice = 0;
     }
-    __device__ __forceinline__ bool add(int at) { return !(atomicOr(&word[at >> 5], 1u << (at & 31)) >> (at & 31) & 1); }      // whether it was not there
+    __device__ __forceinline__ void add(int at) {
+        if (atomicOr(&word[at >> 5], 1u << (at & 31)) >> (at & 31) & 1) twice = 1;
+    }
 };
 
 // A whole row in a workgroup's registers: read once, written once.  Bound by memory where there are many rows: 4000 of 10000 bf16 scores with
@@ -250,7 +260,7 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
     extern __shared__ float s_mem[];
     __shared__ typename H::Vec s_row[REST ? THREADS * NV : 1];
     __shared__ Names<PLACES> names;
-    __shared__ float s_top[2][16], s_lse[1][16], s_sum[6][16];
+    __shared__ float s_top[2][16], s_lse[1][16], s_sum[5][16];
     const Ids ids(s_mem, d.K);
     const int64_t row = d.first + blockIdx.x;
     const float weight = d.weight ? d.weight[row] : 1.0f;
@@ -262,8 +272,7 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
     names.template clear<THREADS>();
     float top[2];                       // of the row (REST: of the others); of the teacher's (REST: of the named)
     top[1] = read_ids<T, THREADS>(d, row, ids);
-    float sum[6] = {};                  // over the row (REST: without the named), over the named, mass, entropy, score, whether some id came twice
-    uint32_t adds = 0;                  // of the thread's ids, a bit each: whether it adds the candidate to the named
+    float sum[5] = {};                  // over the row (REST: without the named), over the named, mass, entropy, score
     if (REST) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) s_row[j * THREADS + threadIdx.x] = held.raw[j];
@@ -273,11 +282,10 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
         top[0] = held.top();
         over_workgroup<THREADS>(top, s_top, Max{});
     }
-    for (int k = threadIdx.x, bit = 0; k < d.K; k += THREADS, ++bit) {
+    for (int k = threadIdx.x; k < d.K; k += THREADS) {
         const int at = ids.id[k];
         if (at < 0) continue;
-        if (names.add(at)) adds |= 1u << bit;
-        else sum[5] = 1.0f;
+        names.add(at);
         if (REST) {
             reinterpret_cast<T*>(s_row)[at + skew] = as_value<T>(-kInf);
             top[1] = fmaxf(top[1], ids.x[k]);
@@ -300,8 +308,8 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
     }
     const float base = base_of(top[0]), by = d.rate * kLog2e;
     if (REST)
-        for (int k = threadIdx.x, bit = 0; k < d.K; k += THREADS, ++bit)
-            if (adds >> bit & 1) sum[1] += __builtin_amdgcn_exp2f((ids.x[k] - base) * by);
+        for (int k = threadIdx.x; k < d.K; k += THREADS)
+            if (ids.id[k] >= 0 && (!names.twice || first_of(ids.id, k))) sum[1] += __builtin_amdgcn_exp2f((ids.x[k] - base) * by);
     const Terms mine = terms_of<T, THREADS>(d, ids, lse, base);
     sum[0] = held.sum(REST ? base_of(others_top) : base, by);
     sum[2] = mine.mass;
@@ -314,7 +322,7 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
     if (REST) s.all = sum[1] + others_scale(s, by) * sum[0];
     const float rest = rest_of(d, t.mass);
     if (threadIdx.x == 0) rows[row] = weight * loss_of(t, rest, s, d.rate);
-    if (dlogits) write_grad<REST, false>(d, held, row, 0, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
+    if (dlogits) write_grad<REST, false>(d, held, row, 0, count, skew, s, t.mass, rest, weight, ids, names.twice, dlogits);
 }
 
 // Rows of several pieces: the pieces' statistics, then their gradients.  200 rows of 500009 fp32 scores: 95 and 142 us before the second pass
@@ -339,7 +347,6 @@ __global__ void __launch_bounds__(kThreads) k_distill_stats(const Distill<T> d, 
     constexpr int NAMED = REST ? kMostIds / kThreads : 0;
     int at[NAMED + 1];                  // the thread's named candidates of the piece, or -1
     float x[NAMED + 1];
-    uint32_t adds = 0;                  // a bit each: whether it adds the candidate to the named
     if (REST) {
 #pragma unroll
         for (int i = 0; i < NAMED; ++i) {
@@ -356,7 +363,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_stats(const Distill<T> d, 
 #pragma unroll
         for (int i = 0; i < NAMED; ++i) {
             if (at[i] < 0) continue;
-            if (names.add(at[i])) adds |= 1u << i;
+            names.add(at[i]);
             reinterpret_cast<T*>(s_row)[at[i] + skew] = as_value<T>(-kInf);
         }
         __syncthreads();
@@ -368,7 +375,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_stats(const Distill<T> d, 
     const float others_top = top[0], base = base_of(fmaxf(top[0], top[1]));
 #pragma unroll
     for (int i = 0; i < NAMED; ++i)
-        if (adds >> i & 1) sum[1] += __builtin_amdgcn_exp2f((x[i] - base) * by);
+        if (at[i] >= 0 && (!names.twice || first_of(d.ids + row * d.K, threadIdx.x + i * kThreads))) sum[1] += __builtin_amdgcn_exp2f((x[i] - base) * by);
     sum[0] = held.sum(base_of(others_top), by);
     over_workgroup<kThreads>(sum, s_sum, Add{});
     if (threadIdx.x) return;
@@ -381,7 +388,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, u
     using H = Held<T, kThreads, kVectors>;
     extern __shared__ float s_mem[];
     __shared__ Names<kThreads * H::N> names;
-    __shared__ float s_top[3][16], s_lse[1][16], s_sum[6][16];
+    __shared__ float s_top[3][16], s_lse[1][16], s_sum[5][16];
     const Ids ids(s_mem, d.K);
     const int64_t row = d.first + blockIdx.x / written, begin = (int64_t)(blockIdx.x % written) * kPiece<T>;
     const int count = (int)min(d.V - begin, (int64_t)kPiece<T>);
@@ -400,7 +407,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, u
     }
     over_workgroup<kThreads>(top, s_top, Max{});
     const float base = base_of(top[0]), others_base = base_of(top[2]), by = d.rate * kLog2e;
-    float sum[6] = {};                  // all, others, mass, entropy, score, whether some id of the piece came twice
+    float sum[5] = {};                  // all, others, mass, entropy, score
     for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
         const Stats o = stats[row * pieces + i];
         sum[0] += o.all == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((base_of(o.top) - base) * by) * o.all;
@@ -408,7 +415,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, u
     }
     for (int k = threadIdx.x; k < d.K; k += kThreads) {
         const int64_t at = ids.id[k] - begin;
-        if (ids.id[k] >= 0 && at >= 0 && at < count && !names.add((int)at)) sum[5] = 1.0f;
+        if (ids.id[k] >= 0 && at >= 0 && at < count) names.add((int)at);
     }
     float lse;
     if (REST) {
@@ -428,7 +435,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, u
     const Stats s = {top[0], top[2], sum[0], sum[1]};
     const float rest = rest_of(d, t.mass);
     if (threadIdx.x == 0 && begin == 0) rows[row] = weight * loss_of(t, rest, s, d.rate);
-    if (dlogits) write_grad<REST, STREAM>(d, held, row, begin, count, skew, s, t.mass, rest, weight, ids, sum[5] != 0.0f, dlogits);
+    if (dlogits) write_grad<REST, STREAM>(d, held, row, begin, count, skew, s, t.mass, rest, weight, ids, names.twice, dlogits);
 }
 
 // Sum of the rows' losses, in a fixed order.

@@ -112,3 +112,21 @@ def test_distill_others_that_are_all_ruled_out(L):      # noqa: F811
         logits[0, 0], logits[0, 2] = 1.0, -3.0
         r = L.distill(logits, ids, teacher, lse=torch.zeros(1, device="cuda"))
         assert float(r["rows"][0]) == inf and not r["dlogits"][0, 3:].any() and bool(r["dlogits"].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype, n", [(F32, 1500), (F32, 9000), (BF16, 5000), (BF16, 20000), (F32, 40000), (BF16, 70000)])
+def test_distill_same_bits_in_every_row_where_ids_come_twice(L, dtype, n):      # noqa: F811
+    """Two thousand rows that are the same one: candidates that threads of different waves name come to the same sum, whichever thread is first."""
+    import torch
+    rng = np.random.default_rng(n)
+    a = the_scores(rng, 1, n, 1024, dtype, True)
+    for k in range(0, 1024, 128):
+        a["ids"][0, k + 64: k + 128] = a["ids"][0, k: k + 64][::-1]      # twice, in the next wave
+    a["ids"][0, 1000:] = a["ids"][0, 100:124]                     # and more often
+    a["logits"][0, a["ids"][0]] += values(rng, 1024, dtype, 2.0)
+    a["lse"][0] = np.log(np.exp(a["teacher"].astype(np.float64)).sum()) + 0.5
+    g = {k: None if v is None else torch_of(np.repeat(v, 2000, 0), dtype if k == "logits" else None) for k, v in a.items()}
+    r = L.distill(**g)
+    assert bool((r["rows"] == r["rows"][0]).all()) and bool((r["dlogits"] == r["dlogits"][0]).all())
+    a["logits"] = g["logits"][:1].float().cpu().numpy()
+    check_distill(L, a, dtype, temperature=1.0)
