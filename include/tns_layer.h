@@ -29,7 +29,8 @@ extern "C" {
  *     score  = scale * q . k + table[bucket][h]
  *     out    = sum p v, p = softmax of the scores over the list
  * An event is left out, whatever its rows of k and v hold, where its mask is 0, its index is outside [0, num), or, head by head, its
- * table entry is -infinity.  Where no event is left out is zero, and its gradients are.
+ * table entry is -infinity (a finite one, however low, leaves nothing out).  Where no event is left out is zero, and its gradients are.
+ * Scores are rounded to fp32: beside a table entry of 1e9, say, what q . k says below 64 is lost.
  *
  *   S, d_rowptr[S+1]  lists, as in tns_recur.  S < 2^31
  *   rows              rows that the events' arrays have room for, at least d_rowptr[S]; rows from d_rowptr[S] on do not count,

@@ -438,11 +438,17 @@ struct Known {
     }
 };
 
+// A table's entry in powers of two.  Times log2 e, the largest finite numbers (the lowest one as a mask is one) would become infinite, and only an infinite
+// entry leaves its events out: from 2^126 on the factor is smaller.  Entries that differ differ by 2^103 or more there, so p is 0 or 1 by any factor.
+__device__ __forceinline__ float in_powers(float v) {
+    constexpr float from = 0x1p126f, by = 0.85f;      // (by * FLT_MAX + from * (log2 e - by) is 3.397e38)
+    return fabsf(v) < from ? v * kLog2e : v * by + copysignf(from * (kLog2e - by), v);
+}
 // Edges and table in LDS, the table in powers of two.
 template <typename T>
 __device__ __forceinline__ void stage(const Attend<T>& a, float* s_edges, float* s_table) {
     for (int i = threadIdx.x; i < a.buckets - 1; i += kWaves * kWave) s_edges[i] = a.edges[i];
-    for (int i = threadIdx.x; i < max(a.buckets, 1) * a.heads; i += kWaves * kWave) s_table[i] = a.buckets ? a.table[i] * kLog2e : 0.0f;
+    for (int i = threadIdx.x; i < max(a.buckets, 1) * a.heads; i += kWaves * kWave) s_table[i] = a.buckets ? in_powers(a.table[i]) : 0.0f;
     __syncthreads();
 }
 

@@ -65,6 +65,49 @@ def test_attend_long_lists_in_blocks_of_512_rows(L):      # noqa: F811
         assert not t.any()                                        # (a NaN is true)
 
 
+# ---- attention: table entries at the ends of fp32 --------------------------------------------------
+
+LOWEST, LARGEST = float(np.finfo(np.float32).min), float(np.finfo(np.float32).max)
+BF16_LOWEST = -float.fromhex("0x1.fep127")
+
+
+def the_ends(rng, dtype, many, gathered=False):
+    """Lists whose events have, by place, table entries of two ends of fp32; equal queries, so that the events of the higher entry have equal p."""
+    lens = np.array([1, 30, 0, 700, 6000, 64, 2] + [5, 0, 12, 1, 9] * (1700 if many else 3))
+    a = the_events(rng, lens, 2, 2, 16, dtype, buckets=2, times=False)
+    a["edges"] = np.float32([3])                                  # three events of the first bucket, the others in the second
+    a["q"][:] = 0
+    if gathered:
+        a["index"] = rng.permutation(int(a["rowptr"][-1])).astype(np.int32)
+    return a, lens
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("many, gathered", [(False, False), (True, False), (True, True)])
+@pytest.mark.parametrize("first, second", [(LOWEST, LOWEST), (LOWEST, 0.0), (0.0, LOWEST), (LOWEST, -3e38), (LOWEST, BF16_LOWEST), (-2.4e38, -2.5e38), (-2.3e38, -2.4e38), (LARGEST, LARGEST), (LARGEST, 3e38),
+                                           (1.0, LARGEST), (LOWEST, LARGEST), (-1e30, LOWEST), (LOWEST, float("-inf")), (float("-inf"), LARGEST), (-8.5e37, -8.6e37), (2.0 ** 126, 2.0 ** 126 * (1 - 2.0 ** -20))])
+def test_attend_table_entries_at_the_ends(L, first, second, many, gathered, dtype):      # noqa: F811
+    """The lowest finite number of a type is a number: events of nothing else have equal parts, and beside a higher one no part.  Only -infinity leaves out."""
+    rng = np.random.default_rng(60)
+    a, lens = the_ends(rng, dtype, many, gathered)
+    a["table"] = np.float32([[first, first], [second, second]])
+    out = L.attend_run(**on_gpu(a, dtype))["out"].float().cpu().numpy()
+    v = a["v"].astype(np.float64) if not gathered else a["v"][a["index"]].astype(np.float64)
+    for s in range(len(lens)):
+        rows = v[a["rowptr"][s]: a["rowptr"][s + 1]]
+        parts = [(entry, of) for entry, of in ((first, rows[:3]), (second, rows[3:])) if len(of) and entry != -np.inf]
+        if not parts:
+            assert not out[s].any()
+            continue
+        top = max(entry for entry, _ in parts)
+        rows = np.concatenate([of for entry, of in parts if entry == top])
+        mean = rows.mean(0)
+        # every p is 1 before the sum and the sum a whole number; at most 128 additions one after the other (a slot takes 64 events, the joins the rest), a
+        # reciprocal and a product
+        off = (128 + 4) * 2.0 ** -24 * np.abs(rows).mean(0) + (2.0 ** -8 * np.abs(mean) if dtype == BF16 else 0)
+        assert (np.abs(out[s] - mean) <= off).all(), s
+
+
 # ---- distillation: named candidates far above the others --------------------------------------------
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
