@@ -127,9 +127,7 @@ def attend(rowptr, q, k, v, t=None, ts=None, edges=None, table=None, index=None,
             if dout is None:
                 continue
             d = dout[s, h].astype(np.float64)
-            # p once more, from the logarithm of the sum: rounded, as is its difference with the score
-            lse = score.v.max() + np.log(total.v)
-            p = V(p.v, p.e + p.v * (4 * U * (np.abs(lse) + np.abs(score.v)) + 8 * U))
+            p = p.wider(8 * U)          # once more, from the largest score and one over the sum, rounded
             dp, delta = V(d[None] * vv).sum(1, dim + 3), (o * d).sum(0, dim + 3)
             ds = p * (dp - delta)
             col = lambda x: V(x.v[:, None], x.e[:, None])      # noqa: E731

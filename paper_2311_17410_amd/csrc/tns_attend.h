@@ -458,6 +458,15 @@ struct Work {
     float* tables;                      // [workgroups of the gradients, buckets * heads]
 };
 
+// What the gradients need of a list's softmax to have its p again: the largest score, in powers of two, and one over the sum of the others by it (0 where no
+// event counts).  The logarithm of the sum, added to the largest score, would be rounded to that one's last place: beside a table of -1e4 p
+// would be off by 7e-4, beside one of -1e9 by any factor.
+struct Norm {
+    float top, inverse;
+    __device__ Norm() {}
+    __device__ Norm(float top, float sum, float inverse) : top(sum == 0.0f ? 0.0f : top), inverse(inverse) {}
+};
+
 // What a kernel is called with, read again where it is used: some sixty scalar registers would hold it otherwise, and as many values of the loops
 // would be moved to vector registers and back.
 template <typename T>
@@ -466,7 +475,8 @@ struct Args {
     Cut cut;
     Work work;
     T* out;
-    float *saved_out, *saved_lse;       // (the gradients read them)
+    float* saved_out;                   // (the gradients read what is saved)
+    Norm* saved_norm;
     const T* dout;
     T *dq, *dk, *dv;
     int tables;                         // whether the table's gradient is wanted
@@ -691,7 +701,7 @@ Layout carve(const tns_attend& a, const Cut& c, bool grad, void* base) {
     return l;
 }
 size_t saved_out_bytes(const tns_attend& a) { return aligned((size_t)a.S * a.heads * a.head_dim * 4); }
-inline size_t saved_bytes(const tns_attend& a) { return saved_out_bytes(a) + aligned((size_t)a.S * a.heads * 4); }
+inline size_t saved_bytes(const tns_attend& a) { return saved_out_bytes(a) + aligned((size_t)a.S * a.heads * sizeof(Norm)); }
 
 template <typename T>
 Attend<T> typed(const tns_attend& a) {

@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kWaves* kWave) k_attend(const Args<T>) {
                 at.write(end.out + row, g * end.a.dim, sums.acc[g]);
                 if (!end.saved_out) continue;
                 at.write(end.saved_out + row, g * end.a.dim, sums.acc[g]);
-                if (at.mine == 0) end.saved_lse[to + at.kv * end.a.group + g] = sums.l[g] == 0.0f ? kInf : sums.m[g] + __builtin_amdgcn_logf(sums.l[g]);
+                if (at.mine == 0) end.saved_norm[to + at.kv * end.a.group + g] = Norm(sums.m[g], sums.l[g], weight);
             }
         }
     Walk<T> walk(begin, stride);
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kWaves* kWave) k_attend(const Args<T>) {
         for (int g = 0; g < G; ++g) {
             if (g >= group) break;
             const float top = over_strided(sums.m[g], width, Max{}), f = sums.m[g] == -kInf ? 0.0f : __builtin_amdgcn_exp2f(sums.m[g] - top);
-            const float sum = over_strided(sums.l[g] * f, width, Add{}), weight = !w.whole ? f : sum == 0.0f ? 0.0f : f * __builtin_amdgcn_rcpf(sum);
+            const float sum = over_strided(sums.l[g] * f, width, Add{}), inverse = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum), weight = w.whole ? f * inverse : f;
 #pragma unroll
             for (int i = 0; i < N; ++i) sums.acc[g][i] *= weight;
             if (at.head && at.slot == 0 && at.mine == 0) {
@@ -184,8 +184,8 @@ __global__ void __launch_bounds__(kWaves* kWave) k_attend(const Args<T>) {
                 if (!w.whole) {
                     *lane_at<float>(end.work.stats + 2 * to, 8 * h) = top;
                     *lane_at<float>(end.work.stats + 2 * to, 8 * h + 4) = sum;
-                } else if (end.saved_lse) {
-                    *lane_at<float>(end.saved_lse + to, 4 * h) = sum == 0.0f ? kInf : top + __builtin_amdgcn_logf(sum);      // (sum is 1 at least)
+                } else if (end.saved_out) {
+                    *lane_at<Norm>(end.saved_norm + to, (uint32_t)sizeof(Norm) * h) = Norm(top, sum, inverse);
                 }
             }
             at.joined(end.a, end.cut, g, sums.acc[g], [&](uint32_t c, float x, float y, auto two_) {
@@ -199,15 +199,16 @@ __global__ void __launch_bounds__(kWaves* kWave) k_attend(const Args<T>) {
 
 // 6563 parts of 3001 histories: 25 us; 13125 of seven lists: 26.
 template <typename T>
-__global__ void __launch_bounds__(1024) k_attend_join(const Attend<T> a, const Cut cut, const Work work, unsigned few, T* out, float* saved_out, float* saved_lse) {
+__global__ void __launch_bounds__(1024) k_attend_join(const Attend<T> a, const Cut cut, const Work work, unsigned few, T* out, float* saved_out, Norm* saved_norm) {
     __shared__ float s_sum[1024];
     auto write = [&](int64_t list, int64_t h, int c, float top, float l, float acc) {
         const int64_t to = list * a.heads + h;
-        acc = l == 0.0f ? 0.0f : acc / l;
+        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+        acc *= inverse;
         out[to * a.dim + c] = as_value<T>(acc);
         if (saved_out) {
             saved_out[to * a.dim + c] = acc;
-            if (c == 0) saved_lse[to] = l == 0.0f ? kInf : top + __log2f(l);
+            if (c == 0) saved_norm[to] = Norm(top, l, inverse);
         }
     };
     if (blockIdx.x < few) {
@@ -317,12 +318,12 @@ int tns_attend_run(const tns_attend* a, void* d_out, void* d_saved, void* d_work
     if (a->S == 0) return TNS_OK;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     float* const saved = static_cast<float*>(d_saved);
-    float* const lse = saved ? saved + saved_out_bytes(*a) / 4 : nullptr;
+    Norm* const norms = saved ? reinterpret_cast<Norm*>(saved + saved_out_bytes(*a) / 4) : nullptr;
     const size_t lds = lds_of(*a, 0);
     choose(*a, c, [&](auto value, auto vec, auto group, auto lanes) {
         using T = decltype(value);
         const Attend<T> t = typed<T>(*a);
-        const Args<T> args = {t, c, l.w, static_cast<T*>(d_out), saved, lse, nullptr, nullptr, nullptr, nullptr, 0};
+        const Args<T> args = {t, c, l.w, static_cast<T*>(d_out), saved, norms, nullptr, nullptr, nullptr, nullptr, 0};
         auto launch = [&](auto kernel, int& per_cu) {
             hipLaunchKernelGGL(kernel, dim3(groups_of(*a, c, resident(kernel, lds, per_cu)), c.turns), dim3(kWaves * kWave), lds, stream, args);
         };
@@ -331,7 +332,7 @@ int tns_attend_run(const tns_attend* a, void* d_out, void* d_saved, void* d_work
         else if (a->d_index) launch(k_attend<T, vec(), group(), lanes(), 1>, per_cu[1]);
         else launch(k_attend<T, vec(), group(), lanes(), 0>, per_cu[0]);
         if (const unsigned few = (unsigned)few_of(*a, c))
-            hipLaunchKernelGGL((k_attend_join<T>), dim3(few + (unsigned)many_of(*a, c)), dim3(1024), 0, stream, t, c, l.w, few, static_cast<T*>(d_out), saved, lse);
+            hipLaunchKernelGGL((k_attend_join<T>), dim3(few + (unsigned)many_of(*a, c)), dim3(1024), 0, stream, t, c, l.w, few, static_cast<T*>(d_out), saved, norms);
     });
     return launched("tns_attend_run");
 }

@@ -8,7 +8,8 @@ template <typename T, int VEC, int G, bool EXACT>
 struct Back {
     static constexpr int N = Row<T, VEC>::N;
     Row<T, VEC> q[G], d[G];             // query, gradient by the output
-    float acc[G][N], lse[G], delta[G];  // gradient by the query; logarithm of the sum, in powers of two; gradient by the output times the output
+    float acc[G][N], delta[G];          // gradient by the query; gradient by the output times the output
+    Norm norm[G];
     __device__ Back() {
 #pragma unroll
         for (int g = 0; g < G; ++g)
@@ -25,7 +26,7 @@ struct Back {
         at.heads(a, a.q + list * a.ld_q, q);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            lse[g] = g < a.group ? now.saved_lse[list * a.heads + at.kv * a.group + g] : kInf;
+            norm[g] = now.saved_norm[list * a.heads + at.kv * a.group + min(g, a.group - 1)];
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) dot += at.counts(i) ? d[g].get(i) * out[g][i] : 0.0f;
@@ -55,7 +56,7 @@ struct Back {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const float score = over_head<LANES>(k.template dot<!EXACT>(q[g], at.mask), cut.lanes), dp = over_head<LANES>(v.template dot<!EXACT>(d[g], at.mask), cut.lanes);
-            const float p = counts[g] ? __builtin_amdgcn_exp2f(score * a.scale + ds[g] - lse[g]) : 0.0f;
+            const float p = counts[g] ? __builtin_amdgcn_exp2f(score * a.scale + ds[g] - norm[g].top) * norm[g].inverse : 0.0f;
             ds[g] = counts[g] ? p * (dp - delta[g]) : 0.0f;
             const float by = ds[g] * scale;
             if (careful) {
@@ -92,7 +93,7 @@ __device__ __forceinline__ void add_to_table(const Attend<T>& a, const Cut& cut,
     }
 }
 
-// One pass over k and v: the scores again, p from the saved logarithm of their sum, and all gradients of an event while its rows are in
+// One pass over k and v: the scores again, p from the largest and the sum that were saved, and all gradients of an event while its rows are in
 // registers.  ds = p (dp - delta) with dp = dout . v; delta = dout . out from outputs saved in fp32 (of bf16 ones the difference would keep their rounding,
 // and the table's gradient, in which most of it cancels, would show it).  Bound by memory: 131072 lists of ten, two heads of 64 bf16 channels, 1.35 GB in
 // 259 us (5.2 TB/s); 3001 histories, eight heads of 32 fp32 channels on four, 1.65 GB in 342 us (4.8).
@@ -310,14 +311,14 @@ int tns_attend_grad(const tns_attend* a, const void* d_saved, const void* d_dout
     if (int e = check_workspace(d_workspace, workspace_bytes, l.bytes)) return e;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const float* const saved = static_cast<const float*>(d_saved);
-    const float* const lse = saved + saved_out_bytes(*a) / 4;
+    const Norm* const norms = reinterpret_cast<const Norm*>(saved + saved_out_bytes(*a) / 4);
     const size_t lds = lds_of(*a, kWaves << c.log_copies);
     if (int e = check_joins(*a, c)) return e;
     const unsigned few = (unsigned)few_of(*a, c), sums = (a->buckets * a->heads + kEntries - 1) / kEntries, joins = sums + few + (unsigned)many_of(*a, c);
     choose(*a, c, [&](auto value, auto vec, auto group, auto lanes) {
         using T = decltype(value);
         const Attend<T> t = typed<T>(*a);
-        const Args<T> args = {t, c, l.w, nullptr, const_cast<float*>(saved), const_cast<float*>(lse), static_cast<const T*>(d_dout), static_cast<T*>(d_dq),
+        const Args<T> args = {t, c, l.w, nullptr, const_cast<float*>(saved), const_cast<Norm*>(norms), static_cast<const T*>(d_dout), static_cast<T*>(d_dq),
                               static_cast<T*>(d_dk), static_cast<T*>(d_dv), d_dtable != nullptr};
         const auto kernel = k_attend_grad<T, vec(), group(), lanes()>;
         static int per_cu;

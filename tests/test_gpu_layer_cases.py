@@ -108,6 +108,23 @@ def test_attend_table_entries_at_the_ends(L, first, second, many, gathered, dtyp
         assert (np.abs(out[s] - mean) <= off).all(), s
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("entry", [100.0, -1e4, 1e4, -1e9, 1e9, -1e30, LOWEST, LARGEST])
+def test_attend_gradients_of_lists_in_one_far_bucket(L, entry, many, dtype):      # noqa: F811
+    """The softmax does not change where all scores have the same summand, and so do the gradients: those without a bias, whatever the entry."""
+    rng = np.random.default_rng(61)
+    a, lens = the_ends(rng, dtype, many)
+    a["table"] = np.full((2, 2), entry, np.float32)
+    dout = values(rng, a["q"].shape, dtype)
+    want = O.attend(**dict(a, table=np.zeros((2, 2), np.float32)), dout=dout)      # (the queries are zero: the entry is the score, exactly)
+    g = on_gpu(a, dtype)
+    r = L.attend_run(**g, save=True)
+    d = L.attend_grad(**g, saved=r["saved"], dout=torch_of(dout, dtype))
+    for name, got in dict(d, out=r["out"]).items():
+        close(name, got, want[name], want[name + "_off"], F32 if name == "dtable" else dtype)
+
+
 # ---- distillation: named candidates far above the others --------------------------------------------
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
