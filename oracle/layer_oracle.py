@@ -224,16 +224,18 @@ def distill(logits, ids, teacher, lse=None, weight=None, temperature=1.0, scale=
         named = (ids[b] >= 0) & (ids[b] < n)
         at = ids[b][named].astype(np.int64)
         with np.errstate(invalid="ignore"):
-            t = np.where(named, teacher[b].astype(np.float64) * rate, -np.inf)[named]
+            t = teacher[b].astype(np.float64)[named]
         some = ~np.isneginf(t)
         if lse is None and not some.any():
             continue
-        tt = V(np.where(some, t, 0.0)).wider(2 * U)
-        if lse is None:
-            top = t.max()
-            l = where(some, (tt - top).exp()).sum(0, len(t) + 30).log() + top
+        by = V(rate, 2 * U * rate)
+        t = np.where(some, t, 0.0)
+        if lse is None:                                           # (from the largest on: beside a far one the logarithm of the sum would be rounded away)
+            t = t - t[some].max()
+            tt = V(t, U * np.abs(t)) * by
+            l = where(some, tt.exp()).sum(0, len(t) + 30).log()
         else:
-            l = V(float(lse[b]))
+            tt, l = V(t) * by, V(float(lse[b]))
         logp = tt - l
         p = where(some, logp.exp())
         mass = p.sum(0, len(t) + 30)

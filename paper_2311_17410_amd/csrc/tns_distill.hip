@@ -119,7 +119,7 @@ __device__ __forceinline__ float base_of(float top) { return top == -kInf ? 0.0f
 // What is known of a row's ids, in LDS.
 struct Ids {
     int32_t* id;                        // -1 outside the candidates
-    float *p, *x;                       // teacher's probability (before it: score / temperature); student's score
+    float *p, *x;                       // teacher's probability (before it: score); student's score
     __device__ Ids(float* mem, int K) : id(reinterpret_cast<int32_t*>(mem)), p(mem + K), x(mem + 2 * K) {}
 };
 constexpr size_t ids_bytes(int K) { return (size_t)K * 12; }
@@ -131,7 +131,7 @@ __device__ __forceinline__ float read_ids(const Distill<T>& d, int64_t row, cons
     for (int k = threadIdx.x; k < d.K; k += THREADS) {
         const int32_t id = d.ids[row * d.K + k];
         const bool is = id >= 0 && id < d.V;
-        const float t = is ? d.teacher[row * d.K + k] * d.rate : -kInf;
+        const float t = is ? d.teacher[row * d.K + k] : -kInf;
         ids.id[k] = is ? id : -1;
         ids.p[k] = t;
         ids.x[k] = is ? as_float(d.logits[row * d.ld + id]) : 0.0f;
@@ -144,11 +144,13 @@ __device__ __forceinline__ float read_ids(const Distill<T>& d, int64_t row, cons
 struct Terms {
     float mass, entropy, score;
 };
+// log p = (teacher's score - from) / temperature - lse: without d_lse from the largest of them on and with the logarithm of their sum by it, since that
+// logarithm added to a far one, and one over the temperature times the lowest number, would be rounded away or infinite.
 template <typename T, int THREADS>
-__device__ __forceinline__ Terms terms_of(const Distill<T>& d, const Ids& ids, float lse, float base) {
+__device__ __forceinline__ Terms terms_of(const Distill<T>& d, const Ids& ids, float from, float lse, float base) {
     Terms t = {0.0f, 0.0f, 0.0f};
     for (int k = threadIdx.x; k < d.K; k += THREADS) {
-        const float l = ids.p[k] - lse, p = expf(l);
+        const float l = (ids.p[k] - from) * d.rate - lse, p = expf(l);
         ids.p[k] = p;
         t.mass += p;
         if (p != 0.0f) {
@@ -161,11 +163,11 @@ __device__ __forceinline__ Terms terms_of(const Distill<T>& d, const Ids& ids, f
 template <typename T>
 __device__ __forceinline__ float teacher_sum(const Distill<T>& d, const Ids& ids, float base, int threads) {
     float sum = 0.0f;
-    for (int k = threadIdx.x; k < d.K; k += threads) sum += expf(ids.p[k] - base);
+    for (int k = threadIdx.x; k < d.K; k += threads) sum += expf((ids.p[k] - base) * d.rate);
     return sum;
 }
 // (no entry: every p is exp(-infinity))
-__device__ __forceinline__ float teacher_lse(float base, float sum) { return sum > 0.0f || sum != sum ? base + logf(sum) : 0.0f; }
+__device__ __forceinline__ float teacher_lse(float sum) { return sum > 0.0f || sum != sum ? logf(sum) : 0.0f; }
 // The others' mass, and 0 without d_lse.
 template <typename T>
 __device__ __forceinline__ float rest_of(const Distill<T>& d, float mass) { return !d.lse ? 0.0f : mass == mass ? fmaxf(1.0f - mass, 0.0f) : mass; }
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
             top[1] = fmaxf(top[1], ids.x[k]);
         }
     }
-    float lse, others_top = -kInf;
+    float lse, from = 0.0f, others_top = -kInf;
     if (REST) {
         lse = d.lse[row];
         __syncthreads();
@@ -302,15 +304,16 @@ __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, flo
         others_top = top[0];
         top[0] = fmaxf(top[0], top[1]);
     } else {
-        float t[1] = {teacher_sum(d, ids, base_of(top[1]), THREADS)};
+        from = base_of(top[1]);
+        float t[1] = {teacher_sum(d, ids, from, THREADS)};
         over_workgroup<THREADS>(t, s_lse, Add{});
-        lse = teacher_lse(base_of(top[1]), t[0]);
+        lse = teacher_lse(t[0]);
     }
     const float base = base_of(top[0]), by = d.rate * kLog2e;
     if (REST)
         for (int k = threadIdx.x; k < d.K; k += THREADS)
             if (ids.id[k] >= 0 && (!names.twice || first_of(ids.id, k))) sum[1] += __builtin_amdgcn_exp2f((ids.x[k] - base) * by);
-    const Terms mine = terms_of<T, THREADS>(d, ids, lse, base);
+    const Terms mine = terms_of<T, THREADS>(d, ids, from, lse, base);
     sum[0] = held.sum(REST ? base_of(others_top) : base, by);
     sum[2] = mine.mass;
     sum[3] = mine.entropy;
@@ -417,15 +420,16 @@ __global__ void __launch_bounds__(kThreads) k_distill_grad(const Distill<T> d, u
         const int64_t at = ids.id[k] - begin;
         if (ids.id[k] >= 0 && at >= 0 && at < count) names.add((int)at);
     }
-    float lse;
+    float lse, from = 0.0f;
     if (REST) {
         lse = d.lse[row];
     } else {
-        float t[1] = {teacher_sum(d, ids, base_of(top[1]), kThreads)};
+        from = base_of(top[1]);
+        float t[1] = {teacher_sum(d, ids, from, kThreads)};
         over_workgroup<kThreads>(t, s_lse, Add{});
-        lse = teacher_lse(base_of(top[1]), t[0]);
+        lse = teacher_lse(t[0]);
     }
-    const Terms mine = terms_of<T, kThreads>(d, ids, lse, base);
+    const Terms mine = terms_of<T, kThreads>(d, ids, from, lse, base);
     sum[2] = mine.mass;
     sum[3] = mine.entropy;
     sum[4] = mine.score;

@@ -190,3 +190,24 @@ def test_distill_same_bits_in_every_row_where_ids_come_twice(L, dtype, n):      
     assert bool((r["rows"] == r["rows"][0]).all()) and bool((r["dlogits"] == r["dlogits"][0]).all())
     a["logits"] = g["logits"][:1].float().cpu().numpy()
     check_distill(L, a, dtype, temperature=1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [40, 3000, 40000])
+@pytest.mark.parametrize("temperature", [0.25, 1.0, 2.0])
+def test_distill_teachers_far_from_zero(L, temperature, n, dtype):      # noqa: F811
+    """The teacher's softmax does not change where all its scores have the same summand: far ones, and lists of nothing but a type's lowest or largest number."""
+    rng = np.random.default_rng(n)
+    a = the_scores(rng, 9, n, 10, dtype)
+    a["teacher"][:7] = np.round(a["teacher"][:7] * 4) / 4         # (whole quarters, which the sums below hold)
+    want = dict(a, teacher=a["teacher"].copy())
+    for b, far in enumerate((1e4, -1e4, 2.0 ** 21, -(2.0 ** 21))):
+        a["teacher"][b] += far
+    a["teacher"][4], a["teacher"][5], a["teacher"][6] = -1e9, LOWEST, LARGEST
+    want["teacher"][4:7] = 0
+    a["teacher"][7, 3:] = LOWEST                                  # beside ordinary ones the lowest number has no part
+    want["teacher"][7, 3:] = -np.inf
+    want = O.distill(**want, temperature=temperature)
+    r = L.distill(**{k: torch_of(v, dtype if k == "logits" else None) for k, v in a.items()}, temperature=temperature)
+    close("rows", r["rows"], want["rows"], want["rows_off"])
+    close("dlogits", r["dlogits"], want["dlogits"], want["dlogits_off"], dtype)
