@@ -426,7 +426,7 @@ struct Known {
         const bool inside = !a.index || (event.index >= 0 && event.index < a.num);
         index = inside ? event.index : 0;
         if (a.buckets > 1) {
-            const float age = a.ts ? gap_of(t, event.ts) : (float)newer;
+            const float age = a.ts ? gap_of(t, event.ts) : __ll2float_rz(newer);      // (rounded down: fp32 edges at or below a place are those at or below this)
             const int edges = a.buckets - 1;
             for (int by = a.steps; by; by >>= 1) {
                 const int to = bucket + by;

@@ -125,6 +125,23 @@ def test_attend_gradients_of_lists_in_one_far_bucket(L, entry, many, dtype):    
         close(name, got, want[name], want[name + "_off"], F32 if name == "dtable" else dtype)
 
 
+@pytest.mark.parametrize("newest_first", [True, False])
+def test_attend_places_beyond_24_bits(L, newest_first):      # noqa: F811
+    """An event with 2^24 + 3 newer ones lies below the border 2^24 + 4, which fp32 holds and rounds the place to; the next one on it."""
+    import torch
+    n, border = (1 << 24) + 64, (1 << 24) + 4
+    v = torch.zeros((n, 1, 1), device="cuda")
+    q, rowptr, edges = torch.zeros((1, 1, 1), device="cuda"), torch.tensor([0, n], device="cuda"), torch.tensor([float(border)], device="cuda")
+    row = lambda place: place if newest_first else n - 1 - place      # noqa: E731
+    for place, counts in ((border - 2, True), (border - 1, True), (border, False), (border + 1, False), (n - 1, False)):
+        mask = torch.zeros(n, dtype=torch.bool, device="cuda")
+        mask[row(place)] = True
+        v[row(place)] = 3.0
+        r = L.attend_run(rowptr, q, v, v, edges=edges, table=torch.tensor([[0.0], [float("-inf")]], device="cuda"), mask=mask, newest_first=newest_first)
+        assert float(r["out"]) == (3.0 if counts else 0.0), place
+        v[row(place)] = 0.0
+
+
 # ---- distillation: named candidates far above the others --------------------------------------------
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
