@@ -614,7 +614,7 @@ int check_arrays(const tns_attend* a) {
     if (a->ld_q < q_row || a->ld_k < k_row || a->ld_v < k_row) return fail(TNS_EINVAL, "rows of q, k or v overlap");
     if (a->ld_k >= (int64_t)1 << 22 || a->ld_v >= (int64_t)1 << 22) return fail(TNS_ESIZE, "rows of k or v are 2^22 values apart or more");
     if (a->S > 0 && (!a->d_rowptr || !a->d_q)) return fail(TNS_EINVAL, "null rowptr or q");
-    if (!a->d_index && a->num) return fail(TNS_EINVAL, "num without index");
+    if (!a->d_index && a->num && a->rows > 0) return fail(TNS_EINVAL, "num without index");      // (an index of no rows may have no address)
     if ((a->d_index ? a->num : a->rows) > 0 && (!a->d_k || !a->d_v)) return fail(TNS_EINVAL, "null k or v");
     if (a->S > 0 && a->rows > 0 && !a->d_t != !a->d_ts) return fail(TNS_EINVAL, "t and ts come together");
     if (a->buckets > 0 && !a->d_table) return fail(TNS_EINVAL, "null table");

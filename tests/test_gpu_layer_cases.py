@@ -142,6 +142,17 @@ def test_attend_places_beyond_24_bits(L, newest_first):      # noqa: F811
         v[row(place)] = 0.0
 
 
+def test_attend_a_batch_without_events_from_a_table(L):      # noqa: F811
+    """Targets that have no event at all, keys and values in a table of nodes: zeros."""
+    import torch
+    k, q, none = torch.full((50, 2, 8), float("nan"), device="cuda"), torch.ones((3, 4, 8), device="cuda"), torch.empty(0, device="cuda")
+    rowptr, index, t = torch.zeros(4, dtype=torch.int64, device="cuda"), none.int(), torch.ones(3, device="cuda")
+    table, edges = torch.ones((3, 4), device="cuda"), torch.tensor([1.0, 2.0], device="cuda")
+    assert not L.attend_run(rowptr, q, k, k, index=index)["out"].any()
+    assert not L.attend_run(rowptr, q, k, k, t=t, ts=none, edges=edges, table=table, index=index, mask=none.bool())["out"].any()
+    assert L.attend_run(rowptr[:1], q[:0], k, k, index=index)["out"].shape == (0, 4, 8)
+
+
 # ---- distillation: named candidates far above the others --------------------------------------------
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

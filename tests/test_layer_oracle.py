@@ -190,6 +190,12 @@ def test_attend_refuses_outputs():
     refused(B.TNS_EINVAL, L.tns_attend_grad, attend(buckets=0, d_table=None, d_edges=None), *ok)
 
 
+def test_no_events_of_a_table_of_nodes():
+    """Without a row, the index has no address: a table of nodes may be there all the same.  (Without lists nothing is launched.)"""
+    L.tns_attend_run(attend(S=0, rows=0, num=4, d_index=None), 0, 0, 0, 0)
+    refused(B.TNS_EINVAL, L.tns_attend_run, attend(S=0, rows=4, num=4, d_index=None), 0, 0, 256, BIG)
+
+
 def block(**kw):
     a = dict(rows=4, dim=8, dtype=0, flags=0, reserved=0, d_x=256, d_branch=256, d_gate=256, ld_x=8, ld_branch=8, ld_gate=8, d_scale=256, d_post=256, d_pre=256, eps=1e-6)
     a.update(kw)
