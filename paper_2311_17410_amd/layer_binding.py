@@ -1,7 +1,7 @@
 """ctypes binding of include/tns_layer.h (attention over event lists, what stands between two layers, distillation): same names, marshalling only.
 
 The functions without the prefix take torch tensors, as those of train_binding.py do: they check them, allocate what they return on the tensors'
-device and enqueue on its current stream.  They record nothing for autograd, and so refuse tensors that require gradients while it records (a
+device and enqueue on its current stream.  They record nothing for autograd, and so refuse tensors that require gradients while it records, and those with tangents (a
 torch.autograd.Function of the caller's may call them).
 """
 from __future__ import annotations

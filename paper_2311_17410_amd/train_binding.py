@@ -2,7 +2,7 @@
 
 The functions without the prefix take torch tensors: they check them, allocate what they return on the tensors' device and
 enqueue on its current stream.  Strides other than those of the last dimension are free where the C interface has them.
-They record nothing for autograd, and so refuse tensors that require gradients while it records (a torch.autograd.Function of the
+They record nothing for autograd, and so refuse tensors that require gradients while it records, and those with tangents (a torch.autograd.Function of the
 caller's may call them); what they change in place (a state table, weights) has its version raised, as by an operation of torch.
 """
 from __future__ import annotations
@@ -120,12 +120,17 @@ def tns_adamw_destroy(opt) -> None:
 # ---- the same on torch tensors ---------------------------------------------------------------------
 
 def _unrecorded(*tensors):
-    """Refuses what autograd would have to follow: the results would look like constants to it."""
+    """Refuses what autograd would have to follow, backwards or forwards: the results would look like constants to it."""
+    import torch
     for t in tensors:
         if t is not None and t.requires_grad:
-            import torch
             if torch.is_grad_enabled():
                 raise ValueError("nothing is recorded for autograd here: call under torch.no_grad(), within a torch.autograd.Function, or on detached tensors")
+    forward_ad = torch.autograd.forward_ad
+    if getattr(forward_ad, "_current_level", 0) >= 0:      # (the level is asked for first: outside of all of them no tensor has a tangent, and each takes 0.3 us to ask)
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("nothing is recorded for autograd here, tangents are not passed on: call within a torch.autograd.Function with a jvp, or on detached tensors")
 
 
 def _dtype_of(t):

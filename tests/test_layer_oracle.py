@@ -258,3 +258,38 @@ def test_tensors_off_the_gpu_or_that_require_gradients_are_refused():
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):
             call()
+
+
+def test_tensors_with_tangents_are_refused():
+    """Results without the tangents that they have would be constants to forward differentiation; a detached tensor has none, nor one within a Function."""
+    import torch
+    from torch.autograd import forward_ad
+    rp, ids = torch.tensor([0, 1, 2, 3, 4]), torch.zeros((4, 2), dtype=torch.int32)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(torch.zeros(4, 8), torch.ones(4, 8))
+        for call in calls(dual, rp, ids):
+            with pytest.raises(ValueError, match="tangents"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="tangents"):
+                call()
+        for call in calls(dual.detach(), rp, ids):
+            with pytest.raises(ValueError, match="on the GPU"):
+                call()
+
+        class Once(torch.autograd.Function):
+            @staticmethod
+            def forward(x):
+                for call in calls(x, rp, ids):
+                    with pytest.raises(ValueError, match="on the GPU"):
+                        call()
+                return 2 * x
+
+            @staticmethod
+            def setup_context(ctx, inputs, output):
+                pass
+
+            @staticmethod
+            def jvp(ctx, tangent):
+                return 2 * tangent
+
+        assert bool((forward_ad.unpack_dual(Once.apply(dual)).tangent == 2).all())

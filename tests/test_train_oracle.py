@@ -333,3 +333,42 @@ def test_an_8_bit_second_moment_is_high_by_its_roundings_variance():
             roots.append((r / np.sqrt(v)).mean())
     # single weights are off by 0.2, so their mean over 256 by 0.0125; four times that
     assert 1.0 < np.mean(squares) < 1.1 and abs(np.mean(roots) - 1.01) < 0.05, (np.mean(squares), np.mean(roots))
+
+
+def test_tensors_with_tangents_are_refused():
+    """Results without the tangents that they have would be constants to forward differentiation; a detached tensor has none, nor one within a Function."""
+    import torch
+    from torch.autograd import forward_ad
+    rp, ids, many = torch.zeros(2, dtype=torch.int64), torch.zeros(4, dtype=torch.int32), torch.zeros(4, 1, 8)
+
+    def calls(v):
+        return [lambda: T.recur_run(rp, v, v), lambda: T.recur_grad(rp, torch.zeros(4, 8), v, None), lambda: T.recur_step(ids, v, v, torch.zeros(4, 8)), lambda: T.pair_loss(v, v, many)]
+
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(torch.zeros(4, 8), torch.ones(4, 8))
+        for call in calls(dual):
+            with pytest.raises(ValueError, match="tangents"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="tangents"):
+                call()
+        for call in calls(dual.detach()):
+            with pytest.raises(ValueError, match="on the GPU"):
+                call()
+
+        class Once(torch.autograd.Function):
+            @staticmethod
+            def forward(x):
+                for call in calls(x):
+                    with pytest.raises(ValueError, match="on the GPU"):
+                        call()
+                return 2 * x
+
+            @staticmethod
+            def setup_context(ctx, inputs, output):
+                pass
+
+            @staticmethod
+            def jvp(ctx, tangent):
+                return 2 * tangent
+
+        assert bool((forward_ad.unpack_dual(Once.apply(dual)).tangent == 2).all())
