@@ -35,7 +35,7 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
     with tempfile.TemporaryDirectory() as at, ThreadPoolExecutor(min(os.cpu_count() or 1, 8)) as pool:
         objects = [os.path.join(at, s + ".o") for s in SOURCES]
         list(pool.map(lambda s, o: run([HIPCC] + flags + ["-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]), SOURCES, objects))
-        run([HIPCC] + FLAGS + objects + ["-o", tmp])
+        run([HIPCC] + FLAGS + (extra or []) + objects + ["-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 
