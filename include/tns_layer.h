@@ -89,7 +89,7 @@ TNS_API int tns_attend_grad(const tns_attend *a, const void *d_saved, const void
  *     out  = x + scale * sigmoid(gate) * post * norm(branch)
  *     next = pre * norm(out)                     (of out before it is rounded to T)
  * norm(v) = v / sqrt(mean(v^2) + eps), with TNS_CENTER of v - mean(v).  Without d_post the branch is taken as it is, without d_gate and
- * d_scale these factors are 1.
+ * d_scale these factors are 1.  Squares are summed in fp32: they hold for values up to 1e17, and without eps from 1e-17 on.
  *
  *   rows < 2^40, dim 1 .. 8192
  *   d_x, d_branch, d_gate   T [rows, dim] with ld; d_gate may be NULL

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import layer_oracle as O
-from test_gpu_layer import L, check_distill, on_gpu, the_events, the_scores      # noqa: F401
+from test_gpu_layer import L, check_block, check_distill, on_gpu, the_block, the_events, the_scores      # noqa: F401
 from test_gpu_train import BF16, F32, close, torch_of, values
 
 pytestmark = pytest.mark.gpu
@@ -239,3 +239,19 @@ def test_distill_teachers_far_from_zero(L, temperature, n, dtype):      # noqa: 
     r = L.distill(**{k: torch_of(v, dtype if k == "logits" else None) for k, v in a.items()}, temperature=temperature)
     close("rows", r["rows"], want["rows"], want["rows_off"])
     close("dlogits", r["dlogits"], want["dlogits"], want["dlogits_off"], dtype)
+
+
+# ---- between two layers: values far from 1 ---------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [2.0 ** 54, 2.0 ** -54])
+@pytest.mark.parametrize("without", [(), ("post",)])
+@pytest.mark.parametrize("center", [False, True])
+@pytest.mark.parametrize("dim", [20, 8192])
+def test_block_values_far_from_one(L, dim, center, without, size, dtype):      # noqa: F811
+    """Rows of the sizes that the header names, without eps."""
+    rng = np.random.default_rng(dim)
+    a = the_block(rng, 6, dim, dtype, **dict.fromkeys(without))
+    a["x"] *= np.float32(size)
+    a["branch"] *= np.float32(size)
+    check_block(L, a, dtype, values(rng, (6, dim), dtype), values(rng, (6, dim), dtype), center=center, eps=0.0)
