@@ -458,8 +458,8 @@ struct Work {
     float* tables;                      // [workgroups of the gradients, buckets * heads]
 };
 
-// What the gradients need of a list's softmax to have its p again: the largest score, in powers of two, and one over the sum of the others by it (0 where no
-// event counts).  The logarithm of the sum, added to the largest score, would be rounded to that one's last place: beside a table of -1e4 p
+// What the gradients need of a list's softmax to have its p again: the largest score, in powers of two, and one over the sum of exponentials by it (0 where
+// no event counts).  The logarithm of the sum, added to the largest score, would be rounded to that one's last place: beside a table of -1e4 p
 // would be off by 7e-4, beside one of -1e9 by any factor.
 struct Norm {
     float top, inverse;

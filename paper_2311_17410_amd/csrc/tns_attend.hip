@@ -73,7 +73,7 @@ struct Running {
 // lists gathered from a table, four heads of 32, 0.34 GB in 56 us (6.1); seven lists of 120000, eight heads of 64 on four, 0.81 GB in 156 us (5.2).
 // What it took: products of two bf16 pairs an instruction; the arguments read again where they are used; one event of every slot ahead rather than two
 // (fewer registers, seven waves instead of five: 63 -> 74 us); no more workgroups than fit (the others would start when these end); flags that the
-// compiler knows instead of branches, from behind which it waits for every request.  600 lists: 7.4 us, five reads one after the other.
+// compiler knows instead of branches, from behind which it waits for every request.  600 lists: 7.7 us, five reads one after the other.
 // GATHER: rows of k and v by their index; 2: looked up when it is needed to be known.
 template <typename T, int VEC, int G, int LANES, int GATHER>
 __global__ void __launch_bounds__(kWaves* kWave) k_attend(const Args<T>) {

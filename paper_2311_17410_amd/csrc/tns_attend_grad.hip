@@ -95,8 +95,10 @@ __device__ __forceinline__ void add_to_table(const Attend<T>& a, const Cut& cut,
 
 // One pass over k and v: the scores again, p from the largest and the sum that were saved, and all gradients of an event while its rows are in
 // registers.  ds = p (dp - delta) with dp = dout . v; delta = dout . out from outputs saved in fp32 (of bf16 ones the difference would keep their rounding,
-// and the table's gradient, in which most of it cancels, would show it).  Bound by memory: 131072 lists of ten, two heads of 64 bf16 channels, 1.35 GB in
-// 259 us (5.2 TB/s); 3001 histories, eight heads of 32 fp32 channels on four, 1.65 GB in 342 us (4.8).
+// and the table's gradient, in which most of it cancels, would show it).  Bound by memory: 131072 lists of ten, two heads of 64 bf16 channels, 1.36 GB in
+// 262 us (5.2 TB/s); 3001 histories, eight heads of 32 fp32 channels on four, 1.68 GB in 343 us (4.9).  Heads that share a key in fours and eights
+// are bound by instructions and by the few waves that their registers leave room for: 30000 lists of ten, eight heads of 64 bf16 channels on two, 0.42 GB
+// in 118 us (3.6 TB/s), on one, 0.29 GB in 220 (1.3).
 template <typename T, int VEC, int G, int LANES>
 __global__ void __launch_bounds__(kWaves* kWave) k_attend_grad(const Args<T>) {
     extern __shared__ float s_mem[];

@@ -136,7 +136,7 @@ struct Team {
     }
 };
 
-// Bound by memory: a million rows of 128 fp32 channels without a gate, 2.05 GB in 395 us (5.2 TB/s); 66600 of 172 bf16, 115 MB in 29 us (3.9): there
+// Bound by memory: a million rows of 128 fp32 channels without a gate, 2.05 GB in 395 us (5.2 TB/s); 66600 of 172 bf16, 116 MB in 29 us (4.0): there
 // the instructions of sums and gates are as many as memory leaves time for.
 template <typename T, int VEC, int G, int NV, bool GATE>
 __global__ void __launch_bounds__(G > 256 ? G : 256) k_block(const Block<T> b, T* out, T* next) {
@@ -190,8 +190,8 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) k_block(const Block<T> b, T
 
 // All gradients of a row while it is in registers; norms and gate are computed again.  Every lane adds up its channels' part of the
 // weights' gradients over the rows it sees: of scale and post the same sum, of (gradient by out) sigmoid(gate) norm(branch).
-// A gradient that is not there is read from x and not used.  A million rows of 128 fp32 channels, 3.07 GB in 622 us (4.9 TB/s); 66600 of 172 bf16,
-// 183 MB in 42 us (4.4).  The next row read ahead made it slower (645 us: fewer waves), as did more workgroups.
+// A gradient that is not there is read from x and not used.  A million rows of 128 fp32 channels, 3.07 GB in 611 us (5.0 TB/s); 66600 of 172 bf16,
+// 185 MB in 41 us (4.5).  The next row read ahead made it slower (5 %: fewer waves), as did more workgroups.
 template <typename T, int VEC, int G, int NV, bool GATE>
 __global__ void __launch_bounds__(G > 256 ? G : 256) k_block_grad(const Block<T> b, const T* dout, int64_t ld_dout, const T* dnext, int64_t ld_dnext, T* dx, T* dbranch, T* dgate, float* shares) {
     using Rows = Team<T, VEC, G, NV>;

@@ -251,10 +251,11 @@ struct Names {
 };
 
 // A whole row in a workgroup's registers: read once, written once.  Bound by memory where there are many rows: 4000 of 10000 bf16 scores with
-// fifty ids, 160 MB in 34 us (4.7 TB/s); with 1024 threads to a row, a bit looked up for every score and bounds checked at every use it was 126 us,
-// bound by instructions.  600 rows of 1000 fp32 scores: 4.9 us, four waits one after the other.  REST: the scores that no id names are added up by themselves (what is left
-// of the sum over all without the named ones would lose them where they are few): the row lies in LDS too, the named ones are crossed
-// out there, and the threads take their values from it again.
+// fifty ids, 161 MB in 31 us (5.2 TB/s); with 1024 threads to a row, a bit looked up for every score and bounds checked at every use it was 126 us,
+// bound by instructions.  600 rows of 1000 fp32 scores: 4.6 us, four waits one after the other.  REST: the scores that no id names are added up by themselves (what is left
+// of the sum over all without the named ones would lose them where they are few) and by their own largest: the row lies in LDS too, the named ones are
+// crossed out there, and the threads take their values from it again (one exchange more: a call of 50000 rows of 50 fp32
+// scores 34 -> 37 us, one of 4000 rows of 10000 bf16 scores 37 -> 34).
 template <typename T, int THREADS, int NV, bool REST>
 __global__ void __launch_bounds__(THREADS) k_distill_row(const Distill<T> d, float* rows, T* dlogits) {
     using H = Held<T, THREADS, NV>;
@@ -502,7 +503,7 @@ int launch(const tns_distill_desc& a, float* loss, float* rows, T* dlogits, void
         const unsigned pieces = (unsigned)pieces_of<T>(a.V), written = dlogits ? pieces : 1;
         // Scores beyond the last-level cache (256 MiB) go through in parts that it holds: the second kernel finds there what the first has
         // read, and writes past it.  200 rows of 500009 fp32 scores, 400 MB: 241 us at once, 225 with the hint on the stores, 213 in parts of
-        // 192 MiB, 228 of 96, 266 of 48 (without the hint 251, 246, 278).
+        // 192 MiB (now 214), 228 of 96, 266 of 48 (without the hint 251, 246, 278).
         const size_t bytes = (size_t)a.B * a.V * sizeof(T);
         const int64_t parts = bytes > size_t(256) << 20 ? (int64_t)(bytes / (size_t(192) << 20)) + 1 : 1;
         const int64_t most = std::max<int64_t>(std::min((a.B + parts - 1) / parts, ((int64_t)1 << 31) / kThreads / pieces), 1);
